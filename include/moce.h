@@ -357,6 +357,123 @@ moce_status moce_logit_backward(int32_t R, int64_t C, int32_t k, const float* L,
                                 float eps, float lambda, float* loss, float* dL, void* ws, size_t ws_bytes,
                                 hipStream_t stream);
 
+/* ---- dense pointwise projections ------------------------------------------
+ *
+ * The projections of a network that stay dense beside its channel-expert
+ * layers: the expansion that closes a bottleneck, the token projections of a
+ * transformer block.  With v[o][p] = sum_c weight[o][c] x[c][p] at position p,
+ *   z[o][p] = scale[o] v[o][p] + shift[o] + residual[o][p],   y = act(z);
+ * scale, shift and residual are optional (NULL: 1, 0, 0). */
+
+/* Activations: z; max(z, 0); z (1 + erf(z / sqrt 2)) / 2; z / (1 + e^-z).
+ * A NaN stays one, and infinities give the limits. */
+enum { MOCE_ACT_NONE = 0, MOCE_ACT_RELU = 1, MOCE_ACT_GELU = 2, MOCE_ACT_SILU = 3 };
+
+typedef struct moce_project_desc {
+    int64_t B, C, H, W;   /* x is B images of C channels over H*W positions */
+    int64_t O;            /* output channels, any number >= 1 */
+    int32_t dtype;        /* of x, weight, residual, y, z and their gradients: MOCE_F32 or MOCE_BF16 */
+    int32_t layout;       /* MOCE_NCHW or MOCE_NHWC, of x and y alike */
+    int32_t act;          /* MOCE_ACT_* */
+    int32_t reserved;     /* set to 0 */
+} moce_project_desc;
+
+/* Bytes of device workspace moce_project needs (0: none, or an invalid
+ * descriptor).  It holds the partial products of shapes with few outputs,
+ * whose contraction is divided. */
+size_t moce_project_workspace_bytes(const moce_project_desc* desc);
+
+/* The projection.  x, residual, y, z: tensors of the descriptor's layout (C
+ * channels for x, O for the others), weight: [O][C] row-major, all of the
+ * descriptor's type, contiguous and 16-byte aligned; scale, shift: float32
+ * [O].  y is fully overwritten, and so is z where it is given (the
+ * pre-activation that moce_project_backward reads, rounded to the type; y
+ * itself comes from the unrounded one).  residual may be y or z (in place);
+ * y, z and the other inputs may not overlap.  Sums are float32.
+ * ws: as sized above, 256-byte aligned, contents on return unspecified; may
+ * be NULL where no bytes are needed.  Asynchronous on `stream`.
+ * Errors: MOCE_ERR_NULL (desc, x, weight, y), MOCE_ERR_SHAPE (a size below 1,
+ * an unknown act, z == y), MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN,
+ * MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED when C or O
+ * exceeds 2^20, B H W 2^29, C H W or O H W 2^31 - 1, or B C H W or B O H W
+ * 2^33. */
+moce_status moce_project(const moce_project_desc* desc, const void* x, const void* weight, const float* scale,
+                         const float* shift, const void* residual, void* y, void* z, void* ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* Gradients of moce_project, each optional (NULL: not computed) and fully
+ * overwritten:
+ *   dz = act'(z) dy;                      dresidual = dz;
+ *   dshift[o] = sum_p dz[o][p];           G[o][c] = sum_p dz[o][p] x[c][p];
+ *   dweight[o][c] = scale[o] G[o][c];     dscale[o] = sum_c weight[o][c] G[o][c];
+ *   dx[c][p] = sum_o scale[o] weight[o][c] dz[o][p]. */
+typedef struct moce_project_grads {
+    void* dx;             /* layout and type of x */
+    void* dweight;        /* [O][C], type of weight */
+    float* dscale;        /* [O]; needs scale; only for MOCE_ACT_NONE and MOCE_ACT_RELU */
+    float* dshift;        /* [O] */
+    void* dresidual;      /* layout and type of y */
+} moce_project_grads;
+
+/* Bytes of device workspace moce_project_backward needs (0 on an invalid
+ * descriptor). */
+size_t moce_project_backward_workspace_bytes(const moce_project_desc* desc);
+
+/* The gradients of moce_project for an upstream gradient dy of y (layout and
+ * type of y).  x, weight, scale as in the forward; z: the pre-activation that
+ * the forward wrote (for MOCE_ACT_RELU its y serves as well; not read for
+ * MOCE_ACT_NONE).  act' of ReLU is 0 where z <= 0.  All tensors contiguous
+ * and 16-byte aligned; dresidual may be dy (in place), no other output may
+ * overlap an input or another output.  For bfloat16, dz enters the products
+ * rounded to its type (exact for MOCE_ACT_NONE and MOCE_ACT_RELU), and so does
+ * the scaled weight of dx; sums are float32.  ws as sized above, 256-byte
+ * aligned.  Errors: those of moce_project; MOCE_ERR_NULL for a missing dy or
+ * z, or dscale without scale; MOCE_ERR_UNSUPPORTED for dscale with
+ * MOCE_ACT_GELU or MOCE_ACT_SILU.  Asynchronous on `stream`. */
+moce_status moce_project_backward(const moce_project_desc* desc, const void* x, const void* weight,
+                                  const float* scale, const void* z, const void* dy,
+                                  const moce_project_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- the global norm of a list of gradients, and clipping ------------------ */
+
+/* One gradient: n elements of `dtype` at src (aligned to its element; n == 0
+ * is allowed).  dst: where the clipped gradient goes, src itself or memory
+ * that overlaps no tensor of the list (not read by moce_gradient_norm). */
+typedef struct moce_gradient {
+    const void* src;
+    void* dst;
+    int64_t n;
+    int32_t dtype;        /* MOCE_F32 or MOCE_BF16 */
+    int32_t reserved;     /* set to 0 */
+} moce_gradient;
+
+/* Bytes of device workspace the two calls below need for this list (0 on an
+ * invalid one). */
+size_t moce_gradient_workspace_bytes(const moce_gradient* grads, int32_t count);
+
+/* *norm (device float) = sqrt(sum over all tensors and elements of g^2),
+ * accumulated in float64: no square of a float32 overflows or is lost.  The
+ * list is host memory, read before the call returns; count == 0 gives 0.  The
+ * order of the sum depends on the sizes alone: the same gradients give the
+ * same bits.  Errors: MOCE_ERR_NULL (norm, the list, a tensor's src with
+ * n > 0), MOCE_ERR_SHAPE (count < 0, n < 0), MOCE_ERR_DTYPE, MOCE_ERR_ALIGN,
+ * MOCE_ERR_WORKSPACE; MOCE_ERR_UNSUPPORTED when the sizes sum to over 2^40.
+ * Asynchronous on `stream`. */
+moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float* norm, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+/* moce_gradient_norm, then dst = src * (max_norm / norm) where norm >
+ * max_norm, else dst = src (nothing is written for dst == src).  The
+ * coefficient is formed on the device: no synchronisation.  A norm that is
+ * not finite leaves every gradient as it is (*norm tells).  Products are
+ * float32, rounded to the tensor's type.  *norm is the norm before clipping.
+ * Errors: those of moce_gradient_norm; MOCE_ERR_NULL for a missing dst;
+ * MOCE_ERR_SHAPE when max_norm is negative or not finite, when two tensors
+ * overlap (a tensor listed twice would be scaled twice), or when a dst
+ * overlaps any src but its own, or its own partly. */
+moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float max_norm, float* norm, void* ws,
+                               size_t ws_bytes, hipStream_t stream);
+
 /* Static string naming a status code. */
 const char* moce_status_str(int status);
 

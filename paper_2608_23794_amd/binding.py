@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(HERE, "libmoce.so")
 MOCE_F32, MOCE_BF16 = 0, 1
 MOCE_NCHW, MOCE_NHWC = 0, 1
 MOCE_GATE_SOFTPLUS_LINEAR, MOCE_GATE_MLP_SIGMOID = 0, 1
+MOCE_ACT_NONE, MOCE_ACT_RELU, MOCE_ACT_GELU, MOCE_ACT_SILU = 0, 1, 2, 3
 
 STATUS = {
     0: "MOCE_OK", -1: "MOCE_ERR_NULL", -2: "MOCE_ERR_SHAPE", -3: "MOCE_ERR_DTYPE",
@@ -31,8 +32,9 @@ ENTRY_POINTS = (
     "moce_support_prepare", "moce_support_prepare16", "moce_pool", "moce_gate", "moce_gate_mix", "moce_mix",
     "moce_forward_workspace_bytes", "moce_forward_path", "moce_forward", "moce_forward_ex", "moce_forward_static",
     "moce_forward_dynamic_workspace_bytes", "moce_forward_dynamic", "moce_backward_workspace_bytes",
-    "moce_backward", "moce_logit_backward_workspace_bytes", "moce_logit_backward", "moce_status_str",
-    "moce_abi_version",
+    "moce_backward", "moce_logit_backward_workspace_bytes", "moce_logit_backward", "moce_project_workspace_bytes",
+    "moce_project", "moce_project_backward_workspace_bytes", "moce_project_backward", "moce_gradient_workspace_bytes",
+    "moce_gradient_norm", "moce_gradient_clip", "moce_status_str", "moce_abi_version",
 )
 
 MOCE_STATIC_SCRATCH_BYTES = 16 << 20
@@ -71,6 +73,22 @@ class moce_epilogue(ctypes.Structure):
 class moce_gate_grads(ctypes.Structure):
     _fields_ = [("da", ctypes.c_void_p), ("dc", ctypes.c_void_p), ("dW1", ctypes.c_void_p),
                 ("db1", ctypes.c_void_p), ("dw2", ctypes.c_void_p), ("db2", ctypes.c_void_p)]
+
+
+class moce_project_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("C", ctypes.c_int64), ("H", ctypes.c_int64), ("W", ctypes.c_int64),
+                ("O", ctypes.c_int64), ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class moce_project_grads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p), ("dscale", ctypes.c_void_p),
+                ("dshift", ctypes.c_void_p), ("dresidual", ctypes.c_void_p)]
+
+
+class moce_gradient(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -112,11 +130,24 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_logit_backward_workspace_bytes.restype = SZ
     lib.moce_logit_backward.argtypes = [I32, ctypes.c_int64, I32, P, P, P, ctypes.c_float, ctypes.c_float, P, P,
                                         P, SZ, P]
+    J = ctypes.POINTER(moce_project_desc)
+    lib.moce_project_workspace_bytes.argtypes = [J]
+    lib.moce_project_workspace_bytes.restype = SZ
+    lib.moce_project.argtypes = [J, P, P, P, P, P, P, P, P, SZ, P]
+    lib.moce_project_backward_workspace_bytes.argtypes = [J]
+    lib.moce_project_backward_workspace_bytes.restype = SZ
+    lib.moce_project_backward.argtypes = [J, P, P, P, P, P, ctypes.POINTER(moce_project_grads), P, SZ, P]
+    # the list as an address: an array of moce_gradient, or memory laid out the same
+    lib.moce_gradient_workspace_bytes.argtypes = [P, I32]
+    lib.moce_gradient_workspace_bytes.restype = SZ
+    lib.moce_gradient_norm.argtypes = [P, I32, P, P, SZ, P]
+    lib.moce_gradient_clip.argtypes = [P, I32, ctypes.c_float, P, P, SZ, P]
     lib.moce_status_str.argtypes = [ctypes.c_int]
     lib.moce_status_str.restype = ctypes.c_char_p
     lib.moce_abi_version.restype = ctypes.c_int
     for name in ("moce_support_prepare", "moce_support_prepare16", "moce_pool", "moce_gate", "moce_gate_mix", "moce_mix", "moce_forward", "moce_forward_ex",
-                 "moce_forward_static", "moce_forward_dynamic", "moce_backward", "moce_logit_backward"):
+                 "moce_forward_static", "moce_forward_dynamic", "moce_backward", "moce_logit_backward",
+                 "moce_project", "moce_project_backward", "moce_gradient_norm", "moce_gradient_clip"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -288,6 +319,61 @@ def moce_logit_backward(R: int, C: int, k: int, L, s, dw, eps: float, lam: float
     _check("moce_logit_backward", load().moce_logit_backward(int(R), int(C), int(k), _ptr(L), _ptr(s), _ptr(dw),
                                                              float(eps), float(lam), _ptr(loss), _ptr(dL),
                                                              _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_project_desc(B: int, C: int, H: int, W: int, O: int, dtype: int, layout: int,
+                      act: int = MOCE_ACT_NONE) -> moce_project_desc:
+    return moce_project_desc(B, C, H, W, O, dtype, layout, act, 0)
+
+
+def moce_project_workspace_bytes(desc: moce_project_desc) -> int:
+    return load().moce_project_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_project(desc: moce_project_desc, x, weight, scale, shift, residual, y, z, ws, ws_bytes: int,
+                 stream=None) -> None:
+    _check("moce_project", load().moce_project(ctypes.byref(desc), _ptr(x), _ptr(weight), _ptr(scale), _ptr(shift),
+                                               _ptr(residual), _ptr(y), _ptr(z), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_project_grads(dx=None, dweight=None, dscale=None, dshift=None, dresidual=None) -> moce_project_grads:
+    """The gradients to compute, device arrays that outlive its use (None: not computed)."""
+    return moce_project_grads(_ptr(dx), _ptr(dweight), _ptr(dscale), _ptr(dshift), _ptr(dresidual))
+
+
+def moce_project_backward_workspace_bytes(desc: moce_project_desc) -> int:
+    return load().moce_project_backward_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_project_backward(desc: moce_project_desc, x, weight, scale, z, dy, grads: moce_project_grads, ws,
+                          ws_bytes: int, stream=None) -> None:
+    _check("moce_project_backward", load().moce_project_backward(ctypes.byref(desc), _ptr(x), _ptr(weight),
+                                                                 _ptr(scale), _ptr(z), _ptr(dy), ctypes.byref(grads),
+                                                                 _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_gradients(tensors, out=None):
+    """The list of gradients for moce_gradient_norm and moce_gradient_clip: float32 or bfloat16 torch tensors, and
+    where the clipped ones go (None: in place)."""
+    arr = (moce_gradient * max(1, len(tensors)))()
+    for g, t, d in zip(arr, tensors, tensors if out is None else out):
+        g.src, g.dst, g.n = t.data_ptr(), d.data_ptr(), t.numel()
+        g.dtype = MOCE_F32 if t.element_size() == 4 else MOCE_BF16
+    return arr
+
+
+def moce_gradient_workspace_bytes(grads, count: int) -> int:
+    return load().moce_gradient_workspace_bytes(ctypes.addressof(grads), count)
+
+
+def moce_gradient_norm(grads, count: int, norm, ws, ws_bytes: int, stream=None) -> None:
+    _check("moce_gradient_norm", load().moce_gradient_norm(ctypes.addressof(grads), count, _ptr(norm), _ptr(ws),
+                                                           ws_bytes, _stream(stream)))
+
+
+def moce_gradient_clip(grads, count: int, max_norm: float, norm, ws, ws_bytes: int, stream=None) -> None:
+    _check("moce_gradient_clip", load().moce_gradient_clip(ctypes.addressof(grads), count, max_norm, _ptr(norm),
+                                                           _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def raw_status(fn: str, *args) -> int:

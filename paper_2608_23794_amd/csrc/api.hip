@@ -1,11 +1,14 @@
 // C ABI of libmoce: host-side validation, workspace layout and dispatch to
-// the kernels of prepare.hip, pool.hip, gate.hip and mix.hip.  Every check that
+// the kernels of the other files.  Every check that
 // can fail on the host runs before anything is enqueued.
 #include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstring>
 #include <mutex>
+#include <new>
+#include <utility>
+#include <vector>
 
 #include "moce_internal.h"
 
@@ -577,6 +580,174 @@ moce_status moce_logit_backward(int32_t R, int64_t C, int32_t k, const float* L,
   if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
   return device_status(moce::launch_logit_backward(R, (int)C, k, L, s, dw, eps, lambda, loss, dL,
                                                    static_cast<float*>(ws), stream));
+}
+
+// ---- dense projections ---------------------------------------------------------
+
+namespace {
+
+moce_status check_project(const moce_project_desc* d, moce::ProjectShape* s) {
+  if (!d) return MOCE_ERR_NULL;
+  if (d->B < 1 || d->C < 1 || d->H < 1 || d->W < 1 || d->O < 1) return MOCE_ERR_SHAPE;
+  if (d->act < MOCE_ACT_NONE || d->act > MOCE_ACT_SILU) return MOCE_ERR_SHAPE;
+  if (d->dtype != MOCE_F32 && d->dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
+  if (d->layout != MOCE_NCHW && d->layout != MOCE_NHWC) return MOCE_ERR_LAYOUT;
+  if (d->H > INT_MAX / d->W) return MOCE_ERR_UNSUPPORTED;
+  s->B = d->B;
+  s->C = d->C;
+  s->HW = d->H * d->W;
+  s->O = d->O;
+  s->elem = d->dtype;
+  s->layout = s->HW == 1 ? MOCE_NHWC : d->layout;   // the same memory
+  s->act = d->act;
+  return moce::project_limits(*s) ? MOCE_OK : MOCE_ERR_UNSUPPORTED;
+}
+
+struct ProjectBwdLayout {
+  size_t dz, weight, shift, part, total;
+};
+ProjectBwdLayout project_bwd_layout(const moce::ProjectShape& s) {
+  const moce::ProjectBwdSizes z = moce::project_backward_sizes(s);
+  ProjectBwdLayout l{};
+  l.dz = 0;
+  l.weight = l.dz + round_up(z.dz);
+  l.shift = l.weight + round_up(z.weight);
+  l.part = l.shift + round_up(z.shift);
+  l.total = l.part + round_up(z.part);
+  return l;
+}
+
+}  // namespace
+
+size_t moce_project_workspace_bytes(const moce_project_desc* desc) {
+  moce::ProjectShape s;
+  if (check_project(desc, &s) != MOCE_OK) return 0;
+  return round_up(moce::project_ws_bytes(s));
+}
+
+moce_status moce_project(const moce_project_desc* desc, const void* x, const void* weight, const float* scale,
+                         const float* shift, const void* residual, void* y, void* z, void* ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  moce::ProjectShape s;
+  const moce_status st = check_project(desc, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !weight || !y) return MOCE_ERR_NULL;
+  if (z == y) return MOCE_ERR_SHAPE;
+  if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(y, 16) || !aligned(residual, 16) || !aligned(z, 16) ||
+      !aligned(scale, 4) || !aligned(shift, 4))
+    return MOCE_ERR_ALIGN;
+  const size_t need = moce::project_ws_bytes(s);
+  if (need > 0 && (!ws || ws_bytes < need)) return MOCE_ERR_WORKSPACE;
+  if (need > 0 && !aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  return device_status(moce::launch_project(s, x, weight, scale, shift, residual, y, z, ws, stream));
+}
+
+size_t moce_project_backward_workspace_bytes(const moce_project_desc* desc) {
+  moce::ProjectShape s;
+  if (check_project(desc, &s) != MOCE_OK) return 0;
+  return project_bwd_layout(s).total;
+}
+
+moce_status moce_project_backward(const moce_project_desc* desc, const void* x, const void* weight,
+                                  const float* scale, const void* z, const void* dy,
+                                  const moce_project_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream) {
+  moce::ProjectShape s;
+  const moce_status st = check_project(desc, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !weight || !dy || !grads || (s.act != MOCE_ACT_NONE && !z)) return MOCE_ERR_NULL;
+  if (grads->dscale && !scale) return MOCE_ERR_NULL;
+  if (grads->dscale && s.act != MOCE_ACT_NONE && s.act != MOCE_ACT_RELU) return MOCE_ERR_UNSUPPORTED;
+  if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(dy, 16) || !aligned(z, 16) || !aligned(grads->dx, 16) ||
+      !aligned(grads->dweight, 16) || !aligned(grads->dresidual, 16) || !aligned(scale, 4) ||
+      !aligned(grads->dscale, 4) || !aligned(grads->dshift, 4))
+    return MOCE_ERR_ALIGN;
+  const ProjectBwdLayout l = project_bwd_layout(s);
+  if (!ws || ws_bytes < l.total) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  char* base = static_cast<char*>(ws);
+  const moce::ProjectBwdWs w{base + l.dz, base + l.weight, reinterpret_cast<float*>(base + l.shift),
+                             reinterpret_cast<float*>(base + l.part)};
+  return device_status(moce::launch_project_backward(s, x, weight, scale, z, dy, *grads, w, stream));
+}
+
+// ---- gradient norm and clipping --------------------------------------------------
+
+namespace {
+
+moce_status check_gradients(const moce_gradient* g, int32_t count) {
+  if (count < 0) return MOCE_ERR_SHAPE;
+  if (count > 0 && !g) return MOCE_ERR_NULL;
+  int64_t total = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (g[i].n < 0) return MOCE_ERR_SHAPE;
+    if (g[i].dtype != MOCE_F32 && g[i].dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
+    if (g[i].n > ((int64_t)1 << 40) - total) return MOCE_ERR_UNSUPPORTED;
+    total += g[i].n;
+    if (g[i].n == 0) continue;
+    if (!g[i].src) return MOCE_ERR_NULL;
+    if (!aligned(g[i].src, g[i].dtype == MOCE_F32 ? 4 : 2)) return MOCE_ERR_ALIGN;
+  }
+  return MOCE_OK;
+}
+
+// Whether the list's memory ranges, sources and destinations of their own, are apart.
+bool ranges_apart(const moce_gradient* g, int32_t count) {
+  auto bytes = [&](int32_t i) { return (uintptr_t)g[i].n * (g[i].dtype == MOCE_F32 ? 4 : 2); };
+  std::vector<std::pair<uintptr_t, uintptr_t>> r;
+  r.reserve((size_t)2 * count);
+  for (int32_t i = 0; i < count; ++i) {
+    if (g[i].n == 0) continue;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(g[i].src), d = reinterpret_cast<uintptr_t>(g[i].dst);
+    r.emplace_back(a, a + bytes(i));
+    if (d != a) r.emplace_back(d, d + bytes(i));
+  }
+  if (!std::is_sorted(r.begin(), r.end())) std::sort(r.begin(), r.end());
+  for (size_t i = 1; i < r.size(); ++i)
+    if (r[i].first < r[i - 1].second) return false;
+  return true;
+}
+
+moce_status check_gradient_ws(const moce_gradient* g, int32_t count, const float* norm, const void* ws,
+                              size_t ws_bytes) {
+  if (!norm) return MOCE_ERR_NULL;
+  if (!aligned(norm, 4)) return MOCE_ERR_ALIGN;
+  if (!ws || ws_bytes < moce::gradient_ws_bytes(g, count)) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  return MOCE_OK;
+}
+
+}  // namespace
+
+size_t moce_gradient_workspace_bytes(const moce_gradient* grads, int32_t count) {
+  if (check_gradients(grads, count) != MOCE_OK) return 0;
+  return round_up(moce::gradient_ws_bytes(grads, count));
+}
+
+moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float* norm, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  moce_status st = check_gradients(grads, count);
+  if (st == MOCE_OK) st = check_gradient_ws(grads, count, norm, ws, ws_bytes);
+  if (st != MOCE_OK) return st;
+  return device_status(moce::launch_gradient_norm(grads, count, norm, ws, stream));
+}
+
+moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float max_norm, float* norm, void* ws,
+                               size_t ws_bytes, hipStream_t stream) {
+  moce_status st = check_gradients(grads, count);
+  if (st == MOCE_OK) st = check_gradient_ws(grads, count, norm, ws, ws_bytes);
+  if (st != MOCE_OK) return st;
+  if (!std::isfinite(max_norm) || max_norm < 0.f) return MOCE_ERR_SHAPE;
+  for (int32_t i = 0; i < count; ++i) {
+    if (grads[i].n == 0) continue;
+    if (!grads[i].dst) return MOCE_ERR_NULL;
+    if (!aligned(grads[i].dst, grads[i].dtype == MOCE_F32 ? 4 : 2)) return MOCE_ERR_ALIGN;
+  }
+  try {
+    if (!ranges_apart(grads, count)) return MOCE_ERR_SHAPE;
+  } catch (const std::bad_alloc&) {
+    return MOCE_ERR_UNSUPPORTED;   // no exception leaves a C entry point
+  }
+  return device_status(moce::launch_gradient_clip(grads, count, max_norm, norm, ws, stream));
 }
 
 }  // extern "C"

@@ -299,4 +299,33 @@ bool logit_backward_supported(int64_t C);
 hipError_t launch_logit_backward(int R, int C, int k, const float* L, const int32_t* s, const float* dw, float eps,
                                  float lambda, float* loss, float* dL, float* ws, hipStream_t st);
 
+// Dense projections and their gradients (project.hip).  One position an image
+// is channels-last in either layout: the caller passes MOCE_NHWC for HW = 1.
+struct ProjectShape {
+  int64_t B, C, HW, O;
+  int elem, layout, act;
+};
+bool project_limits(const ProjectShape& s);
+size_t project_ws_bytes(const ProjectShape& s);   // partial products, 0 where the contraction is not divided
+hipError_t launch_project(const ProjectShape& s, const void* x, const void* w, const float* scale, const float* shift,
+                          const void* res, void* y, void* z, void* ws, hipStream_t st);
+// Workspace of the backward: dz, the scaled weight, the groups' sums of dz, partial products (bytes).
+struct ProjectBwdSizes {
+  size_t dz, weight, shift, part;
+};
+struct ProjectBwdWs {
+  void *dz, *weight;
+  float *shift, *part;
+};
+ProjectBwdSizes project_backward_sizes(const ProjectShape& s);
+hipError_t launch_project_backward(const ProjectShape& s, const void* x, const void* w, const float* scale,
+                                   const void* z, const void* dy, const moce_project_grads& gr,
+                                   const ProjectBwdWs& ws, hipStream_t st);
+
+// The norm of a list of gradients and their clipping (gradclip.hip), over a validated list.
+size_t gradient_ws_bytes(const moce_gradient* g, int count);
+hipError_t launch_gradient_norm(const moce_gradient* g, int count, float* norm, void* ws, hipStream_t st);
+hipError_t launch_gradient_clip(const moce_gradient* g, int count, float max_norm, float* norm, void* ws,
+                                hipStream_t st);
+
 }  // namespace moce

@@ -3,12 +3,17 @@
 ``MoceLayer`` owns the device copies of a layer's parameters (support rows,
 selected logits, gate parameters), prepares the supports once with
 ``moce_support_prepare`` and then forwards batches with ``moce_forward`` or
-the individual ``moce_pool`` / ``moce_gate`` / ``moce_mix`` calls.  Torch
+the individual ``moce_pool`` / ``moce_gate`` / ``moce_mix`` calls.
+``ProjectLayer`` is a dense projection beside it (``moce_project`` and its
+backward), and ``gradient_norm`` / ``clip_gradients`` take the global norm of
+the gradients of both (``moce_gradient_norm`` / ``moce_gradient_clip``).  Torch
 provides device memory and the current stream; every step of the layer runs in
 libmoce's HIP kernels.
 """
 from __future__ import annotations
 
+import contextlib
+import math
 from typing import Optional
 
 import numpy as np
@@ -266,6 +271,167 @@ class DynamicMoceLayer:
         mb.moce_forward_dynamic(self.desc(B), x, self.L, self.router, self.gate, y, S_out, ws, ws.numel(),
                                 torch.cuda.current_stream())
         return y
+
+
+_ACT = {"none": mb.MOCE_ACT_NONE, "relu": mb.MOCE_ACT_RELU, "gelu": mb.MOCE_ACT_GELU, "silu": mb.MOCE_ACT_SILU}
+_DTYPE_OF = {torch.float32: mb.MOCE_F32, torch.bfloat16: mb.MOCE_BF16}
+
+
+def _on(device):
+    """The device as the current one, which the library launches on."""
+    return torch.cuda.device(device) if torch.cuda.current_device() != device.index else contextlib.nullcontext()
+
+
+def _need(name: str, t: torch.Tensor, shape, dtype, device):
+    """Raises unless t is a contiguous tensor of this shape, type and device: the library sees only its address."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', strided'}")
+
+
+class ProjectLayer:
+    """A dense pointwise projection: y = act(scale x W^T + shift + residual) over the channels.
+
+    weight: [O, C], float32 or bfloat16, on the GPU; scale and shift: float32 [O] or None; act: "none", "relu",
+    "gelu" or "silu".  x: [B, C, H, W] for layout "nchw"; [..., C] for "nhwc" (images, tokens or rows).  The layer
+    keeps the tensors it is given: updating them in place updates the layer."""
+
+    def __init__(self, weight: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                 shift: Optional[torch.Tensor] = None, act: str = "none", layout: str = "nhwc"):
+        if act not in _ACT or layout not in _LAYOUT:
+            raise ValueError(f"act {act!r}, layout {layout!r}")
+        if weight.dim() != 2 or weight.dtype not in _DTYPE_OF or not weight.is_cuda:
+            raise ValueError(f"weight has to be a float32 or bfloat16 [O, C] tensor on the GPU, got {weight.dtype} "
+                             f"{tuple(weight.shape)} on {weight.device}")
+        self.O, self.C = weight.shape
+        self.dtype, self.device = weight.dtype, weight.device
+        _need("weight", weight, weight.shape, self.dtype, self.device)
+        for name, t in (("scale", scale), ("shift", shift)):
+            if t is not None:
+                _need(name, t, (self.O,), torch.float32, self.device)
+        self.weight, self.scale, self.shift, self.act, self.layout = weight, scale, shift, act, layout
+
+    def y_shape(self, x_shape):
+        if self.layout == "nchw":
+            return (x_shape[0], self.O) + tuple(x_shape[2:])
+        return tuple(x_shape[:-1]) + (self.O,)
+
+    def desc(self, x_shape) -> mb.moce_project_desc:
+        """The call's descriptor for an x of this shape."""
+        s = x_shape
+        if self.layout == "nchw":
+            if len(s) != 4 or s[1] != self.C:
+                raise ValueError(f"x has to be [B, {self.C}, H, W], got {tuple(s)}")
+            B, H, W = s[0], s[2], s[3]
+        else:
+            if len(s) < 2 or s[-1] != self.C:
+                raise ValueError(f"x has to be [..., {self.C}], got {tuple(s)}")
+            B, H, W = s[0], math.prod(s[1:-1]), 1
+        return mb.moce_project_desc(B, self.C, H, W, self.O, _DTYPE_OF[self.dtype], _LAYOUT[self.layout],
+                                    _ACT[self.act], 0)
+
+    def workspace_bytes(self, x_shape) -> int:
+        return mb.moce_project_workspace_bytes(self.desc(x_shape))
+
+    def backward_workspace_bytes(self, x_shape) -> int:
+        return mb.moce_project_backward_workspace_bytes(self.desc(x_shape))
+
+    def _workspace(self, n: int, ws: Optional[torch.Tensor]):
+        if ws is not None:
+            return ws, ws.numel() * ws.element_size()
+        return (torch.empty(n, dtype=torch.uint8, device=self.device) if n else None), n
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                z: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """moce_project.  z, where given, receives the pre-activation that the backward needs."""
+        desc, shape = self.desc(x.shape), self.y_shape(x.shape)
+        _need("x", x, x.shape, self.dtype, self.device)
+        if y is None:
+            y = torch.empty(shape, dtype=self.dtype, device=self.device)
+        for name, t in (("residual", residual), ("y", y), ("z", z)):
+            if t is not None:
+                _need(name, t, shape, self.dtype, self.device)
+        if x.numel() == 0:
+            return y
+        with _on(self.device):
+            ws, n = self._workspace(mb.moce_project_workspace_bytes(desc), ws)
+            mb.moce_project(desc, x, self.weight, self.scale, self.shift, residual, y, z, ws, n,
+                            torch.cuda.current_stream(self.device))
+        return y
+
+    def backward(self, x: torch.Tensor, dy: torch.Tensor, z: Optional[torch.Tensor] = None, residual: bool = False,
+                 dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> dict:
+        """moce_project_backward: dx, dweight, dscale and dshift where the layer has them (no dscale with "gelu"
+        and "silu"), and with residual=True dresidual."""
+        desc, shape = self.desc(x.shape), self.y_shape(x.shape)
+        f32, dev = torch.float32, self.device
+        _need("x", x, x.shape, self.dtype, dev)
+        _need("dy", dy, shape, self.dtype, dev)
+        if self.act != "none":
+            if z is None:
+                raise ValueError(f"the backward of {self.act!r} needs the pre-activation z")
+            _need("z", z, shape, self.dtype, dev)
+        if dx is None:
+            dx = torch.empty_like(x)
+        _need("dx", dx, x.shape, self.dtype, dev)
+        out = {"dx": dx, "dweight": torch.empty_like(self.weight)}
+        if self.scale is not None and self.act in ("none", "relu"):
+            out["dscale"] = torch.empty(self.O, dtype=f32, device=dev)
+        if self.shift is not None:
+            out["dshift"] = torch.empty(self.O, dtype=f32, device=dev)
+        if residual:
+            out["dresidual"] = torch.empty_like(dy)
+        if x.numel() == 0:
+            for t in out.values():
+                t.zero_()
+            return out
+        with _on(dev):
+            ws, n = self._workspace(mb.moce_project_backward_workspace_bytes(desc), ws)
+            mb.moce_project_backward(desc, x, self.weight, self.scale, z, dy, mb.make_project_grads(**out), ws, n,
+                                     torch.cuda.current_stream(dev))
+        return out
+
+
+def _gradient_list(tensors, out):
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("no gradients")
+    device = tensors[0].device
+    if out is not None:
+        out = list(out)
+        if len(out) != len(tensors):
+            raise ValueError(f"{len(tensors)} gradients, {len(out)} outputs")
+    for name, ts in (("gradient", tensors), ("output", out or ())):
+        for t, like in zip(ts, tensors):
+            if t.dtype not in _DTYPE_OF or not t.is_cuda or t.device != device or not t.is_contiguous():
+                raise ValueError(f"every {name} has to be a contiguous float32 or bfloat16 tensor on {device}, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
+            if t.dtype != like.dtype or t.numel() != like.numel():
+                raise ValueError(f"an output is {t.dtype} {tuple(t.shape)}, its gradient {like.dtype} "
+                                 f"{tuple(like.shape)}")
+    return mb.make_gradients(tensors, out), len(tensors), device
+
+
+def _gradient_call(tensors, out, ws, call):
+    arr, n, device = _gradient_list(tensors, out)
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    with _on(device):
+        if ws is None:
+            ws = torch.empty(mb.moce_gradient_workspace_bytes(arr, n), dtype=torch.uint8, device=device)
+        call(arr, n, norm, ws, ws.numel() * ws.element_size(), torch.cuda.current_stream(device))
+    return norm
+
+
+def gradient_norm(tensors, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """moce_gradient_norm: the 2-norm [1] over every element of a list of float32 and bfloat16 tensors."""
+    return _gradient_call(tensors, None, ws, mb.moce_gradient_norm)
+
+
+def clip_gradients(tensors, max_norm: float, out=None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """moce_gradient_clip: scales the tensors (in place, or into the tensors of `out`) so that their global norm is
+    at most max_norm; returns the norm [1] before.  Nothing waits for the GPU."""
+    return _gradient_call(tensors, out, ws, lambda arr, n, norm, w, nb, st: mb.moce_gradient_clip(
+        arr, n, float(max_norm), norm, w, nb, st))
 
 
 def to_device_x(x: np.ndarray, dtype: str, device: str = "cuda") -> torch.Tensor:

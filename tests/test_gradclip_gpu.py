@@ -1,0 +1,196 @@
+"""The global gradient norm and clipping on the GPU, against float64, and a training step of the layers together."""
+import pytest
+import torch
+
+from paper_2608_23794_amd import binding as mb
+from paper_2608_23794_amd import inputs
+from paper_2608_23794_amd.layer import MoceLayer, ProjectLayer, clip_gradients, gradient_norm, to_device_x
+
+pytestmark = pytest.mark.gpu
+
+
+def normals(sizes, dtypes, seed=0, scale=1.0):
+    """Tensors one after the other in a buffer for each type, so most are aligned to their element only."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    bufs = {d: (torch.randn(sum(sizes) + 1, generator=g, device="cuda") * scale).to(d) for d in set(dtypes)}
+    at, out = {d: 1 for d in bufs}, []
+    for n, d in zip(sizes, dtypes):
+        out.append(bufs[d][at[d]:at[d] + n])
+        at[d] += n
+    return out
+
+
+def norm64(ts):
+    return float(sum((t.double() ** 2).sum() for t in ts)) ** 0.5
+
+
+F, H = torch.float32, torch.bfloat16
+LISTS = [
+    ([1], [F]), ([1], [H]), ([0, 3, 0], [F, H, F]), ([7, 8, 9, 15, 16, 17], [H, F] * 3),
+    ([16383, 16384, 16385, 1], [F, H, H, F]), ([100003], [H]), ([50, 70000, 3], [H, F, H]),
+    ([5] * 127, [F] * 127), ([3, 2] * 64, [H, F] * 64), ([1] * 300 + [40000] + [0] * 200 + [2] * 129, [F, H] * 315),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LISTS)))
+def test_norm_and_clip(case):
+    sizes, dtypes = LISTS[case]
+    ts = normals(sizes, dtypes, seed=case)
+    want = norm64(ts)
+    got = gradient_norm(ts)
+    # float64 sums, one rounding to float32
+    assert got.shape == (1,) and abs(float(got) - want) <= 2.0 ** -23 * want
+    for max_norm in (want * 0.3, want * 3):
+        coef = min(1.0, max_norm / want)
+        before = [t.clone() for t in ts]
+        outs = [torch.full_like(t, 7.0) for t in ts]
+        assert torch.equal(clip_gradients(ts, max_norm, out=outs), got)
+        for t, b, o in zip(ts, before, outs):
+            assert torch.equal(t, b)
+            # the coefficient and the product: half a float32 step each, then half a step of the type
+            half = 2.0 ** -24 if t.dtype == F else 2.0 ** -8
+            tol = (2.0 ** -22 + half) * (t.double().abs() * coef)
+            assert ((o.double() - t.double() * coef).abs() <= tol).all()
+            if coef == 1.0:
+                assert torch.equal(o, t)
+        assert torch.equal(clip_gradients(ts, max_norm), got)
+        assert all(torch.equal(t, o) for t, o in zip(ts, outs))          # in place: the same bits
+        for t, b in zip(ts, before):
+            t.copy_(b)
+
+
+def test_memory_around_the_tensors_stays():
+    buf = torch.full((10007,), 2.0, dtype=H, device="cuda")
+    ts = [buf[3:4], buf[11:5002], buf[5003:9990]]
+    clip_gradients(ts, 1.0)
+    rest = torch.ones(10007, dtype=torch.bool, device="cuda")
+    for a, b in ((3, 4), (11, 5002), (5003, 9990)):
+        rest[a:b] = False
+    assert (buf[rest] == 2.0).all() and (buf[~rest] < 2.0).all()
+
+
+def test_large_and_small_values():
+    for v in (1e30, 1e-30, 3e38, 1e-42):
+        t = torch.full((1000,), v, device="cuda")
+        want = norm64([t])
+        got = float(gradient_norm([t]))
+        if want > 3.4e38:
+            assert got == float("inf")
+        else:
+            # a norm below the normal numbers has fewer bits
+            assert abs(got - want) <= max(2.0 ** -23 * want, 2.0 ** -149)
+    t = torch.full((1000,), 1e30, device="cuda")
+    clip_gradients([t], 1.0)
+    assert abs(norm64([t]) - 1.0) < 1e-6
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_norm_that_is_not_finite_leaves_the_gradients(bad):
+    ts = normals([5, 40000], [F, H])
+    ts[1][777] = bad
+    before = [t.clone() for t in ts]
+    norm = clip_gradients(ts, 1e-3)
+    assert not torch.isfinite(norm).any()
+    assert all(torch.equal(t.nan_to_num(9.0), b.nan_to_num(9.0)) for t, b in zip(ts, before))
+
+
+def test_zero_gradients_and_a_largest_norm_of_zero():
+    z = torch.zeros(100, device="cuda")
+    assert float(clip_gradients([z], 1.0)) == 0.0 and float(z.abs().max()) == 0.0
+    assert float(clip_gradients([z], 0.0)) == 0.0
+    t = torch.ones(100, device="cuda")
+    assert float(clip_gradients([t], 0.0)) == 10.0 and float(t.abs().max()) == 0.0
+    assert float(gradient_norm([torch.empty(0, device="cuda")])) == 0.0
+    e = torch.empty(1, device="cuda")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    mb.moce_gradient_norm((mb.moce_gradient * 1)(), 0, e, ws, 256, torch.cuda.current_stream())
+    assert float(e) == 0.0
+
+
+def test_refusals():
+    t = torch.ones(64, device="cuda")
+    with pytest.raises(mb.MoceError):
+        clip_gradients([t, t], 1.0)
+    with pytest.raises(mb.MoceError):
+        clip_gradients([t[:32], t[16:48]], 1.0)
+    # the norm alone may count it twice (128 ** 0.5 has no float32: the nearest one comes back)
+    assert torch.equal(gradient_norm([t, t]).cpu(), torch.tensor([128 ** 0.5], dtype=torch.float32))
+    with pytest.raises(ValueError):
+        clip_gradients([t.view(8, 8).t()], 1.0)
+    with pytest.raises(ValueError):
+        clip_gradients([t.double()], 1.0)
+    with pytest.raises(ValueError):
+        clip_gradients([t], 1.0, out=[t.bfloat16()])
+    with pytest.raises(ValueError):
+        clip_gradients([t], 1.0, out=[])
+    with pytest.raises(mb.MoceError):
+        clip_gradients([t], float("nan"))
+    with pytest.raises(mb.MoceError):
+        gradient_norm([t], ws=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+def test_same_bits_on_another_stream_and_captured():
+    ts = normals([70000, 3, 20000] * 60, [F, H, H] * 60)
+    keep = [t.clone() for t in ts]
+    outs = [torch.empty_like(t) for t in ts]
+    want = clip_gradients(ts, 1.0, out=outs)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = clip_gradients(ts, 1.0)
+    side.synchronize()
+    assert torch.equal(got, want) and all(torch.equal(t, o) for t, o in zip(ts, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = clip_gradients(ts, 1.0)
+    for f in (1.0, 2.0, 0.25):
+        for t, k in zip(ts, keep):
+            t.copy_(k * f)
+        want = clip_gradients(ts, 1.0, out=outs)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and all(torch.equal(t, o) for t, o in zip(ts, outs))
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_training_step_of_the_layers_together(layout):
+    """A channel-expert layer and the projection after it, with a residual: forward, both backwards and the clipping of
+    every gradient, against the same in float64 from the layers' own activations."""
+    wl = inputs.WORKLOADS["resnet50_stage3"]
+    p = inputs.generate(wl, layout, batch=2)
+    moce = MoceLayer.from_workload(wl, p, layout)
+    x = to_device_x(p["x"], wl.dtype)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = (torch.randn(wl.C, wl.E, generator=g, device="cuda") * wl.E ** -0.5).bfloat16()
+    scale, shift = torch.rand(wl.C, generator=g, device="cuda") + 0.5, torch.randn(wl.C, generator=g, device="cuda")
+    expand = ProjectLayer(w, scale, shift, act="relu", layout=layout)
+
+    h = moce.forward(x)
+    y = expand.forward(h, residual=x)
+    dy = torch.randn(y.shape, generator=g, device="cuda").bfloat16()
+    out = expand.backward(h, dy, z=y, residual=True)
+    inner = moce.backward(x, out["dx"])
+    grads = [out["dweight"], out["dscale"], out["dshift"]] + [inner[n] for n in ("dw", "da", "dc")]
+    before = [t.clone() for t in grads]
+    norm = clip_gradients(grads, 0.5)
+    want = norm64(before)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want and want > 0.5
+    for t, b in zip(grads, before):
+        half = 2.0 ** -24 if t.dtype == F else 2.0 ** -8
+        assert ((t.double() - b.double() * (0.5 / want)).abs() <= (2.0 ** -22 + half) * (b.double().abs() * 0.5 / want)).all()
+
+    def rows(t):
+        t = t.double()
+        return (t.movedim(1, -1) if layout == "nchw" else t).reshape(-1, t.shape[1] if layout == "nchw" else t.shape[-1])
+
+    hr, wd = rows(h), w.double()
+    z = hr @ wd.t() * scale.double() + shift.double() + rows(x)
+    mag = hr.abs() @ wd.abs().t() * scale.double() + shift.double().abs() + rows(x).abs()
+    assert ((rows(y) - z.clamp(min=0)).abs() <= 2.0 ** -8 * 1.01 * z.abs() + (wl.E + 4) * 2.0 ** -24 * mag).all()
+    dz = torch.where(rows(y) > 0, rows(dy), torch.zeros((), dtype=torch.float64, device="cuda"))
+    assert torch.equal(rows(out["dresidual"]), dz)
+    G, Gm = dz.t() @ hr, dz.abs().t() @ hr.abs()
+    dW = scale.double()[:, None] * G
+    tol = 2.0 ** -8 * 1.01 * dW.abs() + scale.double()[:, None] * (hr.shape[0] + 8) * 2.0 ** -24 * Gm
+    assert ((before[0].double() - dW).abs() <= tol).all()
