@@ -18,6 +18,7 @@
 // neighbouring columns of one row.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "moce_internal.h"
 
@@ -47,7 +48,7 @@ struct GemmArgs {
   Operand a, b;
   int R, N, K;            // rows, columns, contraction
   int klen;               // contraction of one split, a multiple of the stage's
-  int pos_rows;           // the grid's x runs over rows (else over columns)
+  int tr, tc;             // tiles down and across
   // output: row r at r ld, columns as an operand's line
   void *y, *z;
   const void* res;
@@ -134,6 +135,12 @@ __device__ __forceinline__ float act_value(float z, int act) {
   if (act == MOCE_ACT_SILU) return fmaxf(z, -1e4f) * sigmoid<T>(z);
   return z;
 }
+template <typename T>
+__device__ __forceinline__ void act_values(float (&v)[8], int act) {
+  if (act == MOCE_ACT_NONE) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = act_value<T>(v[i], act);
+}
 // act'(z) dy; ReLU selects, so that an upstream value that is not finite stays on its own positions
 template <typename T>
 __device__ __forceinline__ float act_gradient(float z, float dy, int act) {
@@ -191,8 +198,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, int r, int c, int spl
       for (int i = 0; i < 8; ++i) v[i] += q[i];
     }
     if (z) store8(z + p, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value<T>(v[i], g.act);
+    act_values<T>(v, g.act);
     store8(y + p, v);
     return;
   }
@@ -259,27 +265,33 @@ struct Stage {
   // byte of chunk c of line i
   static __device__ __forceinline__ int at(int i, int c) { return i * (kPerLine * 16) + ((c ^ key(i)) << 4); }
 
-  static __device__ __forceinline__ int index(int f, int lane) {
-    const int m = lane & 15;
-    return COLS ? 32 * (f >> 1) + 8 * (m >> 2) + 4 * (f & 1) + (m & 3) : 16 * f + m;
+  // Where this lane reads fragment 0 of the 16 rows or columns from w on, step
+  // 0: the others lie at an exclusive or (of bits that w leaves clear) and a
+  // constant from there.
+  static __device__ __forceinline__ int place(int w, int lane) {
+    const int g = lane >> 4, m = lane & 15, n = w + (COLS ? 8 * (m >> 2) + (m & 3) : m);
+    if constexpr (ALONG_K) return at(n, g);
+    if constexpr (sizeof(T) == 4) return at(4 * g, n >> 2) + 4 * (n & 3);
+    const int q = lane & 3;
+    return at(8 * g + ((lane >> 2) & 3), w / 8 + (COLS ? q : q >> 1)) + (COLS ? 0 : 8 * (q & 1));
   }
-  // Fragment f (16 rows or columns from w on) of step ks (64 bytes of k).
-  static __device__ __forceinline__ u32x4 frag(const unsigned char* s, int w, int f, int ks, int lane) {
-    const int g = lane >> 4;
+  // Fragment f of step ks (64 bytes of k).
+  static __device__ __forceinline__ u32x4 frag(const unsigned char* s, int place, int f, int ks) {
+    const int j = f >> 1, h = f & 1;
     if constexpr (ALONG_K) {
-      return *reinterpret_cast<const u32x4*>(s + at(w + index(f, lane), 4 * ks + g));
+      return *reinterpret_cast<const u32x4*>(s + (place ^ (ks << 6)) + (COLS ? 32 * j + 4 * h : 16 * f) * kLine);
     } else if constexpr (sizeof(T) == 2) {
-      const int t = (lane >> 2) & 3, q = lane & 3, k = 32 * ks + 8 * g + t;
-      const int c = w / 8 + (COLS ? 4 * (f >> 1) + q : 2 * f + (q >> 1)), half = COLS ? f & 1 : q & 1;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(s + at(k, c) + 8 * half));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(s + at(k + 4, c) + 8 * half));
+      constexpr int W = kPerLine * 16;
+      const unsigned char* p = s + (place ^ (COLS ? j << 6 : f << 5)) + (COLS ? 8 * h : 0) + 32 * ks * W;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * W));
       return __builtin_bit_cast(u32x4, s16x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w});
     } else {
-      const int n = w + index(f, lane);
+      constexpr int W = kPerLine * 16;
+      const unsigned char* p = s + (place ^ (COLS ? (j << 7) | (h << 4) : f << 6)) + 16 * ks * W;
       u32x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        v[e] = *reinterpret_cast<const unsigned int*>(s + at(16 * ks + 4 * g + e, n >> 2) + 4 * (n & 3));
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const unsigned int*>(p + e * W);
       return v;
     }
   }
@@ -333,28 +345,128 @@ __device__ __forceinline__ u32x4 load_chunk(const Operand& o, int i, int ni, int
   return v;
 }
 
-// One tile of 32 FR rows by 32 FC columns; AK, BK: operands along k.
-template <typename T, bool AK, bool BK, int FR, int FC>
-__global__ void __launch_bounds__(kThreads)
-k_project(GemmArgs g) {
-  constexpr int TR = 32 * FR, TC = 32 * FC;
-  using SA = Stage<T, AK, TR, false>;
-  using SB = Stage<T, BK, TC, true>;
-  constexpr int kDepth = SA::kDepth;
-  __shared__ __attribute__((aligned(16))) unsigned char la[SA::kBytes], lb[SB::kBytes];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = (wave & 1) * 16 * FR, wc = (wave >> 1) * 16 * FC;
-  const int r0 = (g.pos_rows ? blockIdx.x : blockIdx.y) * TR, c0 = (g.pos_rows ? blockIdx.y : blockIdx.x) * TC;
-  const int split = blockIdx.z;
-  const int k0 = split * g.klen, k1 = min(g.K, k0 + g.klen);
+// The tile of a workgroup.  Workgroup u runs on XCD u mod 8 and takes the
+// (u / 8)-th of that XCD's eighth of the tiles, which go down kGroup rows of
+// tiles before they go across: the tiles that run together on an XCD share
+// the lines they read in its L2.  False past the last tile.
+constexpr int kGroup = 8;
+__device__ __forceinline__ bool tile_of(const GemmArgs& g, int& r, int& c) {
+  const int u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  if (u >= g.tr * g.tc) return false;
+  const int band = u / (kGroup * g.tc), r0 = band * kGroup, n = min(kGroup, g.tr - r0), v = u - r0 * g.tc;
+  r = r0 + v % n;
+  c = v / n;
+  return true;
+}
 
-  f32x4 acc[FR][FC];
+// Scales, shifts and stores a wave's fragments: rows r0.., columns c0...
+// They pass through BYTES of LDS at l, the wave's own, so that a row is
+// written (and its residual read) as one run of memory, 32 FC bytes of
+// bfloat16; chunk c of a row lies at c ^ (row & 7).  Where every eight columns
+// are there or not (whole), kBatch rows' residuals are in flight together.
+template <typename T, int BYTES, int FR, int FC>
+__device__ __forceinline__ void finish(const GemmArgs& g, int r0, int c0, int lane, f32x4 (&acc)[FR][FC],
+                                       unsigned char* l) {
+  constexpr int kPitch = FC * 64, kAcross = 2 * FC, kDown = kWave / kAcross;
+  constexpr int kFrags = BYTES / (16 * kPitch) < FR ? BYTES / (16 * kPitch) : FR;   // fragments of rows at a time
+  constexpr int kIters = kFrags * 16 / kDown, kBatch = kIters < 4 ? kIters : 4;
+  static_assert(FR % kFrags == 0 && kIters % kBatch == 0, "whole parts");
+  const int x = lane % kAcross, dr = lane / kAcross, c = c0 + 8 * x;
+  float sc[8], sh[8];
+  column_affine(g, c, sc, sh);
+  const bool whole = g.N % 8 == 0 && g.hw % 8 == 0;
+  int64_t at = c;   // of the lane's columns within a row
+  if (whole && g.hw) at = (c / g.hw) * g.img + c % g.hw;
+#pragma unroll
+  for (int f = 0; f < FR; f += kFrags) {
+#pragma unroll
+    for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+      for (int j = 0; j < FC; ++j) {
+        const int row = 16 * i + (lane & 15), ch = 8 * (j / 2) + 2 * (lane >> 4) + (j & 1);
+        *reinterpret_cast<f32x4*>(l + row * kPitch + ((ch ^ (row & 7)) << 4)) = acc[f + i][j];
+      }
+    auto value = [&](int row, float (&v)[8]) __attribute__((always_inline)) {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(l + row * kPitch + (((2 * x) ^ (row & 7)) << 4));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(l + row * kPitch + (((2 * x + 1) ^ (row & 7)) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = lo[e];
+        v[4 + e] = hi[e];
+      }
+    };
+    const int rf = r0 + 16 * f;
+    if (whole && !g.part) {
+      const T* res = static_cast<const T*>(g.res);
+      T *y = static_cast<T*>(g.y), *z = static_cast<T*>(g.z);
+      for (int it = 0; it < kIters; it += kBatch) {
+        float q[kBatch][8];
+        float rsc[kBatch], rsh[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int r = min(rf + (it + u) * kDown + dr, g.R - 1);
+          rsc[u] = g.per_row && g.scale ? g.scale[r] : 1.f;
+          rsh[u] = g.per_row && g.shift ? g.shift[r] : 0.f;
+          if (res) load8(res + r * g.ld + (c < g.N ? at : 0), q[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = (it + u) * kDown + dr, r = rf + row;
+          float v[8];
+          value(row, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], g.per_row ? rsc[u] : sc[e], g.per_row ? rsh[u] : sh[e]);
+          if (res)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += q[u][e];
+          const bool there = r < g.R && c < g.N;
+          if (z && there) store8(z + r * g.ld + at, v);
+          act_values<T>(v, g.act);
+          if (there) store8(y + r * g.ld + at, v);
+        }
+      }
+    } else {
+      for (int it = 0; it < kIters; ++it) {
+        const int row = it * kDown + dr;
+        float v[8];
+        value(row, v);
+        row_affine(g, rf + row, sc, sh);
+        finish8<T>(g, rf + row, c, blockIdx.y, v, sc, sh);
+      }
+    }
+  }
+}
+
+template <int FR, int FC>
+__device__ __forceinline__ void clear(f32x4 (&acc)[FR][FC]) {
 #pragma unroll
   for (int i = 0; i < FR; ++i)
 #pragma unroll
     for (int j = 0; j < FC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
 
+// Any alignment: one tile of 32 FR rows by 32 FC columns, staged through
+// registers; AK, BK: operands along k.
+template <typename T, bool AK, bool BK, int FR, int FC>
+__global__ void __launch_bounds__(kThreads)
+k_project_any(GemmArgs g) {
+  constexpr int TR = 32 * FR, TC = 32 * FC;
+  using SA = Stage<T, AK, TR, false>;
+  using SB = Stage<T, BK, TC, true>;
+  constexpr int kDepth = SA::kDepth;
+  __shared__ __attribute__((aligned(16))) unsigned char la[SA::kBytes + SB::kBytes];
+  unsigned char* lb = la + SA::kBytes;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = (wave & 1) * 16 * FR, wc = (wave >> 1) * 16 * FC;
+  int r0, c0;
+  if (!tile_of(g, r0, c0)) return;
+  r0 *= TR, c0 *= TC;
+  const int k0 = blockIdx.y * g.klen, k1 = min(g.K, k0 + g.klen);
+
+  f32x4 acc[FR][FC];
+  clear(acc);
+  const int pa = SA::place(wr, lane), pb = SB::place(wc, lane);
   for (int k = k0; k < k1; k += kDepth) {
     auto fetch = [&](auto s, const Operand& o, bool along_k, int n0, int n, unsigned char* l) __attribute__((always_inline)) {
       using S = decltype(s);
@@ -374,30 +486,220 @@ k_project(GemmArgs g) {
     for (int ks = 0; ks < 2; ++ks) {
       u32x4 fa[FR], fb[FC];
 #pragma unroll
-      for (int i = 0; i < FR; ++i) fa[i] = SA::frag(la, wr, i, ks, lane);
+      for (int i = 0; i < FR; ++i) fa[i] = SA::frag(la, pa, i, ks);
 #pragma unroll
-      for (int j = 0; j < FC; ++j) fb[j] = SB::frag(lb, wc, j, ks, lane);
+      for (int j = 0; j < FC; ++j) fb[j] = SB::frag(lb, pb, j, ks);
 #pragma unroll
       for (int i = 0; i < FR; ++i)
 #pragma unroll
         for (int j = 0; j < FC; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
     }
   }
+  __syncthreads();
+  constexpr int kPart = (SA::kBytes + SB::kBytes) / 4;
+  finish<T, kPart>(g, r0 + wr, c0 + wc, lane, acc, la + wave * kPart);
+}
 
+// ---- aligned lines: stages copied by the global-to-LDS loads ---------------------
+//
+// Where every line starts on 16 bytes and holds whole chunks (images too), a
+// stage goes to LDS without passing registers, two stages in LDS: while the
+// matrix cores work on the second half of stage s, whose operands are in
+// registers by then, stage s + 2 is copied over it; its own copies have the
+// time of a whole stage to arrive.  One barrier a stage.  The swizzle is in
+// the lane's source address.  Chunks past the contraction's end come from a
+// line of zeros; rows and columns past the tensor repeat its last ones, and
+// are not stored.
+__device__ __align__(16) unsigned int zero_chunk[4];
+
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+// s_waitcnt operands
+constexpr int vm_wait(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+constexpr int kLgkmWait0 = 0xc07f;
+
+// 16 bytes from a scalar base and the lane's 32-bit offset (a buffer without
+// bounds), to `to` and the lanes' places behind it.  With 64-bit addresses of
+// its own a lane holds two registers for each of its chunks, which the
+// products need.
+__device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t off, lds_byte* to) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass does not know the buffer's type
+  const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, -1, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, to, 16, off, 0, 0, 0);
+#endif
+}
+
+// The chunks of one operand that a thread copies in every stage.  IMG: the
+// lines along k run over images, so that the lanes' places in them differ;
+// else the place is the same for all, and the lanes' offsets from it stay.
+template <typename T, bool ALONG_K, bool IMG, int TILE, bool COLS, int NT>
+struct Copier {
+  using S = Stage<T, ALONG_K, TILE, COLS>;
+  static constexpr int kRounds = S::kChunks / NT;
+  const char* base;      // the stage to copy next
+  uint32_t off[kRounds];
+  int64_t step;
+  // IMG
+  int64_t wrap;
+  int k, hw;             // the lane's first position of the stage in its image
+
+  __device__ __forceinline__ void init(const Operand& o, int n0, int n, int k0, int tid) {
+    constexpr int ES = sizeof(T);
+    base = static_cast<const char*>(o.p);
+    if constexpr (ALONG_K) {
+      const int c = (tid & 7) ^ S::key(tid >> 3);   // the same in every round
+      if constexpr (IMG) {
+        hw = o.hw;
+        k = k0 + c * S::kVec;
+        const int b = k / hw;
+        k -= b * hw;
+        base += (n0 * o.ld + b * o.img + k) * ES;
+        wrap = (o.img - hw) * ES;
+      } else {
+        base += (n0 * o.ld + k0) * ES;
+      }
+      step = kLine;
 #pragma unroll
-  for (int j = 0; j < FC / 2; ++j) {
-    const int c = c0 + wc + 32 * j + 8 * (lane >> 4);
-    float sc[8], sh[8];
-    column_affine(g, c, sc, sh);
+      for (int u = 0; u < kRounds; ++u)
+        off[u] = (uint32_t)((min(n0 + u * (NT / 8) + (tid >> 3), n - 1) - n0) * o.ld * ES) + (IMG ? 0 : c * 16);
+    } else {
+      const int b0 = o.hw ? n0 / o.hw : 0;
+      base += (k0 * o.ld + b0 * o.img) * ES;
+      step = (int64_t)S::kDepth * o.ld * ES;
 #pragma unroll
-    for (int i = 0; i < FR; ++i) {
-      const int r = r0 + wr + 16 * i + (lane & 15);
-      row_affine(g, r, sc, sh);
-      const f32x4 lo = acc[i][2 * j], hi = acc[i][2 * j + 1];
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish8<T>(g, r, c, split, v, sc, sh);
+      for (int u = 0; u < kRounds; ++u) {
+        const int q = tid + u * NT, i = q / S::kPerLine, c = (q % S::kPerLine) ^ S::key(i);
+        const int j = min(n0 + c * S::kVec, n - S::kVec);
+        const int64_t at = o.hw ? (j / o.hw - b0) * o.img + j % o.hw : j;
+        off[u] = (uint32_t)((i * o.ld + at) * ES);
+      }
     }
   }
+  // Copies a stage to l; CUT: of whose k only `left` elements are there.
+  template <bool CUT>
+  __device__ __forceinline__ void copy(unsigned char* l, int tid, int wave, int left) {
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      lds_byte* to = (lds_byte*)(l + (u * NT + wave * kWave) * 16);
+      if constexpr (CUT || IMG) {
+        const char* src = base + off[u];
+        if constexpr (CUT) {
+          const int at = ALONG_K ? ((tid & 7) ^ S::key(tid >> 3)) * S::kVec : (tid + u * NT) / S::kPerLine;
+          if (at >= left) src = reinterpret_cast<const char*>(zero_chunk);
+        }
+        __builtin_amdgcn_global_load_lds((const void*)src, to, 16, 0, 0);
+      } else {
+        buffer_to_lds(base, off[u], to);
+      }
+    }
+    base += step;
+    if constexpr (IMG) {
+      k += S::kDepth;
+      while (k >= hw) {
+        k -= hw;
+        base += wrap;
+      }
+    }
+  }
+};
+
+// WR x WC waves of FR x FC fragments.
+template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC>
+__global__ void __launch_bounds__(64 * WR * WC, 2)
+k_project_copy(GemmArgs g) {
+  constexpr int NT = 64 * WR * WC, TR = 16 * WR * FR, TC = 16 * WC * FC;
+  using SA = Stage<T, AK, TR, false>;
+  using SB = Stage<T, BK, TC, true>;
+  constexpr int kDepth = SA::kDepth;
+  // four arrays, so that the compiler sees the copies and the reads apart and
+  // waits for a copy only where its array is read
+  __shared__ __attribute__((aligned(16))) unsigned char a0[SA::kBytes], b0[SB::kBytes], a1[SA::kBytes], b1[SB::kBytes];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % WR * 16 * FR, wc = wave / WR * 16 * FC;
+  int r0, c0;
+  if (!tile_of(g, r0, c0)) return;
+  r0 *= TR, c0 *= TC;
+  const int k0 = blockIdx.y * g.klen, length = min(g.K, k0 + g.klen) - k0;
+  const int n = (length + kDepth - 1) / kDepth;
+
+  Copier<T, AK, AK && IMG, TR, false, NT> ca;
+  Copier<T, BK, BK && IMG, TC, true, NT> cb;
+  ca.init(g.a, r0, g.R, k0, tid);
+  cb.init(g.b, c0, g.N, k0, tid);
+  f32x4 acc[FR][FC];
+  clear(acc);
+  // A stage goes in four phases: step 0 and 1, the upper and lower half of the
+  // wave's rows; the operands of a phase are read during the one before.
+  constexpr int FH = FR / 2;
+  u32x4 fa[2][FH], fb[2][FC];
+  int pa = SA::place(wr, lane), pb = SB::place(wc, lane);
+  auto read = [&](int phase, const unsigned char* la, const unsigned char* lb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FH; ++i) fa[phase & 1][i] = SA::frag(la, pa, (phase & 1) * FH + i, phase >> 1);
+    if ((phase & 1) == 0)
+#pragma unroll
+      for (int j = 0; j < FC; ++j) fb[phase >> 1][j] = SB::frag(lb, pb, j, phase >> 1);
+  };
+  auto products = [&](int phase) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FH; ++i)
+#pragma unroll
+      for (int j = 0; j < FC; ++j) {
+        f32x4& c = acc[(phase & 1) * FH + i][j];
+        c = multiply<T>(fb[phase >> 1][j], fa[phase & 1][i], c);
+      }
+  };
+  auto publish = [&]() __attribute__((always_inline)) {   // this wave's reads and copies are done, then everyone's
+    __builtin_amdgcn_s_waitcnt(kLgkmWait0);
+    __builtin_amdgcn_s_waitcnt(vm_wait(0));
+    __syncthreads();
+  };
+  // Stage s lies in (la, lb), its first phase's operands in registers; copies
+  // stage s + 2 (cut: `left` of it) and leaves the next one's first operands.
+  auto stage = [&](auto cut, int left, unsigned char* la, unsigned char* lb, unsigned char* na,
+                   unsigned char* nb) __attribute__((always_inline)) {
+    asm volatile("" : "+v"(pa), "+v"(pb));   // the places of the fragments are formed here, not kept
+    read(1, la, lb);
+    products(0);
+    __builtin_amdgcn_sched_barrier(0);   // no phase's reads before the one ahead of it: registers
+    read(2, la, lb);
+    products(1);
+    __builtin_amdgcn_sched_barrier(0);
+    read(3, la, lb);
+    products(2);
+    __builtin_amdgcn_sched_barrier(0);
+    publish();
+    ca.template copy<decltype(cut)::value>(la, tid, wave, left);
+    cb.template copy<decltype(cut)::value>(lb, tid, wave, left);
+    read(0, na, nb);
+    products(3);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const std::integral_constant<bool, true> some{};
+  const std::integral_constant<bool, false> all{};
+  ca.template copy<true>(a0, tid, wave, length);
+  cb.template copy<true>(b0, tid, wave, length);
+  publish();
+  ca.template copy<true>(a1, tid, wave, length - kDepth);
+  cb.template copy<true>(b1, tid, wave, length - kDepth);
+  read(0, a0, b0);
+  int left = length - 2 * kDepth;   // of the stage to copy next
+  int s = 0;
+  for (; left >= 2 * kDepth; s += 2, left -= 2 * kDepth) {
+    stage(all, 0, a0, b0, a1, b1);
+    stage(all, 0, a1, b1, a0, b0);
+  }
+  for (; s + 1 < n; s += 2, left -= 2 * kDepth) {
+    stage(some, left, a0, b0, a1, b1);
+    stage(some, left - kDepth, a1, b1, a0, b0);
+  }
+  if (s < n) stage(some, left, a0, b0, a1, b1);
+  publish();
+  // a wave's part of LDS for its results
+  constexpr int kEach = WR * WC / 4, kPart = (SA::kBytes < SB::kBytes ? SA::kBytes : SB::kBytes) / kEach;
+  const int w = wave / kEach;
+  finish<T, kPart>(g, r0 + wr, c0 + wc, lane, acc, (w == 0 ? a0 : w == 1 ? b0 : w == 2 ? a1 : b1) + wave % kEach * kPart);
 }
 
 // Sums the splits' partial products, in order, and finishes them.
@@ -586,32 +888,76 @@ k_project_scale(const T* __restrict__ weight, const float* __restrict__ scale, i
 
 // ---- launches --------------------------------------------------------------------
 
-constexpr int kFrag = 2;                 // fragments of a wave in each direction
-constexpr int kTile = 32 * kFrag;
 constexpr int kWantTiles = 512;          // two workgroups a CU
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How often the contraction is divided: where the outputs alone make too few
-// tiles for the GPU, into lengths of 256 or more.
+// How a product is cut: tiles of `tile` rows and columns and, where these
+// make too few workgroups for the GPU, the contraction in lengths of 256 or more.
 struct Plan {
-  int splits, klen;
+  int tile, splits, klen;
 };
 Plan plan(int64_t R, int64_t N, int64_t K, int elem) {
   const int depth = kLine / (elem == MOCE_F32 ? 4 : 2);
-  const int64_t tiles = ceil_div(R, kTile) * ceil_div(N, kTile);
+  int tile = 64;
+  if (ceil_div(R, 128) * ceil_div(N, 128) >= 256) tile = 128;
+  if (elem == MOCE_BF16 && ceil_div(R, 256) * ceil_div(N, 256) >= 256) tile = 256;
+  const int64_t tiles = ceil_div(R, tile) * ceil_div(N, tile);
   int64_t s = std::min(std::max<int64_t>(1, kWantTiles / tiles), std::max<int64_t>(1, K / 256));
   s = std::min<int64_t>(s, 256);
   const int64_t klen = ceil_div(ceil_div(K, s), depth) * depth;
-  return Plan{(int)ceil_div(K, klen), (int)klen};
+  return Plan{tile, (int)ceil_div(K, klen), (int)klen};
 }
 size_t part_bytes(int64_t R, int64_t N, const Plan& p) { return (size_t)p.splits * R * N * sizeof(float); }
 
+// Whether the copying kernel can read this operand: whole chunks, at offsets of 31 bits within a tile.
+bool whole_chunks(const Operand& o, bool along_k, int64_t length, int elem) {
+  const int es = elem == MOCE_F32 ? 4 : 2, vec = 16 / es;
+  if (o.ld % vec || o.hw % vec || length % vec) return false;
+  const int64_t span = along_k ? 256 * o.ld : (kLine / es) * o.ld + (o.hw ? (256 / o.hw + 2) * o.img : 0);
+  return span * es < INT_MAX;
+}
+
+template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int F, int FC>
+void launch_copy(GemmArgs g, int splits, hipStream_t st) {
+  g.tr = (int)ceil_div(g.R, 16 * WR * F), g.tc = (int)ceil_div(g.N, 16 * WC * FC);
+  const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc, 8) * 8), splits);
+  hipLaunchKernelGGL((k_project_copy<T, AK, BK, IMG, WR, WC, F, FC>), grid, dim3(64 * WR * WC), 0, st, g);
+}
+
+template <typename T, bool AK, bool BK, int F>
+void launch_any(GemmArgs g, int splits, hipStream_t st) {
+  g.tr = (int)ceil_div(g.R, 32 * F), g.tc = (int)ceil_div(g.N, 32 * F);
+  const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc, 8) * 8), splits);
+  hipLaunchKernelGGL((k_project_any<T, AK, BK, F, F>), grid, dim3(kThreads), 0, st, g);
+}
+
 template <typename T, bool AK, bool BK>
-hipError_t launch_product(const GemmArgs& g, int splits, hipStream_t st) {
-  const int64_t tr = ceil_div(g.R, kTile), tc = ceil_div(g.N, kTile);
-  const dim3 grid(g.pos_rows ? tr : tc, g.pos_rows ? tc : tr, splits);
-  hipLaunchKernelGGL((k_project<T, AK, BK, kFrag, kFrag>), grid, dim3(kThreads), 0, st, g);
+hipError_t launch_product(const GemmArgs& g, const Plan& p, hipStream_t st) {
+  const int elem = sizeof(T) == 4 ? MOCE_F32 : MOCE_BF16;
+  const bool whole = whole_chunks(g.a, AK, AK ? g.K : g.R, elem) && whole_chunks(g.b, BK, BK ? g.K : g.N, elem);
+  auto copy = [&](auto img) {
+    constexpr bool IMG = decltype(img)::value;
+    if (p.tile == 64)
+      launch_copy<T, AK, BK, IMG, 2, 2, 2, 2>(g, p.splits, st);
+    else if (p.tile == 128 || sizeof(T) == 4)
+      launch_copy<T, AK, BK, IMG, 2, 2, 4, 4>(g, p.splits, st);
+    else if constexpr (sizeof(T) == 2)
+      launch_copy<T, AK, BK, IMG, 2, 4, 8, 4>(g, p.splits, st);
+  };
+  if (!whole) {
+    if (p.tile == 64)
+      launch_any<T, AK, BK, 2>(g, p.splits, st);
+    else
+      launch_any<T, AK, BK, 4>(g, p.splits, st);
+  } else if constexpr (AK && BK) {
+    if (g.a.hw)
+      copy(std::true_type{});
+    else
+      copy(std::false_type{});
+  } else {
+    copy(std::false_type{});
+  }
   return hipGetLastError();
 }
 
@@ -627,7 +973,7 @@ template <typename T, bool AK, bool BK>
 hipError_t launch_whole(GemmArgs g, const Plan& p, float* part, hipStream_t st) {
   g.klen = p.klen;
   g.part = p.splits > 1 ? part : nullptr;
-  const hipError_t e = launch_product<T, AK, BK>(g, p.splits, st);
+  const hipError_t e = launch_product<T, AK, BK>(g, p, st);
   if (e != hipSuccess || p.splits == 1) return e;
   return launch_join<T>(g, p.splits, st);
 }
@@ -644,7 +990,7 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
   g.scale = scale, g.shift = shift, g.res = res, g.y = y, g.z = z, g.act = s.act;
   const Operand wo{w, s.C, 0, 0};
   if (s.layout == MOCE_NHWC) {
-    g.a = Operand{x, s.C, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.O, g.ld = s.O, g.pos_rows = 1;
+    g.a = Operand{x, s.C, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.O, g.ld = s.O;
     return launch_whole<T, true, true>(g, plan(g.R, g.N, g.K, s.elem), part, st);
   }
   g.a = wo, g.b = Operand{x, s.HW, s.C * s.HW, hw}, g.R = (int)s.O, g.N = P, g.per_row = 1;
@@ -764,7 +1110,7 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
     const Operand wo{row_scale ? ws.weight : w, s.C, 0, 0};
     g.K = (int)s.O, g.y = gr.dx;
     if (nhwc) {
-      g.a = Operand{dz, s.O, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.C, g.ld = s.C, g.pos_rows = 1;
+      g.a = Operand{dz, s.O, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.C, g.ld = s.C;
       e = launch_whole<T, true, false>(g, plan(g.R, g.N, g.K, s.elem), ws.part, st);
     } else {
       g.a = wo, g.b = Operand{dz, s.HW, s.O * s.HW, hw}, g.R = (int)s.C, g.N = P;
@@ -781,10 +1127,10 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
     if (join) g.part = ws.part;
     if (nhwc) {
       g.a = Operand{dz, s.O, 0, 0}, g.b = Operand{x, s.C, 0, 0};
-      e = launch_product<T, false, false>(g, p.splits, st);
+      e = launch_product<T, false, false>(g, p, st);
     } else {
       g.a = Operand{dz, s.HW, s.O * s.HW, hw}, g.b = Operand{x, s.HW, s.C * s.HW, hw};
-      e = launch_product<T, true, true>(g, p.splits, st);
+      e = launch_product<T, true, true>(g, p, st);
     }
     if (e != hipSuccess) return e;
     if (join) {

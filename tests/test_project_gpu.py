@@ -360,3 +360,22 @@ def test_many_positions(layout):
     check_forward(t, "bf16", layout, "relu", t["residual"], y, z)
     t["z"] = z
     check_backward(t, "bf16", layout, "relu", t["layer"].backward(t["x"], t["dy"], z=z, residual=True))
+
+
+# aligned shapes that take each tile with edges in it, contractions that end inside a stage, images shorter and longer
+# than a stage
+TILES = [(1, 200, 328, 700, 1, "nhwc"), (3, 136, 264, 40, 24, "nchw"), (2, 1096, 520, 33, 16, "nhwc"),
+         (5, 64, 72, 8, 9, "nchw"), (300, 328, 264, 1, 1, "nhwc"), (64, 24, 2056, 72, 1, "nhwc"), (40, 2056, 24, 8, 10, "nchw"),
+         (9, 1032, 1544, 1000, 1, "nhwc"), (10, 1544, 1032, 24, 25, "nchw")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", TILES, ids=str)
+def test_tiles(size, dtype):
+    B, C, O, H, W, layout = size
+    act, scale, shift, residual = KINDS[TILES.index(size) % len(KINDS)]
+    t = make(B, C, O, H, W, dtype, layout, act, scale, shift, seed=7)
+    res, z = t["residual"] if residual else None, torch.empty_like(t["z"])
+    y = t["layer"].forward(t["x"], residual=res, z=z)
+    check_forward(t, dtype, layout, act, res, y, z)
+    check_backward(t, dtype, layout, act, t["layer"].backward(t["x"], t["dy"], z=t["z"], residual=residual))
