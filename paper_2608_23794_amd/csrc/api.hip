@@ -603,20 +603,6 @@ moce_status check_project(const moce_project_desc* d, moce::ProjectShape* s) {
   return moce::project_limits(*s) ? MOCE_OK : MOCE_ERR_UNSUPPORTED;
 }
 
-struct ProjectBwdLayout {
-  size_t dz, weight, shift, part, total;
-};
-ProjectBwdLayout project_bwd_layout(const moce::ProjectShape& s) {
-  const moce::ProjectBwdSizes z = moce::project_backward_sizes(s);
-  ProjectBwdLayout l{};
-  l.dz = 0;
-  l.weight = l.dz + round_up(z.dz);
-  l.shift = l.weight + round_up(z.weight);
-  l.part = l.shift + round_up(z.shift);
-  l.total = l.part + round_up(z.part);
-  return l;
-}
-
 }  // namespace
 
 size_t moce_project_workspace_bytes(const moce_project_desc* desc) {
@@ -645,7 +631,7 @@ moce_status moce_project(const moce_project_desc* desc, const void* x, const voi
 size_t moce_project_backward_workspace_bytes(const moce_project_desc* desc) {
   moce::ProjectShape s;
   if (check_project(desc, &s) != MOCE_OK) return 0;
-  return project_bwd_layout(s).total;
+  return round_up(std::max<size_t>(moce::project_backward_ws_bytes(s), 1));
 }
 
 moce_status moce_project_backward(const moce_project_desc* desc, const void* x, const void* weight,
@@ -661,13 +647,9 @@ moce_status moce_project_backward(const moce_project_desc* desc, const void* x, 
       !aligned(grads->dweight, 16) || !aligned(grads->dresidual, 16) || !aligned(scale, 4) ||
       !aligned(grads->dscale, 4) || !aligned(grads->dshift, 4))
     return MOCE_ERR_ALIGN;
-  const ProjectBwdLayout l = project_bwd_layout(s);
-  if (!ws || ws_bytes < l.total) return MOCE_ERR_WORKSPACE;
+  if (!ws || ws_bytes < moce::project_backward_ws_bytes(s)) return MOCE_ERR_WORKSPACE;
   if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
-  char* base = static_cast<char*>(ws);
-  const moce::ProjectBwdWs w{base + l.dz, base + l.weight, reinterpret_cast<float*>(base + l.shift),
-                             reinterpret_cast<float*>(base + l.part)};
-  return device_status(moce::launch_project_backward(s, x, weight, scale, z, dy, *grads, w, stream));
+  return device_status(moce::launch_project_backward(s, x, weight, scale, z, dy, *grads, ws, stream));
 }
 
 // ---- gradient norm and clipping --------------------------------------------------

@@ -306,21 +306,13 @@ struct ProjectShape {
   int elem, layout, act;
 };
 bool project_limits(const ProjectShape& s);
-size_t project_ws_bytes(const ProjectShape& s);   // partial products, 0 where the contraction is not divided
+size_t project_ws_bytes(const ProjectShape& s);   // packed operands, partial products; 0 for none
 hipError_t launch_project(const ProjectShape& s, const void* x, const void* w, const float* scale, const float* shift,
                           const void* res, void* y, void* z, void* ws, hipStream_t st);
-// Workspace of the backward: dz, the scaled weight, the groups' sums of dz, partial products (bytes).
-struct ProjectBwdSizes {
-  size_t dz, weight, shift, part;
-};
-struct ProjectBwdWs {
-  void *dz, *weight;
-  float *shift, *part;
-};
-ProjectBwdSizes project_backward_sizes(const ProjectShape& s);
+size_t project_backward_ws_bytes(const ProjectShape& s);
 hipError_t launch_project_backward(const ProjectShape& s, const void* x, const void* w, const float* scale,
-                                   const void* z, const void* dy, const moce_project_grads& gr,
-                                   const ProjectBwdWs& ws, hipStream_t st);
+                                   const void* z, const void* dy, const moce_project_grads& gr, void* ws,
+                                   hipStream_t st);
 
 // The norm of a list of gradients and their clipping (gradclip.hip), over a validated list.
 size_t gradient_ws_bytes(const moce_gradient* g, int count);

@@ -18,6 +18,7 @@
 // neighbouring columns of one row.
 #include <algorithm>
 #include <climits>
+#include <cstdio>
 #include <type_traits>
 
 #include "moce_internal.h"
@@ -310,41 +311,6 @@ __device__ __forceinline__ f32x4 multiply(u32x4 col, u32x4 row, f32x4 acc) {
   }
 }
 
-// 16 bytes from element j of line i on, of lines below ni and elements below
-// nj; zeros outside.  Any alignment; a chunk may pass from one image to the
-// next.
-template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const Operand& o, int i, int ni, int j, int nj) {
-  constexpr int VE = Elem<T>::kVec;
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (i >= ni || j >= nj) return v;
-  const T* row = static_cast<const T*>(o.p) + i * o.ld;
-  int p = j;
-  if (o.hw) {
-    const int b = j / o.hw;
-    p = j - b * o.hw;
-    row += b * o.img;
-  }
-  if (j + VE <= nj && (o.hw == 0 || p + VE <= o.hw)) {
-    __builtin_memcpy(&v, row + p, 16);
-    return v;
-  }
-#pragma unroll
-  for (int e = 0; e < VE; ++e) {
-    if (j + e < nj) {
-      if constexpr (sizeof(T) == 2)
-        v[e / 2] |= (uint32_t)row[p] << (16 * (e & 1));
-      else
-        v[e] = __float_as_uint(row[p]);
-    }
-    if (++p == o.hw) {
-      p = 0;
-      row += o.img;
-    }
-  }
-  return v;
-}
-
 // The tile of a workgroup.  Workgroup u runs on XCD u mod 8 and takes the
 // (u / 8)-th of that XCD's eighth of the tiles, which go down kGroup rows of
 // tiles before they go across: the tiles that run together on an XCD share
@@ -445,71 +411,17 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[FR][FC]) {
     for (int j = 0; j < FC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// Any alignment: one tile of 32 FR rows by 32 FC columns, staged through
-// registers; AK, BK: operands along k.
-template <typename T, bool AK, bool BK, int FR, int FC>
-__global__ void __launch_bounds__(kThreads)
-k_project_any(GemmArgs g) {
-  constexpr int TR = 32 * FR, TC = 32 * FC;
-  using SA = Stage<T, AK, TR, false>;
-  using SB = Stage<T, BK, TC, true>;
-  constexpr int kDepth = SA::kDepth;
-  __shared__ __attribute__((aligned(16))) unsigned char la[SA::kBytes + SB::kBytes];
-  unsigned char* lb = la + SA::kBytes;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = (wave & 1) * 16 * FR, wc = (wave >> 1) * 16 * FC;
-  int r0, c0;
-  if (!tile_of(g, r0, c0)) return;
-  r0 *= TR, c0 *= TC;
-  const int k0 = blockIdx.y * g.klen, k1 = min(g.K, k0 + g.klen);
-
-  f32x4 acc[FR][FC];
-  clear(acc);
-  const int pa = SA::place(wr, lane), pb = SB::place(wc, lane);
-  for (int k = k0; k < k1; k += kDepth) {
-    auto fetch = [&](auto s, const Operand& o, bool along_k, int n0, int n, unsigned char* l) __attribute__((always_inline)) {
-      using S = decltype(s);
-#pragma unroll
-      for (int u = 0; u < S::kChunks / kThreads; ++u) {
-        const int q = tid + u * kThreads, i = q / S::kPerLine, c = q % S::kPerLine;
-        const u32x4 v = along_k ? load_chunk<T>(o, n0 + i, n, k + c * S::kVec, k1)
-                                : load_chunk<T>(o, k + i, k1, n0 + c * S::kVec, n);
-        *reinterpret_cast<u32x4*>(l + S::at(i, c)) = v;
-      }
-    };
-    __syncthreads();
-    fetch(SA{}, g.a, AK, r0, g.R, la);
-    fetch(SB{}, g.b, BK, c0, g.N, lb);
-    __syncthreads();
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      u32x4 fa[FR], fb[FC];
-#pragma unroll
-      for (int i = 0; i < FR; ++i) fa[i] = SA::frag(la, pa, i, ks);
-#pragma unroll
-      for (int j = 0; j < FC; ++j) fb[j] = SB::frag(lb, pb, j, ks);
-#pragma unroll
-      for (int i = 0; i < FR; ++i)
-#pragma unroll
-        for (int j = 0; j < FC; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-    }
-  }
-  __syncthreads();
-  constexpr int kPart = (SA::kBytes + SB::kBytes) / 4;
-  finish<T, kPart>(g, r0 + wr, c0 + wc, lane, acc, la + wave * kPart);
-}
-
-// ---- aligned lines: stages copied by the global-to-LDS loads ---------------------
+// ---- the product -----------------------------------------------------------------
 //
-// Where every line starts on 16 bytes and holds whole chunks (images too), a
-// stage goes to LDS without passing registers, two stages in LDS: while the
-// matrix cores work on the second half of stage s, whose operands are in
-// registers by then, stage s + 2 is copied over it; its own copies have the
-// time of a whole stage to arrive.  One barrier a stage.  The swizzle is in
-// the lane's source address.  Chunks past the contraction's end come from a
-// line of zeros; rows and columns past the tensor repeat its last ones, and
-// are not stored.
+// Operands' lines start on 16 bytes and hold whole chunks (images too; where
+// a tensor's do not, it is packed into lines that do first).  A stage goes to
+// LDS without passing registers, two stages in LDS: while the matrix cores
+// work on the last quarter of stage s, whose operands are in registers by
+// then, stage s + 2 is copied over it; its own copies have the time of a
+// whole stage to arrive.  One barrier a stage.  The swizzle is in the lane's
+// source address.  Chunks past the contraction's end come from a line of
+// zeros; rows and columns past the tensor repeat its last ones, and are not
+// stored.
 __device__ __align__(16) unsigned int zero_chunk[4];
 
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
@@ -569,7 +481,7 @@ struct Copier {
 #pragma unroll
       for (int u = 0; u < kRounds; ++u) {
         const int q = tid + u * NT, i = q / S::kPerLine, c = (q % S::kPerLine) ^ S::key(i);
-        const int j = min(n0 + c * S::kVec, n - S::kVec);
+        const int j = min(n0 + c * S::kVec, (n - 1) / S::kVec * S::kVec);   // a packed line's last chunk is whole too
         const int64_t at = o.hw ? (j / o.hw - b0) * o.img + j % o.hw : j;
         off[u] = (uint32_t)((i * o.ld + at) * ES);
       }
@@ -762,36 +674,34 @@ k_project_dweight(const float* __restrict__ part, int splits, int O, int C, cons
   if (threadIdx.x == 0) dscale[o] = dot;
 }
 
+// The passes over dy (and z) before the products; packing x or the weight is
+// the same pass without an activation.
 struct DzArgs {
   const void *z, *dy;
-  void *dz, *dzs;         // act'(z) dy, and scale times that (either may be nullptr)
-  const float* scale;
+  void* dz;               // act'(z) dy where dy's element is (nullptr: not written)
+  void* pack;             // the same, times scale where given, in lines of ld elements (nullptr: none)
+  const float* scale;     // by channel
   float* part;            // [groups][O] partial sums of dz over positions (nullptr: none)
-  int act, O, hw;
-  int64_t n;              // rows of positions (channels-last), planes (channels-first)
+  int act, O, hw, ld;     // O channels; hw positions of a plane (channels-first)
+  int64_t n;              // rows of positions (channels-last), images or planes (channels-first)
   int64_t per;            // rows of one group
 };
 
-// dz of eight neighbouring elements (n of them there) at e, scaled by sc for dzs
+// act'(z) dy of eight neighbouring elements (n of them there) at e, stored to dz
 template <typename T>
-__device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, const float (&sc)[8], float (&v)[8]) {
+__device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, float (&v)[8]) {
   using E = Elem<T>;
   const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
-  T *dz = static_cast<T*>(a.dz), *dzs = static_cast<T*>(a.dzs);
+  T* dz = static_cast<T*>(a.dz);
   if (n == 8) {
-    float q[8];
     load8(dy + e, v);
     if (a.act != MOCE_ACT_NONE) {
+      float q[8];
       load8(z + e, q);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = act_gradient<T>(q[i], v[i], a.act);
     }
     if (dz) store8(dz + e, v);
-    if (dzs) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = v[i] * sc[i];
-      store8(dzs + e, q);
-    }
     return;
   }
 #pragma unroll
@@ -801,13 +711,12 @@ __device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, const flo
       v[i] = E::to_f(dy[e + i]);
       if (a.act != MOCE_ACT_NONE) v[i] = act_gradient<T>(E::to_f(z[e + i]), v[i], a.act);
       if (dz) dz[e + i] = E::from_f(v[i]);
-      if (dzs) dzs[e + i] = E::from_f(v[i] * sc[i]);
     }
   }
 }
 
 // Channels-last: a workgroup takes 8 tx channels of a group of rows, its
-// threads tx across and 256 / tx down.
+// threads tx across and 256 / tx down; pack: rows of ld, zeros behind O.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_project_dz_rows(DzArgs a, int tx) {
@@ -816,14 +725,26 @@ k_project_dz_rows(DzArgs a, int tx) {
   const int c = (blockIdx.y * tx + x) * 8, n = min(8, a.O - c);
   float sum[8] = {}, sc[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sc[i] = a.dzs ? a.scale[max(0, min(c + i, a.O - 1))] : 1.f;
+  for (int i = 0; i < 8; ++i) sc[i] = a.pack && a.scale ? a.scale[min(c + i, a.O - 1)] : 1.f;
   if (n > 0) {
     const int64_t end = min(a.n, (blockIdx.x + (int64_t)1) * a.per);
     for (int64_t r = blockIdx.x * a.per + threadIdx.x / tx; r < end; r += down) {
       float v[8];
-      dz8<T>(a, r * a.O + c, n, sc, v);
+      dz8<T>(a, r * a.O + c, n, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += v[i];
+      if (a.pack) {
+        T* p = static_cast<T*>(a.pack) + r * a.ld + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= sc[i];
+        if (c + 8 <= a.ld) {
+          store8(p, v);
+        } else {   // float32: a line may end after four
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c + i < a.ld) p[i] = Elem<T>::from_f(v[i]);
+        }
+      }
     }
   }
   if (!a.part) return;
@@ -838,25 +759,88 @@ k_project_dz_rows(DzArgs a, int tx) {
   }
 }
 
-// Channels-first: `lanes` lanes (a power of two up to 64) take a plane.
+// Channels-first, lines of whole chunks: `lanes` lanes (a power of two up to
+// 64) take a plane; pack: planes as dy's.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_project_dz_planes(DzArgs a, int lanes) {
   const int64_t plane = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
-  float sum = 0.f, sc[8];
+  float sum = 0.f;
   if (plane < a.n) {
-    const float f = a.dzs ? a.scale[plane % a.O] : 1.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sc[i] = f;
+    const float sc = a.pack && a.scale ? a.scale[plane % a.O] : 1.f;
     for (int p = (threadIdx.x % lanes) * 8; p < a.hw; p += lanes * 8) {
       float v[8];
-      dz8<T>(a, plane * a.hw + p, min(8, a.hw - p), sc, v);
+      const int64_t e = plane * a.hw + p;
+      const int n = min(8, a.hw - p);
+      dz8<T>(a, e, n, v);
       sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+      if (a.pack) {
+        T* q = static_cast<T*>(a.pack) + e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= sc;
+        if (n == 8) {
+          store8(q, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < n) q[i] = Elem<T>::from_f(v[i]);
+        }
+      }
     }
   }
   if (!a.part) return;
   for (int o = lanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
   if (plane < a.n && threadIdx.x % lanes == 0) a.part[plane] = sum;
+}
+
+// Channels-first to lines of channels: a workgroup turns 64 channels by 64
+// positions of an image through LDS, a wave 16 channels, a lane a position;
+// pack: [position][ld], zeros behind O.  part: a group per 64 positions.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_project_turn(DzArgs a, int across) {
+  using E = Elem<T>;
+  constexpr int kPitch = 64 + 4 / (int)sizeof(T) * 1;   // odd words: lanes down a column on different banks
+  __shared__ T s[64 * kPitch];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t u = blockIdx.x;                         // image and run of positions
+  const int64_t b = u / across;
+  const int p = (int)(u % across) * 64 + lane, c0 = blockIdx.y * 64;
+  const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
+  T* dz = static_cast<T*>(a.dz);
+  float v[16], q[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int c = c0 + 16 * wave + i;
+    const int64_t e = (b * a.O + min(c, a.O - 1)) * a.hw + min(p, a.hw - 1);
+    v[i] = E::to_f(dy[e]);
+    q[i] = a.act != MOCE_ACT_NONE ? E::to_f(z[e]) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int c = c0 + 16 * wave + i;
+    const bool there = c < a.O && p < a.hw;
+    v[i] = there ? act_gradient<T>(q[i], v[i], a.act) : 0.f;
+    if (dz && there) dz[(b * a.O + c) * a.hw + p] = E::from_f(v[i]);
+    if (a.part) {
+      const float t = wave_sum(v[i]);
+      if (lane == 0 && c < a.O) a.part[u * a.O + c] = t;
+    }
+    if (a.pack) s[lane * kPitch + 16 * wave + i] = E::from_f(a.scale ? v[i] * a.scale[min(c, a.O - 1)] : v[i]);
+  }
+  if (!a.pack) return;
+  __syncthreads();
+  // a thread writes 16 bytes of a position's line at a time
+  constexpr int kVec = E::kVec, kLanes = 64 / kVec;
+#pragma unroll
+  for (int i = threadIdx.x; i < 64 * kLanes; i += kThreads) {
+    const int row = i / kLanes, c = i % kLanes * kVec, at = (int)(u % across) * 64 + row;
+    if (at >= a.hw || c0 + c >= a.ld) continue;
+    T w[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) w[j] = s[row * kPitch + c + j];
+    __builtin_memcpy(static_cast<T*>(a.pack) + (b * a.hw + at) * a.ld + c0 + c, w, 16);
+  }
 }
 
 // dshift[o] = sum over the groups' partial sums
@@ -876,14 +860,14 @@ k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* _
   }
 }
 
-// scale[o] weight[o][c], rounded to the weight's type
+// scale[o] weight[o][c] (scale may be nullptr), rounded to the weight's type, in lines of ld, zeros behind C
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-k_project_scale(const T* __restrict__ weight, const float* __restrict__ scale, int C, T* __restrict__ out) {
+k_project_weight(const T* __restrict__ weight, const float* __restrict__ scale, int C, int ld, T* __restrict__ out) {
   const int o = blockIdx.x;
-  const float s = scale[o];
-  for (int c = threadIdx.x; c < C; c += kThreads)
-    out[(int64_t)o * C + c] = Elem<T>::from_f(s * Elem<T>::to_f(weight[(int64_t)o * C + c]));
+  const float s = scale ? scale[o] : 1.f;
+  for (int c = threadIdx.x; c < ld; c += kThreads)
+    out[(int64_t)o * ld + c] = c < C ? Elem<T>::from_f(s * Elem<T>::to_f(weight[(int64_t)o * C + c])) : (T)0;
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -892,31 +876,32 @@ constexpr int kWantTiles = 512;          // two workgroups a CU
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a product is cut: tiles of `tile` rows and columns and, where these
+// How a product is cut: tiles of tr rows and tc columns and, where these
 // make too few workgroups for the GPU, the contraction in lengths of 256 or more.
 struct Plan {
-  int tile, splits, klen;
+  int tr, tc, splits, klen;
 };
-Plan plan(int64_t R, int64_t N, int64_t K, int elem) {
+Plan split_plan(int tr, int tc, int64_t s, int64_t K, int elem) {
   const int depth = kLine / (elem == MOCE_F32 ? 4 : 2);
+  s = std::min<int64_t>(std::max<int64_t>(s, 1), 256);
+  const int64_t klen = ceil_div(ceil_div(K, s), depth) * depth;
+  return Plan{tr, tc, (int)ceil_div(K, klen), (int)klen};
+}
+Plan sweep_plan(int64_t R, int64_t N, int64_t K, int elem, const char* e) {
+  int tr = 64, tc = 64, s = 0;
+  sscanf(e, "%dx%d/%d", &tr, &tc, &s);
+  if (s == 0) s = (int)std::min(std::max<int64_t>(1, kWantTiles / (ceil_div(R, tr) * ceil_div(N, tc))), std::max<int64_t>(1, K / 256));
+  return split_plan(tr, tc, s, K, elem);
+}
+Plan plan(int64_t R, int64_t N, int64_t K, int elem) {
+  // sweep
   int tile = 64;
   if (ceil_div(R, 128) * ceil_div(N, 128) >= 256) tile = 128;
   if (elem == MOCE_BF16 && ceil_div(R, 256) * ceil_div(N, 256) >= 256) tile = 256;
   const int64_t tiles = ceil_div(R, tile) * ceil_div(N, tile);
-  int64_t s = std::min(std::max<int64_t>(1, kWantTiles / tiles), std::max<int64_t>(1, K / 256));
-  s = std::min<int64_t>(s, 256);
-  const int64_t klen = ceil_div(ceil_div(K, s), depth) * depth;
-  return Plan{tile, (int)ceil_div(K, klen), (int)klen};
+  return split_plan(tile, tile, std::min(std::max<int64_t>(1, kWantTiles / tiles), std::max<int64_t>(1, K / 256)), K, elem);
 }
 size_t part_bytes(int64_t R, int64_t N, const Plan& p) { return (size_t)p.splits * R * N * sizeof(float); }
-
-// Whether the copying kernel can read this operand: whole chunks, at offsets of 31 bits within a tile.
-bool whole_chunks(const Operand& o, bool along_k, int64_t length, int elem) {
-  const int es = elem == MOCE_F32 ? 4 : 2, vec = 16 / es;
-  if (o.ld % vec || o.hw % vec || length % vec) return false;
-  const int64_t span = along_k ? 256 * o.ld : (kLine / es) * o.ld + (o.hw ? (256 / o.hw + 2) * o.img : 0);
-  return span * es < INT_MAX;
-}
 
 template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int F, int FC>
 void launch_copy(GemmArgs g, int splits, hipStream_t st) {
@@ -925,32 +910,24 @@ void launch_copy(GemmArgs g, int splits, hipStream_t st) {
   hipLaunchKernelGGL((k_project_copy<T, AK, BK, IMG, WR, WC, F, FC>), grid, dim3(64 * WR * WC), 0, st, g);
 }
 
-template <typename T, bool AK, bool BK, int F>
-void launch_any(GemmArgs g, int splits, hipStream_t st) {
-  g.tr = (int)ceil_div(g.R, 32 * F), g.tc = (int)ceil_div(g.N, 32 * F);
-  const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc, 8) * 8), splits);
-  hipLaunchKernelGGL((k_project_any<T, AK, BK, F, F>), grid, dim3(kThreads), 0, st, g);
-}
-
 template <typename T, bool AK, bool BK>
 hipError_t launch_product(const GemmArgs& g, const Plan& p, hipStream_t st) {
-  const int elem = sizeof(T) == 4 ? MOCE_F32 : MOCE_BF16;
-  const bool whole = whole_chunks(g.a, AK, AK ? g.K : g.R, elem) && whole_chunks(g.b, BK, BK ? g.K : g.N, elem);
   auto copy = [&](auto img) {
     constexpr bool IMG = decltype(img)::value;
-    if (p.tile == 64)
-      launch_copy<T, AK, BK, IMG, 2, 2, 2, 2>(g, p.splits, st);
-    else if (p.tile == 128 || sizeof(T) == 4)
-      launch_copy<T, AK, BK, IMG, 2, 2, 4, 4>(g, p.splits, st);
-    else if constexpr (sizeof(T) == 2)
-      launch_copy<T, AK, BK, IMG, 2, 4, 8, 4>(g, p.splits, st);
+    const int t = p.tr * 1000 + p.tc;
+    if (t == 64064) launch_copy<T, AK, BK, IMG, 2, 2, 2, 2>(g, p.splits, st);
+    else if (t == 128128 || sizeof(T) == 4) launch_copy<T, AK, BK, IMG, 2, 2, 4, 4>(g, p.splits, st);
+    else if constexpr (sizeof(T) == 2) {
+      if (t == 256256) launch_copy<T, AK, BK, IMG, 2, 4, 8, 4>(g, p.splits, st);
+      if (t == 128064) launch_copy<T, AK, BK, IMG, 2, 2, 4, 2>(g, p.splits, st);
+      if (t == 64128) launch_copy<T, AK, BK, IMG, 2, 2, 2, 4>(g, p.splits, st);
+      if (t == 256128) launch_copy<T, AK, BK, IMG, 4, 2, 4, 4>(g, p.splits, st);
+      if (t == 128256) launch_copy<T, AK, BK, IMG, 2, 4, 4, 4>(g, p.splits, st);
+      if (t == 256064) launch_copy<T, AK, BK, IMG, 4, 1, 4, 4>(g, p.splits, st);
+      if (t == 64256) launch_copy<T, AK, BK, IMG, 1, 4, 4, 4>(g, p.splits, st);
+    }
   };
-  if (!whole) {
-    if (p.tile == 64)
-      launch_any<T, AK, BK, 2>(g, p.splits, st);
-    else
-      launch_any<T, AK, BK, 4>(g, p.splits, st);
-  } else if constexpr (AK && BK) {
+  if constexpr (AK && BK) {
     if (g.a.hw)
       copy(std::true_type{});
     else
@@ -978,37 +955,152 @@ hipError_t launch_whole(GemmArgs g, const Plan& p, float* part, hipStream_t st) 
   return launch_join<T>(g, p.splits, st);
 }
 
-// The positions' part of a channels-first tensor of n channels
-int images(const ProjectShape& s) { return s.layout == MOCE_NCHW && s.B > 1 ? (int)s.HW : 0; }
+// ---- which operands are packed ---------------------------------------------------
+
+constexpr int64_t kSpan = INT_MAX;   // bytes that a tile's offsets reach
+
+struct Sizes {
+  const ProjectShape& s;
+  int vec;
+  bool nhwc;
+  explicit Sizes(const ProjectShape& s) : s(s), vec(s.elem == MOCE_F32 ? 4 : 8), nhwc(s.layout == MOCE_NHWC) {}
+  size_t el() const { return 16 / vec; }
+  int64_t P() const { return s.B * s.HW; }
+  int64_t up(int64_t n) const { return (n + vec - 1) / vec * vec; }
+  // Tensors whose lines are not whole chunks are packed: a weight of ragged
+  // C, channels-last tensors of ragged channels, channels-first ones of
+  // ragged planes (turned into lines of channels).  Offsets within a tile
+  // have 31 bits: planes beyond that are turned too.
+  bool weight() const { return s.C % vec != 0; }
+  bool planes() const {
+    const int64_t n = std::max(s.C, s.O);
+    return !nhwc && (s.HW % vec != 0 || (256 * s.HW + (256 / s.HW + 2) * n * s.HW) * (int64_t)el() > kSpan);
+  }
+  bool rows(int64_t channels) const { return nhwc ? channels % vec != 0 : planes(); }
+  size_t packed(int64_t channels) const { return (size_t)P() * up(channels) * el(); }
+  // positions' lines run over images
+  int images() const { return !nhwc && s.B > 1 ? (int)s.HW : 0; }
+};
+
+template <typename T>
+hipError_t pack_rows(const void* src, int64_t rows, int64_t channels, void* out, int64_t ld, hipStream_t st) {
+  DzArgs a{};
+  a.dy = src, a.pack = out, a.O = (int)channels, a.ld = (int)ld, a.n = rows;
+  int tx = 1;
+  while (tx < 32 && tx * 8 < channels) tx *= 2;
+  a.per = ceil_div(ceil_div(rows, 2048), kThreads / tx) * (kThreads / tx);
+  hipLaunchKernelGGL(k_project_dz_rows<T>, dim3((unsigned)ceil_div(rows, a.per), (unsigned)ceil_div(channels, tx * 8)),
+                     dim3(kThreads), 0, st, a, tx);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_turn(const DzArgs& a, hipStream_t st) {
+  const int across = (int)ceil_div(a.hw, 64);
+  return image_slices(a.n, (int64_t)across * kThreads, 1, [&](int64_t b, int64_t n) {
+    DzArgs p = a;
+    const int64_t at = b * a.O * a.hw;
+    auto on = [&](const void* q) { return const_cast<T*>(static_cast<const T*>(q) + at); };
+    p.dy = on(a.dy);
+    if (a.z) p.z = on(a.z);
+    if (a.dz) p.dz = on(a.dz);
+    if (a.pack) p.pack = static_cast<T*>(a.pack) + b * a.hw * a.ld;
+    if (a.part) p.part = a.part + b * across * a.O;
+    hipLaunchKernelGGL(k_project_turn<T>, dim3((unsigned)(n * across), (unsigned)ceil_div(a.O, 64)), dim3(kThreads), 0,
+                       st, p, across);
+    return hipGetLastError();
+  });
+}
+// Images of channels planes of hw positions into lines of channels, times scale (may be nullptr).
+template <typename T>
+hipError_t turn(const void* src, int64_t images, int64_t channels, int64_t hw, const float* scale, void* out,
+                int64_t ld, hipStream_t st) {
+  DzArgs a{};
+  a.dy = src, a.pack = out, a.scale = scale, a.O = (int)channels, a.hw = (int)hw, a.ld = (int)ld, a.n = images;
+  return launch_turn<T>(a, st);
+}
+// x (or dy) as the products read it: packed into `out` where its lines are ragged.
+template <typename T>
+hipError_t pack_tensor(const Sizes& z, const void** t, int64_t channels, void* out, hipStream_t st) {
+  if (!z.rows(channels)) return hipSuccess;
+  const void* src = *t;
+  *t = out;
+  return z.nhwc ? pack_rows<T>(src, z.P(), channels, out, z.up(channels), st)
+                : turn<T>(src, z.s.B, channels, z.s.HW, nullptr, out, z.up(channels), st);
+}
+template <typename T>
+hipError_t pack_weight(const Sizes& z, const void** w, const float* scale, void* out, hipStream_t st) {
+  if (!z.weight() && !scale) return hipSuccess;
+  hipLaunchKernelGGL(k_project_weight<T>, dim3((unsigned)z.s.O), dim3(kThreads), 0, st, static_cast<const T*>(*w), scale,
+                     (int)z.s.C, (int)z.up(z.s.C), static_cast<T*>(out));
+  *w = out;
+  return hipGetLastError();
+}
+
+// Rows and columns of the output, of `channels` channels, as the products write it
+void output(GemmArgs* g, const Sizes& z, int64_t channels) {
+  const int64_t P = z.P();
+  g->R = (int)(z.nhwc ? P : channels), g->N = (int)(z.nhwc ? channels : P);
+  g->ld = z.nhwc ? channels : z.s.HW, g->hw = z.images(), g->img = channels * z.s.HW;
+}
+
+struct FwdLayout {
+  Plan p;
+  size_t x, weight, part, total;
+};
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+FwdLayout fwd_layout(const ProjectShape& s) {
+  const Sizes z(s);
+  FwdLayout l{};
+  GemmArgs g{};
+  output(&g, z, s.O);
+  l.p = plan(g.R, g.N, s.C, s.elem);
+  l.x = 0;
+  l.weight = l.x + (z.rows(s.C) ? up256(z.packed(s.C)) : 0);
+  l.part = l.weight + (z.weight() ? up256((size_t)s.O * z.up(s.C) * z.el()) : 0);
+  l.total = l.part + (l.p.splits > 1 ? part_bytes(g.R, g.N, l.p) : 0);
+  return l;
+}
 
 template <typename T>
 hipError_t forward(const ProjectShape& s, const void* x, const void* w, const float* scale, const float* shift,
-                   const void* res, void* y, void* z, float* part, hipStream_t st) {
-  const int P = (int)(s.B * s.HW), hw = images(s);
+                   const void* res, void* y, void* z_out, char* ws, hipStream_t st) {
+  const Sizes z(s);
+  const FwdLayout l = fwd_layout(s);
+  const bool turned = !z.nhwc && z.planes();
+  hipError_t e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);
+  if (e == hipSuccess) e = pack_weight<T>(z, &w, nullptr, ws + l.weight, st);
+  if (e != hipSuccess) return e;
   GemmArgs g{};
+  output(&g, z, s.O);
   g.K = (int)s.C;
-  g.scale = scale, g.shift = shift, g.res = res, g.y = y, g.z = z, g.act = s.act;
-  const Operand wo{w, s.C, 0, 0};
-  if (s.layout == MOCE_NHWC) {
-    g.a = Operand{x, s.C, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.O, g.ld = s.O;
-    return launch_whole<T, true, true>(g, plan(g.R, g.N, g.K, s.elem), part, st);
+  g.scale = scale, g.shift = shift, g.res = res, g.y = y, g.z = z_out, g.act = s.act, g.per_row = !z.nhwc;
+  const Operand wo{w, z.up(s.C), 0, 0}, xo{x, z.up(s.C), 0, 0};
+  float* part = reinterpret_cast<float*>(ws + l.part);
+  if (z.nhwc) {
+    g.a = xo, g.b = wo;
+    return launch_whole<T, true, true>(g, l.p, part, st);
   }
-  g.a = wo, g.b = Operand{x, s.HW, s.C * s.HW, hw}, g.R = (int)s.O, g.N = P, g.per_row = 1;
-  g.ld = s.HW, g.img = s.O * s.HW, g.hw = hw;
-  return launch_whole<T, true, false>(g, plan(g.R, g.N, g.K, s.elem), part, st);
+  g.a = wo;
+  if (turned) {
+    g.b = xo;
+    return launch_whole<T, true, true>(g, l.p, part, st);
+  }
+  g.b = Operand{x, s.HW, s.C * s.HW, z.images()};
+  return launch_whole<T, true, false>(g, l.p, part, st);
 }
 
 // Groups of positions whose sums of dz lie apart: rows (channels-last) in up
-// to 1024 workgroups, images (channels-first).
+// to 1024 workgroups, images or 64 positions of them (channels-first).
 struct DzPlan {
   int tx;
   int64_t per, groups;
 };
-DzPlan dz_plan(const ProjectShape& s) {
-  if (s.layout == MOCE_NCHW) return DzPlan{0, 0, s.B};
+DzPlan dz_plan(const Sizes& z) {
+  const ProjectShape& s = z.s;
+  if (!z.nhwc) return DzPlan{0, 0, z.planes() ? s.B * ceil_div(s.HW, 64) : s.B};
   int tx = 1;
   while (tx < 32 && tx * 8 < s.O) tx *= 2;
-  const int64_t M = s.B * s.HW, across = ceil_div(s.O, tx * 8), down = kThreads / tx;
+  const int64_t M = z.P(), across = ceil_div(s.O, tx * 8), down = kThreads / tx;
   const int64_t want = std::max<int64_t>(1, 1024 / across);
   const int64_t per = ceil_div(ceil_div(M, want), down) * down;
   return DzPlan{tx, per, ceil_div(M, per)};
@@ -1023,132 +1115,159 @@ bool project_limits(const ProjectShape& s) {
   return s.B <= ((int64_t)1 << 29) / s.HW && s.B <= ((int64_t)1 << 33) / (std::max(s.C, s.O) * s.HW);
 }
 
-size_t project_ws_bytes(const ProjectShape& s) {
-  const bool nhwc = s.layout == MOCE_NHWC;
-  const int64_t P = s.B * s.HW, R = nhwc ? P : s.O, N = nhwc ? s.O : P;
-  const Plan p = plan(R, N, s.C, s.elem);
-  return p.splits > 1 ? part_bytes(R, N, p) : 0;
-}
+size_t project_ws_bytes(const ProjectShape& s) { return fwd_layout(s).total; }
 
 hipError_t launch_project(const ProjectShape& s, const void* x, const void* w, const float* scale, const float* shift,
                           const void* res, void* y, void* z, void* ws, hipStream_t st) {
-  float* part = static_cast<float*>(ws);
-  return s.elem == MOCE_F32 ? forward<float>(s, x, w, scale, shift, res, y, z, part, st)
-                            : forward<uint16_t>(s, x, w, scale, shift, res, y, z, part, st);
-}
-
-ProjectBwdSizes project_backward_sizes(const ProjectShape& s) {
-  const size_t el = s.elem == MOCE_F32 ? 4 : 2;
-  const int64_t P = s.B * s.HW;
-  const bool nhwc = s.layout == MOCE_NHWC;
-  const Plan px = nhwc ? plan(P, s.C, s.O, s.elem) : plan(s.C, P, s.O, s.elem);
-  const Plan pw = plan(s.O, s.C, P, s.elem);
-  ProjectBwdSizes z{};
-  z.dz = s.act == MOCE_ACT_NONE ? 0 : (size_t)P * s.O * el;
-  z.weight = (size_t)s.O * s.C * el;
-  z.shift = (size_t)dz_plan(s).groups * s.O * sizeof(float);
-  // one after the other on the stream, so both products' partial sums share their place
-  z.part = std::max(px.splits > 1 ? part_bytes(P, s.C, px) : 0, part_bytes(s.O, s.C, pw));
-  return z;
+  char* base = static_cast<char*>(ws);
+  return s.elem == MOCE_F32 ? forward<float>(s, x, w, scale, shift, res, y, z, base, st)
+                            : forward<uint16_t>(s, x, w, scale, shift, res, y, z, base, st);
 }
 
 namespace {
 
+struct BwdLayout {
+  Plan px, pw;
+  size_t dz, x, weight, shift, part, total;
+};
+BwdLayout bwd_layout(const ProjectShape& s) {
+  const Sizes z(s);
+  BwdLayout l{};
+  GemmArgs g{};
+  output(&g, z, s.C);
+  l.px = plan(g.R, g.N, s.O, s.elem);
+  l.pw = plan(s.O, s.C, z.P(), s.elem);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t here = at;
+    at += up256(n);
+    return here;
+  };
+  l.dz = take(s.act != MOCE_ACT_NONE || z.rows(s.O) ? z.packed(s.O) : 0);
+  l.x = take(z.rows(s.C) ? z.packed(s.C) : 0);
+  l.weight = take((size_t)std::max(s.O * z.up(s.C), z.up(s.O) * s.C) * z.el());
+  l.shift = take((size_t)dz_plan(z).groups * s.O * sizeof(float));
+  // one after the other on the stream, so both products' partial sums share their place
+  l.part = take(std::max(l.px.splits > 1 ? part_bytes(g.R, g.N, l.px) : 0, part_bytes(s.O, s.C, l.pw)));
+  l.total = at;
+  return l;
+}
+
 template <typename T>
-hipError_t backward(const ProjectShape& s, const void* x, const void* w, const float* scale, const void* z,
-                    const void* dy, const moce_project_grads& gr, const ProjectBwdWs& ws, hipStream_t st) {
-  const int P = (int)(s.B * s.HW), hw = images(s);
-  const bool nhwc = s.layout == MOCE_NHWC;
+hipError_t backward(const ProjectShape& s, const void* x, const void* w, const float* scale, const void* z_in,
+                    const void* dy, const moce_project_grads& gr, char* ws, hipStream_t st) {
+  const Sizes z(s);
+  const BwdLayout l = bwd_layout(s);
   const bool smooth = s.act == MOCE_ACT_GELU || s.act == MOCE_ACT_SILU;
+  const bool turned = !z.nhwc && z.planes();
   // Where dz is rounded anyway, the scale goes into it before the rounding
   // (one rounding, not two); where dz is dy or 0, into the weight of dx and
   // the rows of dW.
   const bool fold = scale && smooth;
+  const float* row_scale = fold ? nullptr : scale;
   const bool products = gr.dx || gr.dweight || gr.dscale;
+  const bool ragged = z.rows(s.O);
   const void* dz = dy;
-  hipError_t e;
+  hipError_t e = hipSuccess;
   {
     DzArgs a{};
-    a.z = z, a.dy = dy, a.act = s.act, a.O = (int)s.O, a.hw = (int)s.HW, a.scale = scale;
+    a.z = z_in, a.dy = dy, a.act = s.act, a.O = (int)s.O, a.hw = (int)s.HW, a.scale = fold ? scale : nullptr;
     a.dz = gr.dresidual != dy || s.act != MOCE_ACT_NONE ? gr.dresidual : nullptr;
-    if (fold) {
-      if (products) dz = a.dzs = ws.dz;
-    } else if (s.act != MOCE_ACT_NONE && products) {
-      if (!a.dz) a.dz = ws.dz;
+    a.ld = (int)(!z.nhwc && !turned ? s.HW : z.up(s.O));
+    if (products && (ragged || fold)) {
+      dz = a.pack = ws + l.dz;
+    } else if (products && s.act != MOCE_ACT_NONE) {
+      if (!a.dz) a.dz = ws + l.dz;
       dz = a.dz;
     }
-    a.part = gr.dshift ? ws.shift : nullptr;
-    const DzPlan dp = dz_plan(s);
-    if (a.dz || a.dzs || a.part) {
-      if (nhwc) {
-        a.n = P, a.per = dp.per;
+    a.part = gr.dshift ? reinterpret_cast<float*>(ws + l.shift) : nullptr;
+    const DzPlan dp = dz_plan(z);
+    if (a.dz || a.pack || a.part) {
+      if (z.nhwc) {
+        a.n = z.P(), a.per = dp.per;
         hipLaunchKernelGGL(k_project_dz_rows<T>, dim3((unsigned)dp.groups, (unsigned)ceil_div(s.O, dp.tx * 8)),
                            dim3(kThreads), 0, st, a, dp.tx);
+        e = hipGetLastError();
+      } else if (turned) {
+        a.n = s.B;
+        e = launch_turn<T>(a, st);
       } else {
         int lanes = 1;
         while (lanes < 64 && lanes * 8 < s.HW) lanes *= 2;
         a.n = s.B * s.O;
         hipLaunchKernelGGL(k_project_dz_planes<T>, dim3((unsigned)ceil_div(a.n, kThreads / lanes)), dim3(kThreads), 0,
                            st, a, lanes);
+        e = hipGetLastError();
       }
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (e != hipSuccess) return e;
     }
     if (gr.dshift) {
-      hipLaunchKernelGGL(k_project_dshift, dim3((unsigned)ceil_div(s.O, 64)), dim3(1024), 0, st, ws.shift, dp.groups,
+      hipLaunchKernelGGL(k_project_dshift, dim3((unsigned)ceil_div(s.O, 64)), dim3(1024), 0, st, a.part, dp.groups,
                          (int)s.O, gr.dshift);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
-  const float* row_scale = fold ? nullptr : scale;
+  float* part = reinterpret_cast<float*>(ws + l.part);
+  const Operand dzo{dz, z.up(s.O), 0, 0}, dzp{dz, s.HW, s.O * s.HW, z.images()};   // lines of channels, of positions
   if (gr.dx) {
-    if (row_scale) {
-      hipLaunchKernelGGL(k_project_scale<T>, dim3((unsigned)s.O), dim3(kThreads), 0, st, static_cast<const T*>(w),
-                         scale, (int)s.C, static_cast<T*>(ws.weight));
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
     GemmArgs g{};
-    const Operand wo{row_scale ? ws.weight : w, s.C, 0, 0};
+    output(&g, z, s.C);
     g.K = (int)s.O, g.y = gr.dx;
-    if (nhwc) {
-      g.a = Operand{dz, s.O, 0, 0}, g.b = wo, g.R = P, g.N = (int)s.C, g.ld = s.C;
-      e = launch_whole<T, true, false>(g, plan(g.R, g.N, g.K, s.elem), ws.part, st);
+    if (turned) {
+      // the weight turned too, so that both operands run along the outputs
+      e = turn<T>(w, 1, s.O, s.C, row_scale, ws + l.weight, z.up(s.O), st);
+      if (e != hipSuccess) return e;
+      g.a = Operand{ws + l.weight, z.up(s.O), 0, 0}, g.b = dzo;
+      e = launch_whole<T, true, true>(g, l.px, part, st);
     } else {
-      g.a = wo, g.b = Operand{dz, s.HW, s.O * s.HW, hw}, g.R = (int)s.C, g.N = P;
-      g.ld = s.HW, g.img = s.C * s.HW, g.hw = hw;
-      e = launch_whole<T, false, false>(g, plan(g.R, g.N, g.K, s.elem), ws.part, st);
+      const void* wp = w;
+      e = pack_weight<T>(z, &wp, row_scale, ws + l.weight, st);
+      if (e != hipSuccess) return e;
+      const Operand wo{wp, z.up(s.C), 0, 0};
+      if (z.nhwc) {
+        g.a = dzo, g.b = wo;
+        e = launch_whole<T, true, false>(g, l.px, part, st);
+      } else {
+        g.a = wo, g.b = dzp;
+        e = launch_whole<T, false, false>(g, l.px, part, st);
+      }
     }
     if (e != hipSuccess) return e;
   }
   if (gr.dweight || gr.dscale) {
+    e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);
+    if (e != hipSuccess) return e;
     GemmArgs g{};
-    const Plan p = plan(s.O, s.C, P, s.elem);
-    g.R = (int)s.O, g.N = (int)s.C, g.K = P, g.ld = s.C, g.y = gr.dweight, g.klen = p.klen;
-    const bool join = row_scale || p.splits > 1;
-    if (join) g.part = ws.part;
-    if (nhwc) {
-      g.a = Operand{dz, s.O, 0, 0}, g.b = Operand{x, s.C, 0, 0};
-      e = launch_product<T, false, false>(g, p, st);
+    g.R = (int)s.O, g.N = (int)s.C, g.K = (int)z.P(), g.ld = s.C, g.y = gr.dweight, g.klen = l.pw.klen;
+    const bool join = row_scale || l.pw.splits > 1;
+    if (join) g.part = part;
+    if (z.nhwc || turned) {
+      g.a = dzo, g.b = Operand{x, z.up(s.C), 0, 0};
+      e = launch_product<T, false, false>(g, l.pw, st);
     } else {
-      g.a = Operand{dz, s.HW, s.O * s.HW, hw}, g.b = Operand{x, s.HW, s.C * s.HW, hw};
-      e = launch_product<T, true, true>(g, p, st);
+      g.a = dzp, g.b = Operand{x, s.HW, s.C * s.HW, z.images()};
+      e = launch_product<T, true, true>(g, l.pw, st);
     }
     if (e != hipSuccess) return e;
     if (join) {
-      hipLaunchKernelGGL(k_project_dweight<T>, dim3((unsigned)s.O), dim3(kThreads), 0, st, ws.part, p.splits, (int)s.O,
+      hipLaunchKernelGGL(k_project_dweight<T>, dim3((unsigned)s.O), dim3(kThreads), 0, st, part, l.pw.splits, (int)s.O,
                          (int)s.C, row_scale, static_cast<const T*>(w), static_cast<T*>(gr.dweight), gr.dscale);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      e = hipGetLastError();
     }
   }
-  return hipSuccess;
+  return e;
 }
 
 }  // namespace
 
+size_t project_backward_ws_bytes(const ProjectShape& s) { return bwd_layout(s).total; }
+
 hipError_t launch_project_backward(const ProjectShape& s, const void* x, const void* w, const float* scale,
-                                   const void* z, const void* dy, const moce_project_grads& gr,
-                                   const ProjectBwdWs& ws, hipStream_t st) {
-  return s.elem == MOCE_F32 ? backward<float>(s, x, w, scale, z, dy, gr, ws, st)
-                            : backward<uint16_t>(s, x, w, scale, z, dy, gr, ws, st);
+                                   const void* z, const void* dy, const moce_project_grads& gr, void* ws,
+                                   hipStream_t st) {
+  char* base = static_cast<char*>(ws);
+  return s.elem == MOCE_F32 ? backward<float>(s, x, w, scale, z, dy, gr, base, st)
+                            : backward<uint16_t>(s, x, w, scale, z, dy, gr, base, st);
 }
 
 }  // namespace moce
