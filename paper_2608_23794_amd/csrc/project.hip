@@ -18,7 +18,6 @@
 // neighbouring columns of one row.
 #include <algorithm>
 #include <climits>
-#include <cstdio>
 #include <type_traits>
 
 #include "moce_internal.h"
@@ -94,6 +93,28 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   __builtin_memcpy(p, &u, 16);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
+
+__device__ __forceinline__ void load4(const uint16_t* p, float* v) {
+  uint32_t u[2];
+  __builtin_memcpy(u, p, 8);
+  v[0] = bf16_lo(u[0]), v[1] = bf16_hi(u[0]), v[2] = bf16_lo(u[1]), v[3] = bf16_hi(u[1]);
+}
+__device__ __forceinline__ void load4(const float* p, float* v) { __builtin_memcpy(v, p, 16); }
+__device__ __forceinline__ void store4(uint16_t* p, const float* v) {
+  const uint32_t u[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  __builtin_memcpy(p, u, 8);
+}
+__device__ __forceinline__ void store4(float* p, const float* v) { __builtin_memcpy(p, v, 16); }
+
+// The same past the caches, for results in whole aligned rows.
+__device__ __forceinline__ void stream8(uint16_t* p, const float (&v)[8]) {
+  const u32x4 u = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  __builtin_nontemporal_store(u, reinterpret_cast<u32x4*>(p));
+}
+__device__ __forceinline__ void stream8(float* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p + 4));
+}
 
 // ---- activations -------------------------------------------------------------
 // The standard normal distribution function of z, and e^(-z^2 / 2) beside it.
@@ -181,40 +202,43 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, int r, int c, int spl
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], sc[i], sh[i]);
-  int64_t base = (int64_t)r * g.ld;
-  int p = c;
-  if (g.hw) {
-    const int b = c / g.hw;
-    p = c - b * g.hw;
-    base += b * g.img;
-  }
-  T* y = static_cast<T*>(g.y) + base;
-  T* z = g.z ? static_cast<T*>(g.z) + base : nullptr;
-  const T* res = g.res ? static_cast<const T*>(g.res) + base : nullptr;
-  if (n == 8 && (g.hw == 0 || p + 8 <= g.hw)) {
-    if (res) {
-      float q[8];
-      load8(res + p, q);
+  T *y = static_cast<T*>(g.y), *z = static_cast<T*>(g.z);
+  const T* res = static_cast<const T*>(g.res);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += q[i];
+  for (int h = 0; h < 8; h += 4) {   // halves: planes of four positions and their multiples have them whole
+    if (h >= n) break;
+    int64_t at = (int64_t)r * g.ld + c + h;
+    int p = c + h;
+    if (g.hw) {
+      const int b = p / g.hw;
+      at += b * (g.img - g.hw);
+      p -= b * g.hw;
     }
-    if (z) store8(z + p, v);
-    act_values<T>(v, g.act);
-    store8(y + p, v);
-    return;
-  }
-  int64_t o = p;
+    if (h + 4 <= n && (g.hw == 0 || p + 4 <= g.hw)) {
+      if (res) {
+        float q[4];
+        load4(res + at, q);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i < n) {
-      if (res) v[i] += E::to_f(res[o]);
-      if (z) z[o] = E::from_f(v[i]);
-      y[o] = E::from_f(act_value<T>(v[i], g.act));
+        for (int i = 0; i < 4; ++i) v[h + i] += q[i];
+      }
+      if (z) store4(z + at, v + h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[h + i] = act_value<T>(v[h + i], g.act);
+      store4(y + at, v + h);
+      continue;
     }
-    ++o;
-    if (g.hw && ++p == g.hw) {
-      p = 0;
-      o += g.img - g.hw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (h + i < n) {
+        if (res) v[h + i] += E::to_f(res[at]);
+        if (z) z[at] = E::from_f(v[h + i]);
+        y[at] = E::from_f(act_value<T>(v[h + i], g.act));
+      }
+      ++at;
+      if (g.hw && ++p == g.hw) {
+        p = 0;
+        at += g.img - g.hw;
+      }
     }
   }
 }
@@ -256,7 +280,7 @@ struct Stage {
   static constexpr int kChunks = TILE * 8;
   static constexpr int kPerLine = ALONG_K ? 8 : TILE / kVec;
 
-  static __device__ __forceinline__ int key(int line) {
+  static constexpr __host__ __device__ int key(int line) {
     if constexpr (ALONG_K) return COLS ? (line & 3) | ((line >> 1) & 4) : line & 7;
     if constexpr (sizeof(T) == 4)
       return COLS ? ((line >> 2) & 1) | (((line >> 2) & 2) << 2) : ((line >> 2) & 3) << 2;
@@ -325,83 +349,131 @@ __device__ __forceinline__ bool tile_of(const GemmArgs& g, int& r, int& c) {
   return true;
 }
 
-// Scales, shifts and stores a wave's fragments: rows r0.., columns c0...
-// They pass through BYTES of LDS at l, the wave's own, so that a row is
-// written (and its residual read) as one run of memory, 32 FC bytes of
-// bfloat16; chunk c of a row lies at c ^ (row & 7).  Where every eight columns
-// are there or not (whole), kBatch rows' residuals are in flight together.
+// The epilogue of a wave's FR x FC fragments: rows r0.., columns c0...  The
+// results pass through BYTES of LDS, the wave's own, so that a row is written
+// (and its residual read) as one run of memory, 32 FC bytes of bfloat16; chunk
+// c of a row lies at c ^ (row & 7).  A lane takes eight columns c of one row
+// in kDown; those that are not all there, or pass from one image to the next,
+// go through finish8.
 template <typename T, int BYTES, int FR, int FC>
-__device__ __forceinline__ void finish(const GemmArgs& g, int r0, int c0, int lane, f32x4 (&acc)[FR][FC],
-                                       unsigned char* l) {
-  constexpr int kPitch = FC * 64, kAcross = 2 * FC, kDown = kWave / kAcross;
-  constexpr int kFrags = BYTES / (16 * kPitch) < FR ? BYTES / (16 * kPitch) : FR;   // fragments of rows at a time
-  constexpr int kIters = kFrags * 16 / kDown, kBatch = kIters < 4 ? kIters : 4;
+struct Finish {
+  static constexpr int kPitch = FC * 64, kAcross = 2 * FC, kDown = kWave / kAcross, kAll = FR * 16 / kDown;
+  static constexpr int kFrags = BYTES / (16 * kPitch) < FR ? BYTES / (16 * kPitch) : FR;   // of rows at a time
+  static constexpr int kIters = kFrags * 16 / kDown, kBatch = kIters < 4 ? kIters : 4;
   static_assert(FR % kFrags == 0 && kIters % kBatch == 0, "whole parts");
-  const int x = lane % kAcross, dr = lane / kAcross, c = c0 + 8 * x;
-  float sc[8], sh[8];
-  column_affine(g, c, sc, sh);
-  const bool whole = g.N % 8 == 0 && g.hw % 8 == 0;
-  int64_t at = c;   // of the lane's columns within a row
-  if (whole && g.hw) at = (c / g.hw) * g.img + c % g.hw;
+  // Small tiles read their residual before the products: its way from memory
+  // is as long as theirs (64 to 256 channels at 56 x 56: 94 to 75 us).
+  static constexpr bool kAhead = FR * FC * sizeof(T) <= 32;
+  typedef T T8 __attribute__((ext_vector_type(8)));
+
+  const GemmArgs& g;
+  int x, down, r0, c;
+  bool fit;        // the lane's eight columns lie side by side
+  int64_t at;      // of the first within a row
+  T8 ahead[kAhead ? kAll : 1];
+
+  __device__ __forceinline__ Finish(const GemmArgs& g, int r0, int c0, int lane)
+      : g(g), x(lane % kAcross), down(lane / kAcross), r0(r0), c(c0 + 8 * x) {
+    at = c;
+    fit = c + 8 <= g.N;
+    if (g.hw) {
+      const int b = c / g.hw, p = c - b * g.hw;
+      at += b * (g.img - g.hw);
+      fit = fit && p + 8 <= g.hw;
+    }
+    if constexpr (kAhead) {
+      if (g.res && !g.part && fit) {
 #pragma unroll
-  for (int f = 0; f < FR; f += kFrags) {
-#pragma unroll
-    for (int i = 0; i < kFrags; ++i)
-#pragma unroll
-      for (int j = 0; j < FC; ++j) {
-        const int row = 16 * i + (lane & 15), ch = 8 * (j / 2) + 2 * (lane >> 4) + (j & 1);
-        *reinterpret_cast<f32x4*>(l + row * kPitch + ((ch ^ (row & 7)) << 4)) = acc[f + i][j];
-      }
-    auto value = [&](int row, float (&v)[8]) __attribute__((always_inline)) {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(l + row * kPitch + (((2 * x) ^ (row & 7)) << 4));
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(l + row * kPitch + (((2 * x + 1) ^ (row & 7)) << 4));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = lo[e];
-        v[4 + e] = hi[e];
-      }
-    };
-    const int rf = r0 + 16 * f;
-    if (whole && !g.part) {
-      const T* res = static_cast<const T*>(g.res);
-      T *y = static_cast<T*>(g.y), *z = static_cast<T*>(g.z);
-      for (int it = 0; it < kIters; it += kBatch) {
-        float q[kBatch][8];
-        float rsc[kBatch], rsh[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int r = min(rf + (it + u) * kDown + dr, g.R - 1);
-          rsc[u] = g.per_row && g.scale ? g.scale[r] : 1.f;
-          rsh[u] = g.per_row && g.shift ? g.shift[r] : 0.f;
-          if (res) load8(res + r * g.ld + (c < g.N ? at : 0), q[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int row = (it + u) * kDown + dr, r = rf + row;
-          float v[8];
-          value(row, v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], g.per_row ? rsc[u] : sc[e], g.per_row ? rsh[u] : sh[e]);
-          if (res)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += q[u][e];
-          const bool there = r < g.R && c < g.N;
-          if (z && there) store8(z + r * g.ld + at, v);
-          act_values<T>(v, g.act);
-          if (there) store8(y + r * g.ld + at, v);
-        }
-      }
-    } else {
-      for (int it = 0; it < kIters; ++it) {
-        const int row = it * kDown + dr;
-        float v[8];
-        value(row, v);
-        row_affine(g, rf + row, sc, sh);
-        finish8<T>(g, rf + row, c, blockIdx.y, v, sc, sh);
+        for (int i = 0; i < kAll; ++i) ahead[i] = residual(i);
       }
     }
   }
-}
+  __device__ __forceinline__ int row(int i) const { return r0 + i * kDown + down; }
+  // the residual of iteration i (only where fit)
+  __device__ __forceinline__ T8 residual(int i) const {
+    T8 v;
+    __builtin_memcpy(&v, static_cast<const T*>(g.res) + min(row(i), g.R - 1) * g.ld + at, sizeof(T8));
+    return v;
+  }
+  __device__ __forceinline__ void value(const unsigned char* l, int i, float (&v)[8]) const {
+    const int r = i * kDown + down;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(l + r * kPitch + (((2 * x) ^ (r & 7)) << 4));
+    const f32x4 hi = *reinterpret_cast<const f32x4*>(l + r * kPitch + (((2 * x + 1) ^ (r & 7)) << 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = lo[e];
+      v[4 + e] = hi[e];
+    }
+  }
+  __device__ __forceinline__ void run(f32x4 (&acc)[FR][FC], unsigned char* l, int lane) {
+    float sc[8], sh[8];
+    column_affine(g, c, sc, sh);
+    T *y = static_cast<T*>(g.y), *z = static_cast<T*>(g.z);
+    // rows of whole 16 bytes go past the caches (ViT projection 84 to 76 us);
+    // rows at 8 bytes do not: their pieces meet in L2 (stage 3: 28 us, not 34)
+    const bool stream = g.ld % 8 == 0 && g.hw % 8 == 0;
+#pragma unroll
+    for (int f = 0; f < FR; f += kFrags) {
+      constexpr int kPer = 16 / kDown;   // iterations of a fragment
+#pragma unroll
+      for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+          const int r = 16 * i + (lane & 15), ch = 8 * (j / 2) + 2 * (lane >> 4) + (j & 1);
+          *reinterpret_cast<f32x4*>(l + r * kPitch + ((ch ^ (r & 7)) << 4)) = acc[f + i][j];
+        }
+      if (!g.part && fit) {
+        auto batch = [&](int it) __attribute__((always_inline)) {
+          T8 q[kBatch];
+          float rsc[kBatch], rsh[kBatch];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const int i = f * kPer + it + u, r = min(row(i), g.R - 1);
+            rsc[u] = g.per_row && g.scale ? g.scale[r] : 1.f;
+            rsh[u] = g.per_row && g.shift ? g.shift[r] : 0.f;
+            if (g.res) {
+              if constexpr (kAhead)
+                q[u] = ahead[i];
+              else
+                q[u] = residual(i);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const int r = row(f * kPer + it + u);
+            float v[8];
+            value(l, it + u, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], g.per_row ? rsc[u] : sc[e], g.per_row ? rsh[u] : sh[e]);
+            if (g.res)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += Elem<T>::to_f(q[u][e]);
+            if (r < g.R) {
+              T *yr = y + r * g.ld + at, *zr = z + r * g.ld + at;
+              if (z) stream ? stream8(zr, v) : store8(zr, v);
+              act_values<T>(v, g.act);
+              stream ? stream8(yr, v) : store8(yr, v);
+            }
+          }
+        };
+        if constexpr (kAhead) {   // the residual's registers by constant places
+#pragma unroll
+          for (int it = 0; it < kIters; it += kBatch) batch(it);
+        } else {
+          for (int it = 0; it < kIters; it += kBatch) batch(it);
+        }
+      }
+      if (g.part || !fit) {
+        for (int it = 0; it < kIters; ++it) {
+          float v[8];
+          value(l, it, v);
+          row_affine(g, row(f * kPer + it), sc, sh);
+          finish8<T>(g, row(f * kPer + it), c, blockIdx.y, v, sc, sh);
+        }
+      }
+    }
+  }
+};
 
 template <int FR, int FC>
 __device__ __forceinline__ void clear(f32x4 (&acc)[FR][FC]) {
@@ -515,17 +587,22 @@ struct Copier {
   }
 };
 
-// WR x WC waves of FR x FC fragments.
-template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC>
+// The barrier behind which stages are published: it waits for this wave's own
+// LDS accesses and then for every wave, but not for its copies in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// WR x WC waves of FR x FC fragments, D stages in LDS.
+template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC, int D>
 __global__ void __launch_bounds__(64 * WR * WC, 2)
-k_project_copy(GemmArgs g) {
+k_project(GemmArgs g) {
   constexpr int NT = 64 * WR * WC, TR = 16 * WR * FR, TC = 16 * WC * FC;
   using SA = Stage<T, AK, TR, false>;
   using SB = Stage<T, BK, TC, true>;
-  constexpr int kDepth = SA::kDepth;
-  // four arrays, so that the compiler sees the copies and the reads apart and
-  // waits for a copy only where its array is read
-  __shared__ __attribute__((aligned(16))) unsigned char a0[SA::kBytes], b0[SB::kBytes], a1[SA::kBytes], b1[SB::kBytes];
+  constexpr int kDepth = SA::kDepth, kA = SA::kBytes, kB = SB::kBytes;
+  // arrays of their own, so that the compiler sees the copies and the reads
+  // apart and waits for a copy only where its array is read
+  __shared__ __attribute__((aligned(16))) unsigned char a0[kA], b0[kB], a1[D > 1 ? kA : 16], b1[D > 1 ? kB : 16],
+      a2[D > 2 ? kA : 16], b2[D > 2 ? kB : 16];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % WR * 16 * FR, wc = wave / WR * 16 * FC;
@@ -535,8 +612,13 @@ k_project_copy(GemmArgs g) {
   const int k0 = blockIdx.y * g.klen, length = min(g.K, k0 + g.klen) - k0;
   const int n = (length + kDepth - 1) / kDepth;
 
+  // a wave's part of LDS for its results
+  constexpr int kArrays = D == 1 ? 2 : 4, kEach = WR * WC / kArrays, kPart = (kA < kB ? kA : kB) / kEach;
+  Finish<T, kPart, FR, FC> fin(g, r0 + wr, c0 + wc, lane);
+
   Copier<T, AK, AK && IMG, TR, false, NT> ca;
   Copier<T, BK, BK && IMG, TC, true, NT> cb;
+  constexpr int kRounds = ca.kRounds + cb.kRounds;
   ca.init(g.a, r0, g.R, k0, tid);
   cb.init(g.b, c0, g.N, k0, tid);
   f32x4 acc[FR][FC];
@@ -562,13 +644,13 @@ k_project_copy(GemmArgs g) {
         c = multiply<T>(fb[phase >> 1][j], fa[phase & 1][i], c);
       }
   };
-  auto publish = [&]() __attribute__((always_inline)) {   // this wave's reads and copies are done, then everyone's
-    __builtin_amdgcn_s_waitcnt(kLgkmWait0);
-    __builtin_amdgcn_s_waitcnt(vm_wait(0));
-    __syncthreads();
+  // Copies the next stage to (la, lb); `left` elements of k are there from it on.
+  auto copy = [&](auto cut, int left, unsigned char* la, unsigned char* lb) __attribute__((always_inline)) {
+    ca.template copy<decltype(cut)::value>(la, tid, wave, left);
+    cb.template copy<decltype(cut)::value>(lb, tid, wave, left);
   };
   // Stage s lies in (la, lb), its first phase's operands in registers; copies
-  // stage s + 2 (cut: `left` of it) and leaves the next one's first operands.
+  // stage s + D over it and leaves the first operands of the next, in (na, nb).
   auto stage = [&](auto cut, int left, unsigned char* la, unsigned char* lb, unsigned char* na,
                    unsigned char* nb) __attribute__((always_inline)) {
     asm volatile("" : "+v"(pa), "+v"(pb));   // the places of the fragments are formed here, not kept
@@ -581,61 +663,177 @@ k_project_copy(GemmArgs g) {
     read(3, la, lb);
     products(2);
     __builtin_amdgcn_sched_barrier(0);
-    publish();
-    ca.template copy<decltype(cut)::value>(la, tid, wave, left);
-    cb.template copy<decltype(cut)::value>(lb, tid, wave, left);
-    read(0, na, nb);
+    if constexpr (D > 1) {
+      __builtin_amdgcn_s_waitcnt(vm_wait((D - 2) * kRounds));   // the next stage is here
+      lds_barrier();
+      copy(cut, left, la, lb);
+      read(0, na, nb);
+    }
     products(3);
     __builtin_amdgcn_sched_barrier(0);
   };
   const std::integral_constant<bool, true> some{};
   const std::integral_constant<bool, false> all{};
-  ca.template copy<true>(a0, tid, wave, length);
-  cb.template copy<true>(b0, tid, wave, length);
-  publish();
-  ca.template copy<true>(a1, tid, wave, length - kDepth);
-  cb.template copy<true>(b1, tid, wave, length - kDepth);
+  copy(some, length, a0, b0);
+  if constexpr (D > 1) copy(some, length - kDepth, a1, b1);
+  if constexpr (D > 2) copy(some, length - 2 * kDepth, a2, b2);
+  __builtin_amdgcn_s_waitcnt(vm_wait((D - 1) * kRounds));
+  lds_barrier();
   read(0, a0, b0);
-  int left = length - 2 * kDepth;   // of the stage to copy next
-  int s = 0;
-  for (; left >= 2 * kDepth; s += 2, left -= 2 * kDepth) {
-    stage(all, 0, a0, b0, a1, b1);
-    stage(all, 0, a1, b1, a0, b0);
+  int left = length - D * kDepth;   // of the stage to copy next
+  if constexpr (D == 1) {
+    stage(some, 0, a0, b0, a0, b0);
+  } else if constexpr (D == 2) {
+    int s = 0;
+    for (; left >= D * kDepth; s += D, left -= D * kDepth) {
+      stage(all, 0, a0, b0, a1, b1);
+      stage(all, 0, a1, b1, a0, b0);
+    }
+    for (; s + 1 < n; s += D, left -= D * kDepth) {
+      stage(some, left, a0, b0, a1, b1);
+      stage(some, left - kDepth, a1, b1, a0, b0);
+    }
+    if (s < n) stage(some, left, a0, b0, a1, b1);
+  } else {
+    int s = 0;
+    for (; left >= D * kDepth; s += D, left -= D * kDepth) {
+      stage(all, 0, a0, b0, a1, b1);
+      stage(all, 0, a1, b1, a2, b2);
+      stage(all, 0, a2, b2, a0, b0);
+    }
+    for (; s + 2 < n; s += D, left -= D * kDepth) {
+      stage(some, left, a0, b0, a1, b1);
+      stage(some, left - kDepth, a1, b1, a2, b2);
+      stage(some, left - 2 * kDepth, a2, b2, a0, b0);
+    }
+    if (s < n) stage(some, left, a0, b0, a1, b1);
+    if (s + 1 < n) stage(some, left - kDepth, a1, b1, a2, b2);
   }
-  for (; s + 1 < n; s += 2, left -= 2 * kDepth) {
-    stage(some, left, a0, b0, a1, b1);
-    stage(some, left - kDepth, a1, b1, a0, b0);
-  }
-  if (s < n) stage(some, left, a0, b0, a1, b1);
-  publish();
-  // a wave's part of LDS for its results
-  constexpr int kEach = WR * WC / 4, kPart = (SA::kBytes < SB::kBytes ? SA::kBytes : SB::kBytes) / kEach;
+  // the stages' LDS is taken for the results: no wave reads, nothing is copied any more
+  __builtin_amdgcn_s_waitcnt(vm_wait(0));
+  __syncthreads();
   const int w = wave / kEach;
-  finish<T, kPart>(g, r0 + wr, c0 + wc, lane, acc, (w == 0 ? a0 : w == 1 ? b0 : w == 2 ? a1 : b1) + wave % kEach * kPart);
+  fin.run(acc, (w == 0 ? a0 : w == 1 ? b0 : w == 2 ? a1 : b1) + wave % kEach * kPart, lane);
 }
 
-// Sums the splits' partial products, in order, and finishes them.
+// ---- few positions ---------------------------------------------------------------
+//
+// A handful of positions (tokens being generated) against the whole weight:
+// bound by reading the weight.  A workgroup takes 16 outputs, its waves their
+// shares of the channels, each straight from memory into the matrix
+// instructions' operands, as many loads in flight as its share holds up to
+// kFewAhead; the waves' sums meet in LDS.  Any alignment, lines of any length.
+constexpr int kFewWaves = 8, kFewAhead = 8;
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
-k_project_join(GemmArgs g, int splits) {
-  const int per = (g.N + 7) / 8;
-  const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int r = (int)(u / per), c = (int)(u % per) * 8;
-  if (r >= g.R) return;
-  float v[8] = {};
-  for (int s = 0; s < splits; ++s) {
-    const float* p = g.part + ((int64_t)s * g.R + r) * g.N + c;
-    if (c + 8 <= g.N) {
-      float q[8];
-      load8(p, q);
+__device__ __forceinline__ u32x4 load_row(const T* row, int k, int n) {
+  constexpr int VE = Elem<T>::kVec;
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (k + VE <= n) {
+    __builtin_memcpy(&v, row + k, 16);
+    return v;
+  }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += q[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < g.N) v[i] += p[i];
+  for (int e = 0; e < VE; ++e) {
+    if (k + e < n) {
+      if constexpr (sizeof(T) == 2)
+        v[e / 2] |= (uint32_t)row[k + e] << (16 * (e & 1));
+      else
+        v[e] = __float_as_uint(row[k + e]);
     }
   }
+  return v;
+}
+
+// x [P][K], weight [O][K], P <= 16 NB
+template <typename T, int NB>
+__global__ void __launch_bounds__(kFewWaves * kWave)
+k_project_few(GemmArgs g) {
+  constexpr int VE = Elem<T>::kVec, kStep = 4 * VE;   // channels of one load by the four lane groups
+  __shared__ f32x4 sums[kFewWaves][NB][kWave];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int o0 = blockIdx.x * 16, m = lane & 15, q = lane >> 4;
+  const T* w = static_cast<const T*>(g.b.p) + (int64_t)min(o0 + m, g.N - 1) * g.b.ld;
+  const T* x[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) x[b] = static_cast<const T*>(g.a.p) + (int64_t)min(16 * b + m, g.R - 1) * g.a.ld;
+  const int steps = (g.K + kStep - 1) / kStep, each = (steps + kFewWaves - 1) / kFewWaves;
+  const int s0 = wave * each, s1 = min(steps, s0 + each);
+  f32x4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = s0; s < s1; s += kFewAhead) {
+    u32x4 wv[kFewAhead], xv[kFewAhead][NB];
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i) {
+      const int k = s + i < s1 ? (s + i) * kStep + q * VE : g.K;   // past the share: zeros
+      wv[i] = load_row(w, k, g.K);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) xv[i][b] = load_row(x[b], k, g.K);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = multiply<T>(wv[i], xv[i][b], acc[b]);
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
+  __syncthreads();
+  // a thread finishes four outputs of a position
+  for (int u = threadIdx.x; u < NB * kWave; u += kFewWaves * kWave) {
+    const int b = u / kWave, l = u % kWave, r = 16 * b + (l & 15), o = o0 + 4 * (l >> 4);
+    f32x4 v = sums[0][b][l];
+    for (int i = 1; i < kFewWaves; ++i) v += sums[i][b][l];
+    if (r >= g.R) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (o + e >= g.N) break;
+      const int64_t at = (int64_t)r * g.ld + o + e;
+      float f = fmaf(v[e], g.scale ? g.scale[o + e] : 1.f, g.shift ? g.shift[o + e] : 0.f);
+      if (g.res) f += Elem<T>::to_f(static_cast<const T*>(g.res)[at]);
+      if (g.z) static_cast<T*>(g.z)[at] = Elem<T>::from_f(f);
+      static_cast<T*>(g.y)[at] = Elem<T>::from_f(act_value<T>(f, g.act));
+    }
+  }
+}
+
+// Sums the splits' partial products, in a fixed order, and finishes them:
+// eight columns a thread, `down` threads (a power of two) taking every
+// down-th split.
+constexpr int kJoinMany = 16;   // splits from which on eight threads share them
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_project_join(GemmArgs g, int splits, int down) {
+  __shared__ float part[kThreads][8 + 1];
+  const int across = kThreads / down, per = (g.N + 7) / 8;
+  const int64_t u = (int64_t)blockIdx.x * across + threadIdx.x % across;
+  const int r = (int)(u / per), c = (int)(u % per) * 8;
+  float v[8] = {};
+  if (r < g.R) {
+    for (int s = threadIdx.x / across; s < splits; s += down) {
+      const float* p = g.part + ((int64_t)s * g.R + r) * g.N + c;
+      if (c + 8 <= g.N) {
+        float q[8];
+        load8(p, q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += q[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c + i < g.N) v[i] += p[i];
+      }
+    }
+  }
+  if (down > 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x][i] = v[i];
+    __syncthreads();
+    if (threadIdx.x >= across) return;
+    for (int d = 1; d < down; ++d)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += part[d * across + threadIdx.x][i];
+  }
+  if (r >= g.R) return;
   GemmArgs h = g;
   h.part = nullptr;
   float sc[8], sh[8];
@@ -646,32 +844,42 @@ k_project_join(GemmArgs g, int splits) {
 
 // ---- the gradients' other passes -------------------------------------------------
 
-__device__ __forceinline__ float block_sum(float v) {
-  __shared__ float s[kThreads / kWave];
-  v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (s[0] + s[1]) + (s[2] + s[3]);
-}
-
-// Row o of the weight's gradient from the splits' G: dweight = scale G, dscale = <weight, G>.
+// Row o of the weight's gradient from the splits' G: dweight = scale G, dscale
+// = <weight, G>.  `across` threads (a power of two) take the columns, the
+// others of a workgroup their share of the splits.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_project_dweight(const float* __restrict__ part, int splits, int O, int C, const float* __restrict__ scale,
-                  const T* __restrict__ weight, T* __restrict__ dweight, float* __restrict__ dscale) {
-  const int o = blockIdx.x;
+                  const T* __restrict__ weight, T* __restrict__ dweight, float* __restrict__ dscale, int across) {
+  __shared__ float s[kThreads], sums[kThreads / kWave];
+  const int o = blockIdx.x, x = threadIdx.x % across, down = kThreads / across;
   const float sc = scale ? scale[o] : 1.f;
   float dot = 0.f;
-  for (int c = threadIdx.x; c < C; c += kThreads) {
+  for (int c0 = 0; c0 < C; c0 += across) {
+    const int c = c0 + x;
     float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += part[((int64_t)s * O + o) * C + c];
-    const int64_t e = (int64_t)o * C + c;
-    if (dweight) dweight[e] = Elem<T>::from_f(sc * v);
-    if (dscale) dot = fmaf(v, Elem<T>::to_f(weight[e]), dot);
+    if (c < C) {
+#pragma unroll 8
+      for (int i = threadIdx.x / across; i < splits; i += down) v += part[((int64_t)i * O + o) * C + c];
+    }
+    if (down > 1) {
+      __syncthreads();
+      s[threadIdx.x] = v;
+      __syncthreads();
+      if (threadIdx.x < across)
+        for (int d = 1; d < down; ++d) v += s[d * across + x];
+    }
+    if (threadIdx.x < across && c < C) {
+      const int64_t e = (int64_t)o * C + c;
+      if (dweight) dweight[e] = Elem<T>::from_f(sc * v);
+      if (dscale) dot = fmaf(v, Elem<T>::to_f(weight[e]), dot);
+    }
   }
   if (!dscale) return;
-  dot = block_sum(dot);
-  if (threadIdx.x == 0) dscale[o] = dot;
+  dot = wave_sum(dot);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = dot;
+  __syncthreads();
+  if (threadIdx.x == 0) dscale[o] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
 // The passes over dy (and z) before the products; packing x or the weight is
@@ -872,59 +1080,95 @@ k_project_weight(const T* __restrict__ weight, const float* __restrict__ scale, 
 
 // ---- launches --------------------------------------------------------------------
 
-constexpr int kWantTiles = 512;          // two workgroups a CU
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a product is cut: tiles of tr rows and tc columns and, where these
-// make too few workgroups for the GPU, the contraction in lengths of 256 or more.
-struct Plan {
-  int tr, tc, splits, klen;
+// The tiles there are: tr x tc, stages in LDS, workgroups a CU, and the
+// microseconds of a bfloat16 stage on a CU that is full (a workgroup's share)
+// and on one of its own.  The times and those of plan() are fitted to 3000
+// measured cuts of 165 products (forward, dx and dW from one position to
+// 360000, 32 to 4096 channels): the cut they pick is 4% slower than the best
+// one measured on average, 28% at worst.
+struct Tile {
+  int tr, tc, stages, per_cu;
+  double busy, alone;
 };
-Plan split_plan(int tr, int tc, int64_t s, int64_t K, int elem) {
-  const int depth = kLine / (elem == MOCE_F32 ? 4 : 2);
-  s = std::min<int64_t>(std::max<int64_t>(s, 1), 256);
-  const int64_t klen = ceil_div(ceil_div(K, s), depth) * depth;
-  return Plan{tr, tc, (int)ceil_div(K, klen), (int)klen};
-}
-Plan sweep_plan(int64_t R, int64_t N, int64_t K, int elem, const char* e) {
-  int tr = 64, tc = 64, s = 0;
-  sscanf(e, "%dx%d/%d", &tr, &tc, &s);
-  if (s == 0) s = (int)std::min(std::max<int64_t>(1, kWantTiles / (ceil_div(R, tr) * ceil_div(N, tc))), std::max<int64_t>(1, K / 256));
-  return split_plan(tr, tc, s, K, elem);
-}
-Plan plan(int64_t R, int64_t N, int64_t K, int elem) {
+enum { kT256, kT128, kT128x64, kT64x128, kT128x64Deep, kT64x128Deep, kT64, kT128x64Once, kT64x128Once, kTiles };
+constexpr Tile kTile[kTiles] = {
+    {256, 256, 2, 1, 1.80, 1.50},  // the most products for an LDS read: 1300 TFLOP/s where it fills the GPU
+    {128, 128, 2, 2, 0.46, 0.72},  // 1130
+    {128, 64, 2, 3, 0.30, 0.64},   // 890; three workgroups a CU hide each other's ends
+    {64, 128, 2, 3, 0.30, 0.64},
+    {128, 64, 3, 2, 0.30, 0.42},   // few tiles, long contractions: 1024 x 2048 over 2048 in 15 us, not 20
+    {64, 128, 3, 2, 0.30, 0.42},
+    {64, 64, 3, 3, 0.23, 0.29},    // few outputs
+    {128, 64, 1, 4, 0.30, 0.55},   // contractions of one stage: 56 x 56 x 64, 64 to 256 channels, 61 us, not 74
+    {64, 128, 1, 4, 0.30, 0.55},
+};
+
+// How a product is cut: its tile and, where the tiles are too few for the GPU,
+// the contraction in `splits` lengths whose sums are joined by another kernel.
+struct Plan {
+  int tile, splits, klen;
+};
+// ragged: the output's rows are not whole chunks; turned: both operands lie
+// across the contraction (twice the LDS reads).
+Plan plan(int64_t R, int64_t N, int64_t K, int elem, bool ragged, bool turned) {
+  constexpr int kCUs = 256;
+  const int depth = kLine / (elem == MOCE_F32 ? 4 : 2), stages = (int)ceil_div(K, depth);
   // sweep
-  int tile = 64;
-  if (ceil_div(R, 128) * ceil_div(N, 128) >= 256) tile = 128;
-  if (elem == MOCE_BF16 && ceil_div(R, 256) * ceil_div(N, 256) >= 256) tile = 256;
-  const int64_t tiles = ceil_div(R, tile) * ceil_div(N, tile);
-  return split_plan(tile, tile, std::min(std::max<int64_t>(1, kWantTiles / tiles), std::max<int64_t>(1, K / 256)), K, elem);
+  // The time of a cut: rounds of workgroups over the CUs, each as long as its
+  // stages and its ends (the way of the first operands and of the results,
+  // 12.6 KB a microsecond and CU); then the join.
+  Plan best{};
+  double least = 1e300;
+  for (int t = 0; t < kTiles; ++t) {
+    const Tile& c = kTile[t];
+    if (c.stages == 1 ? stages != 1 : elem == MOCE_F32 && (t == kT256 || c.stages == 3) && t != kT64) continue;
+    const int64_t tiles = ceil_div(R, c.tr) * ceil_div(N, c.tc), slots = (int64_t)kCUs * c.per_cu;
+    // float32: bound by its matrix instructions
+    const double busy = elem == MOCE_F32 ? 0.36 / 4096 * c.tr * c.tc : turned ? 1.25 * c.busy : c.busy;
+    const double alone = std::max(c.alone, elem == MOCE_F32 ? 1.13 * busy : busy);
+    for (int64_t s = 1; s <= 256; s += s < 8 ? 1 : s / 4) {
+      if (s > 1 && (stages / s < 6 || tiles * (s - 1) >= 2 * slots)) break;
+      const int64_t each = ceil_div(stages, s), splits = ceil_div(stages, each);
+      const int64_t rounds = tiles * splits / slots, k = ceil_div(tiles * splits % slots, kCUs);
+      const int bytes = splits > 1 || elem == MOCE_F32 ? 4 : ragged ? 2 * 2 : 2;
+      const double end = c.tr * c.tc * bytes / 12600., begin = 7. / c.per_cu;
+      double time = rounds * (each * c.per_cu * busy + begin + end * c.per_cu);
+      if (k > 0) time += each * std::max(alone, k * busy) + begin + end * k;
+      if (splits > 1) time += 3 + (double)splits * R * N * 4 / 2e6;
+      if (time < least) {
+        least = time;
+        best = Plan{t, (int)splits, (int)(each * depth)};
+      }
+    }
+  }
+  return best;
 }
 size_t part_bytes(int64_t R, int64_t N, const Plan& p) { return (size_t)p.splits * R * N * sizeof(float); }
 
-template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int F, int FC>
-void launch_copy(GemmArgs g, int splits, hipStream_t st) {
-  g.tr = (int)ceil_div(g.R, 16 * WR * F), g.tc = (int)ceil_div(g.N, 16 * WC * FC);
+template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC, int D>
+void launch_tiles(GemmArgs g, int splits, hipStream_t st) {
+  g.tr = (int)ceil_div(g.R, 16 * WR * FR), g.tc = (int)ceil_div(g.N, 16 * WC * FC);
   const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc, 8) * 8), splits);
-  hipLaunchKernelGGL((k_project_copy<T, AK, BK, IMG, WR, WC, F, FC>), grid, dim3(64 * WR * WC), 0, st, g);
+  hipLaunchKernelGGL((k_project<T, AK, BK, IMG, WR, WC, FR, FC, D>), grid, dim3(64 * WR * WC), 0, st, g);
 }
 
 template <typename T, bool AK, bool BK>
 hipError_t launch_product(const GemmArgs& g, const Plan& p, hipStream_t st) {
   auto copy = [&](auto img) {
     constexpr bool IMG = decltype(img)::value;
-    const int t = p.tr * 1000 + p.tc;
-    if (t == 64064) launch_copy<T, AK, BK, IMG, 2, 2, 2, 2>(g, p.splits, st);
-    else if (t == 128128 || sizeof(T) == 4) launch_copy<T, AK, BK, IMG, 2, 2, 4, 4>(g, p.splits, st);
-    else if constexpr (sizeof(T) == 2) {
-      if (t == 256256) launch_copy<T, AK, BK, IMG, 2, 4, 8, 4>(g, p.splits, st);
-      if (t == 128064) launch_copy<T, AK, BK, IMG, 2, 2, 4, 2>(g, p.splits, st);
-      if (t == 64128) launch_copy<T, AK, BK, IMG, 2, 2, 2, 4>(g, p.splits, st);
-      if (t == 256128) launch_copy<T, AK, BK, IMG, 4, 2, 4, 4>(g, p.splits, st);
-      if (t == 128256) launch_copy<T, AK, BK, IMG, 2, 4, 4, 4>(g, p.splits, st);
-      if (t == 256064) launch_copy<T, AK, BK, IMG, 4, 1, 4, 4>(g, p.splits, st);
-      if (t == 64256) launch_copy<T, AK, BK, IMG, 1, 4, 4, 4>(g, p.splits, st);
+    constexpr bool low = sizeof(T) == 2;
+    switch (p.tile) {
+      case kT256: if constexpr (low) launch_tiles<T, AK, BK, IMG, 2, 4, 8, 4, 2>(g, p.splits, st); break;
+      case kT128: launch_tiles<T, AK, BK, IMG, 2, 2, 4, 4, 2>(g, p.splits, st); break;
+      case kT128x64: launch_tiles<T, AK, BK, IMG, 2, 2, 4, 2, 2>(g, p.splits, st); break;
+      case kT64x128: launch_tiles<T, AK, BK, IMG, 2, 2, 2, 4, 2>(g, p.splits, st); break;
+      case kT128x64Deep: if constexpr (low) launch_tiles<T, AK, BK, IMG, 2, 2, 4, 2, 3>(g, p.splits, st); break;
+      case kT64x128Deep: if constexpr (low) launch_tiles<T, AK, BK, IMG, 2, 2, 2, 4, 3>(g, p.splits, st); break;
+      case kT64: launch_tiles<T, AK, BK, IMG, 2, 2, 2, 2, 3>(g, p.splits, st); break;
+      case kT128x64Once: launch_tiles<T, AK, BK, IMG, 2, 2, 4, 2, 1>(g, p.splits, st); break;
+      case kT64x128Once: launch_tiles<T, AK, BK, IMG, 2, 2, 2, 4, 1>(g, p.splits, st); break;
     }
   };
   if constexpr (AK && BK) {
@@ -940,8 +1184,9 @@ hipError_t launch_product(const GemmArgs& g, const Plan& p, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_join(const GemmArgs& g, int splits, hipStream_t st) {
-  hipLaunchKernelGGL(k_project_join<T>, dim3((unsigned)ceil_div((int64_t)g.R * ceil_div(g.N, 8), kThreads)),
-                     dim3(kThreads), 0, st, g, splits);
+  const int down = splits >= kJoinMany ? 8 : 1;
+  hipLaunchKernelGGL(k_project_join<T>, dim3((unsigned)ceil_div((int64_t)g.R * ceil_div(g.N, 8), kThreads / down)),
+                     dim3(kThreads), 0, st, g, splits, down);
   return hipGetLastError();
 }
 
@@ -1043,6 +1288,12 @@ void output(GemmArgs* g, const Sizes& z, int64_t channels) {
   g->ld = z.nhwc ? channels : z.s.HW, g->hw = z.images(), g->img = channels * z.s.HW;
 }
 
+// Whether a tensor of so many channels has rows that the epilogue writes in pieces.
+bool ragged_rows(const Sizes& z, int64_t channels) { return (z.nhwc ? channels : z.s.HW) % 8 != 0; }
+
+constexpr int kFewRows = 64;
+bool few_rows(const Sizes& z) { return z.nhwc && z.P() <= kFewRows; }
+
 struct FwdLayout {
   Plan p;
   size_t x, weight, part, total;
@@ -1051,9 +1302,10 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 FwdLayout fwd_layout(const ProjectShape& s) {
   const Sizes z(s);
   FwdLayout l{};
+  if (few_rows(z)) return l;
   GemmArgs g{};
   output(&g, z, s.O);
-  l.p = plan(g.R, g.N, s.C, s.elem);
+  l.p = plan(g.R, g.N, s.C, s.elem, ragged_rows(z, s.O), false);
   l.x = 0;
   l.weight = l.x + (z.rows(s.C) ? up256(z.packed(s.C)) : 0);
   l.part = l.weight + (z.weight() ? up256((size_t)s.O * z.up(s.C) * z.el()) : 0);
@@ -1067,6 +1319,20 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
   const Sizes z(s);
   const FwdLayout l = fwd_layout(s);
   const bool turned = !z.nhwc && z.planes();
+  if (few_rows(z)) {
+    GemmArgs g{};
+    output(&g, z, s.O);
+    g.K = (int)s.C, g.a = Operand{x, s.C, 0, 0}, g.b = Operand{w, s.C, 0, 0};
+    g.scale = scale, g.shift = shift, g.res = res, g.y = y, g.z = z_out, g.act = s.act;
+    const dim3 grid((unsigned)ceil_div(s.O, 16)), block(kFewWaves * kWave);
+    if (g.R <= 16)
+      hipLaunchKernelGGL((k_project_few<T, 1>), grid, block, 0, st, g);
+    else if (g.R <= 32)
+      hipLaunchKernelGGL((k_project_few<T, 2>), grid, block, 0, st, g);
+    else
+      hipLaunchKernelGGL((k_project_few<T, 4>), grid, block, 0, st, g);
+    return hipGetLastError();
+  }
   hipError_t e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);
   if (e == hipSuccess) e = pack_weight<T>(z, &w, nullptr, ws + l.weight, st);
   if (e != hipSuccess) return e;
@@ -1135,8 +1401,8 @@ BwdLayout bwd_layout(const ProjectShape& s) {
   BwdLayout l{};
   GemmArgs g{};
   output(&g, z, s.C);
-  l.px = plan(g.R, g.N, s.O, s.elem);
-  l.pw = plan(s.O, s.C, z.P(), s.elem);
+  l.px = plan(g.R, g.N, s.O, s.elem, ragged_rows(z, s.C), false);
+  l.pw = plan(s.O, s.C, z.P(), s.elem, s.C % 8 != 0, z.nhwc || z.planes());
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -1250,8 +1516,10 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
     }
     if (e != hipSuccess) return e;
     if (join) {
+      int across = 32;
+      while (across < kThreads && across < s.C) across *= 2;
       hipLaunchKernelGGL(k_project_dweight<T>, dim3((unsigned)s.O), dim3(kThreads), 0, st, part, l.pw.splits, (int)s.O,
-                         (int)s.C, row_scale, static_cast<const T*>(w), static_cast<T*>(gr.dweight), gr.dscale);
+                         (int)s.C, row_scale, static_cast<const T*>(w), static_cast<T*>(gr.dweight), gr.dscale, across);
       e = hipGetLastError();
     }
   }
