@@ -13,6 +13,8 @@ import ctypes
 import os
 from typing import Optional, Tuple
 
+import numpy as np
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmoce.so")
 
@@ -352,28 +354,30 @@ def moce_project_backward(desc: moce_project_desc, x, weight, scale, z, dy, grad
                                                                  _ptr(ws), ws_bytes, _stream(stream)))
 
 
-def make_gradients(tensors, out=None):
-    """The list of gradients for moce_gradient_norm and moce_gradient_clip: float32 or bfloat16 torch tensors, and
-    where the clipped ones go (None: in place)."""
-    arr = (moce_gradient * max(1, len(tensors)))()
-    for g, t, d in zip(arr, tensors, tensors if out is None else out):
-        g.src, g.dst, g.n = t.data_ptr(), d.data_ptr(), t.numel()
-        g.dtype = MOCE_F32 if t.element_size() == 4 else MOCE_BF16
-    return arr
+def make_gradients(src, dst, sizes, dtypes) -> np.ndarray:
+    """The list of gradients for moce_gradient_norm and moce_gradient_clip (an array of moce_gradient) from lists of
+    addresses, element counts and MOCE_F32 / MOCE_BF16."""
+    grads = np.empty((len(src), 4), np.int64)      # the last word: the type, then the reserved zero
+    grads[:, 0], grads[:, 1], grads[:, 2], grads[:, 3] = src, dst, sizes, dtypes
+    return grads
+
+
+def _list(grads: np.ndarray) -> int:
+    return grads.__array_interface__["data"][0]
 
 
 def moce_gradient_workspace_bytes(grads, count: int) -> int:
-    return load().moce_gradient_workspace_bytes(ctypes.addressof(grads), count)
+    return load().moce_gradient_workspace_bytes(_list(grads), count)
 
 
 def moce_gradient_norm(grads, count: int, norm, ws, ws_bytes: int, stream=None) -> None:
-    _check("moce_gradient_norm", load().moce_gradient_norm(ctypes.addressof(grads), count, _ptr(norm), _ptr(ws),
-                                                           ws_bytes, _stream(stream)))
+    _check("moce_gradient_norm", load().moce_gradient_norm(_list(grads), count, _ptr(norm), _ptr(ws), ws_bytes,
+                                                           _stream(stream)))
 
 
 def moce_gradient_clip(grads, count: int, max_norm: float, norm, ws, ws_bytes: int, stream=None) -> None:
-    _check("moce_gradient_clip", load().moce_gradient_clip(ctypes.addressof(grads), count, max_norm, _ptr(norm),
-                                                           _ptr(ws), ws_bytes, _stream(stream)))
+    _check("moce_gradient_clip", load().moce_gradient_clip(_list(grads), count, max_norm, _ptr(norm), _ptr(ws),
+                                                           ws_bytes, _stream(stream)))
 
 
 def raw_status(fn: str, *args) -> int:

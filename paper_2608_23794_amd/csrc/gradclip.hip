@@ -18,8 +18,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSumThreads = 1024;
 constexpr int kList = 128;                       // tensors a launch: 3.6 KB of arguments
-constexpr int64_t kChunk = 16384;                // elements of a chunk, and
-constexpr int64_t kMaxChunks = 65536;            // more of them where this many would not do
+// Elements of a chunk: enough chunks to fill the GPU (8 a CU), of 8 to 128 KB
+// of float32, and more where kMaxChunks would not do.
+constexpr int64_t kWantChunks = 2048, kMinChunk = 2048, kMaxChunk = 32768, kMaxChunks = 65536;
+// Chunks whose sums every workgroup of the scaling adds up by itself, which
+// saves the launch between (clip_gradients of a layer's four: 16 us, not 20).
+constexpr int kFewChunks = 4096;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -54,38 +58,64 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 
 __device__ __forceinline__ double square(float v) { return (double)v * (double)v; }
 
-// Gradients lie at any multiple of their element, so vector accesses are unaligned ones.
+// The range of chunk q of a list.
+struct Part {
+  int t;
+  bool bf16;
+  int64_t i0, i1;
+};
+__device__ __forceinline__ Part part_of(const List& l, int q, int64_t chunk) {
+  Part p;
+  p.t = tensor_of(l, q);
+  p.bf16 = l.n[p.t] < 0;
+  const int64_t n = p.bf16 ? ~l.n[p.t] : l.n[p.t];
+  p.i0 = (int64_t)(q - l.first[p.t]) * chunk;
+  p.i1 = min(n, p.i0 + chunk);
+  return p;
+}
+
+// Gradients lie at any multiple of their element, so vector accesses are
+// unaligned ones.  kAhead of a thread's are in flight together.
+constexpr int kAhead = 4;
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void each_vector(const T* p, const Part& r, F&& vector, G&& element) {
+  constexpr int VE = 16 / sizeof(T);
+  int64_t i = r.i0 + threadIdx.x * VE;
+  for (; i + (kAhead - 1) * kThreads * VE + VE <= r.i1; i += kAhead * kThreads * VE) {
+    u32x4 v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) __builtin_memcpy(&v[u], p + i + u * kThreads * VE, 16);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) vector(i + u * kThreads * VE, v[u]);
+  }
+  for (; i + VE <= r.i1; i += kThreads * VE) {
+    u32x4 v;
+    __builtin_memcpy(&v, p + i, 16);
+    vector(i, v);
+  }
+  for (int e = 0; e < VE && i + e < r.i1; ++e) element(i + e);
+}
+
 __global__ void __launch_bounds__(kThreads)
 k_gradient_squares(List l, int64_t chunk, double* __restrict__ part) {
   __shared__ double s[kThreads / kWave];
-  const int t = tensor_of(l, blockIdx.x);
-  const bool bf16 = l.n[t] < 0;
-  const int64_t n = bf16 ? ~l.n[t] : l.n[t];
-  const int64_t i0 = (int64_t)(blockIdx.x - l.first[t]) * chunk, i1 = min(n, i0 + chunk);
+  const Part r = part_of(l, blockIdx.x, chunk);
   double a = 0., b = 0.;
-  if (bf16) {
-    const uint16_t* p = static_cast<const uint16_t*>(l.src[t]);
-    int64_t i = i0 + threadIdx.x * 8;
-    for (; i + 8 <= i1; i += kThreads * 8) {
-      u32x4 v;
-      __builtin_memcpy(&v, p + i, 16);
+  if (r.bf16) {
+    const uint16_t* p = static_cast<const uint16_t*>(l.src[r.t]);
+    each_vector(p, r, [&](int64_t, u32x4 v) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         a += square(bf16_lo(v[e]));
         b += square(bf16_hi(v[e]));
       }
-    }
-    for (int e = 0; e < 8 && i + e < i1; ++e) a += square(bf16_to_f32(p[i + e]));
+    }, [&](int64_t i) __attribute__((always_inline)) { a += square(bf16_to_f32(p[i])); });
   } else {
-    const float* p = static_cast<const float*>(l.src[t]);
-    int64_t i = i0 + threadIdx.x * 4;
-    for (; i + 4 <= i1; i += kThreads * 4) {
-      float v[4];
-      __builtin_memcpy(v, p + i, 16);
-      a += square(v[0]) + square(v[1]);
-      b += square(v[2]) + square(v[3]);
-    }
-    for (int e = 0; e < 4 && i + e < i1; ++e) a += square(p[i + e]);
+    const float* p = static_cast<const float*>(l.src[r.t]);
+    each_vector(p, r, [&](int64_t, u32x4 v) __attribute__((always_inline)) {
+      a += square(__uint_as_float(v[0])) + square(__uint_as_float(v[1]));
+      b += square(__uint_as_float(v[2])) + square(__uint_as_float(v[3]));
+    }, [&](int64_t i) __attribute__((always_inline)) { a += square(p[i]); });
   }
   a = wave_sum_f64(a + b);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = a;
@@ -93,65 +123,77 @@ k_gradient_squares(List l, int64_t chunk, double* __restrict__ part) {
   if (threadIdx.x == 0) part[l.base + blockIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// The norm, and the coefficient 1 or max_norm / norm (coef may be nullptr).
-__global__ void __launch_bounds__(kSumThreads)
-k_gradient_norm(const double* __restrict__ part, int chunks, float max_norm, float* __restrict__ norm,
-                float* __restrict__ coef) {
-  __shared__ double s[kSumThreads / kWave];
+// The norm from the chunks' sums, by a workgroup of NT threads (every thread has it).
+template <int NT>
+__device__ __forceinline__ double norm_of_parts(const double* __restrict__ part, int chunks) {
+  __shared__ double s[NT / kWave];
   double a = 0.;
-  for (int i = threadIdx.x; i < chunks; i += kSumThreads) a += part[i];
+#pragma unroll 4
+  for (int i = threadIdx.x; i < chunks; i += NT) a += part[i];
   a = wave_sum_f64(a);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = a;
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int w = 1; w < kSumThreads / kWave; ++w) a += s[w];
-  a = sqrt(a);
-  const float f = (float)a;
-  *norm = f;
-  if (coef) *coef = a > (double)max_norm && __builtin_isfinite(f) ? (float)((double)max_norm / a) : 1.f;
+  a = s[0];
+#pragma unroll
+  for (int w = 1; w < NT / kWave; ++w) a += s[w];
+  return sqrt(a);
+}
+__device__ __forceinline__ float coefficient(double norm, float max_norm) {
+  return norm > (double)max_norm && __builtin_isfinite((float)norm) ? (float)((double)max_norm / norm) : 1.f;
 }
 
+// The norm, and the coefficient 1 or max_norm / norm (coef may be nullptr).
+template <int NT>
+__global__ void __launch_bounds__(NT)
+k_gradient_norm(const double* __restrict__ part, int chunks, float max_norm, float* __restrict__ norm,
+                float* __restrict__ coef) {
+  const double a = norm_of_parts<NT>(part, chunks);
+  if (threadIdx.x != 0) return;
+  *norm = (float)a;
+  if (coef) *coef = coefficient(a, max_norm);
+}
+
+// FEW: the norm from the parts, else the coefficient is there.  The chunks go
+// backwards: those read last for the norm are still in the infinity cache.
+template <bool FEW>
 __global__ void __launch_bounds__(kThreads)
-k_gradient_scale(List l, int64_t chunk, const float* __restrict__ coef) {
-  const float c = *coef;
-  const int t = tensor_of(l, blockIdx.x);
-  if (c == 1.f && l.src[t] == l.dst[t]) return;
-  const bool bf16 = l.n[t] < 0;
-  const int64_t n = bf16 ? ~l.n[t] : l.n[t];
-  const int64_t i0 = (int64_t)(blockIdx.x - l.first[t]) * chunk, i1 = min(n, i0 + chunk);
-  if (bf16) {
-    const uint16_t* p = static_cast<const uint16_t*>(l.src[t]);
-    uint16_t* d = static_cast<uint16_t*>(l.dst[t]);
-    int64_t i = i0 + threadIdx.x * 8;
-    for (; i + 8 <= i1; i += kThreads * 8) {
-      u32x4 v;
-      __builtin_memcpy(&v, p + i, 16);
+k_gradient_scale(List l, int64_t chunk, const double* __restrict__ part, int chunks, float max_norm,
+                 float* __restrict__ norm, const float* __restrict__ coef) {
+  float c;
+  if constexpr (FEW) {
+    const double a = norm_of_parts<kThreads>(part, chunks);
+    if (l.base + (int)blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)a;
+    c = coefficient(a, max_norm);
+  } else {
+    c = *coef;
+  }
+  const Part r = part_of(l, gridDim.x - 1 - blockIdx.x, chunk);
+  if (c == 1.f && l.src[r.t] == l.dst[r.t]) return;
+  if (r.bf16) {
+    const uint16_t* p = static_cast<const uint16_t*>(l.src[r.t]);
+    uint16_t* d = static_cast<uint16_t*>(l.dst[r.t]);
+    each_vector(p, r, [&](int64_t i, u32x4 v) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = pack_bf16x2(bf16_lo(v[e]) * c, bf16_hi(v[e]) * c);
       __builtin_memcpy(d + i, &v, 16);
-    }
-    for (int e = 0; e < 8 && i + e < i1; ++e) d[i + e] = f32_to_bf16(bf16_to_f32(p[i + e]) * c);
+    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = f32_to_bf16(bf16_to_f32(p[i]) * c); });
   } else {
-    const float* p = static_cast<const float*>(l.src[t]);
-    float* d = static_cast<float*>(l.dst[t]);
-    int64_t i = i0 + threadIdx.x * 4;
-    for (; i + 4 <= i1; i += kThreads * 4) {
-      float v[4];
-      __builtin_memcpy(v, p + i, 16);
+    const float* p = static_cast<const float*>(l.src[r.t]);
+    float* d = static_cast<float*>(l.dst[r.t]);
+    each_vector(p, r, [&](int64_t i, u32x4 v) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= c;
-      __builtin_memcpy(d + i, v, 16);
-    }
-    for (int e = 0; e < 4 && i + e < i1; ++e) d[i + e] = p[i + e] * c;
+      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * c);
+      __builtin_memcpy(d + i, &v, 16);
+    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = p[i] * c; });
   }
 }
 
-// Elements of a chunk: a multiple of a workgroup's vector accesses.
 int64_t chunk_size(const moce_gradient* g, int count) {
   int64_t total = 0;
   for (int i = 0; i < count; ++i) total += g[i].n;
-  const int64_t want = (total + kMaxChunks - 1) / kMaxChunks;
-  return std::max(kChunk, (want + 2047) / 2048 * 2048);
+  auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+  const int64_t want = std::clamp(up(total, kWantChunks), kMinChunk, kMaxChunk);
+  return up(std::max(want, up(total, kMaxChunks)), kMinChunk) * kMinChunk;
 }
 int64_t chunk_count(const moce_gradient* g, int count, int64_t chunk) {
   int64_t c = 0;
@@ -186,15 +228,29 @@ hipError_t each_list(const moce_gradient* g, int count, int64_t chunk, F&& f) {
 
 constexpr size_t kPartAt = 256;   // the workspace: the coefficient, then the chunks' sums
 
-hipError_t norm_of(const moce_gradient* g, int count, float max_norm, float* norm, float* coef, double* part,
-                   int64_t chunk, hipStream_t st) {
-  const hipError_t e = each_list(g, count, chunk, [&](const List& l, int32_t chunks) {
-    hipLaunchKernelGGL(k_gradient_squares, dim3(chunks), dim3(kThreads), 0, st, l, chunk, part);
+struct Work {
+  int64_t chunk;
+  int chunks;
+  float* coef;
+  double* part;
+  Work(const moce_gradient* g, int count, void* ws)
+      : chunk(chunk_size(g, count)), chunks((int)chunk_count(g, count, chunk)), coef(static_cast<float*>(ws)),
+        part(reinterpret_cast<double*>(static_cast<char*>(ws) + kPartAt)) {}
+};
+
+hipError_t squares(const moce_gradient* g, int count, const Work& w, hipStream_t st) {
+  return each_list(g, count, w.chunk, [&](const List& l, int32_t chunks) {
+    hipLaunchKernelGGL(k_gradient_squares, dim3(chunks), dim3(kThreads), 0, st, l, w.chunk, w.part);
     return hipGetLastError();
   });
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_gradient_norm, dim3(1), dim3(kSumThreads), 0, st, part, (int)chunk_count(g, count, chunk),
-                     max_norm, norm, coef);
+}
+hipError_t norm_of(const Work& w, float max_norm, float* norm, float* coef, hipStream_t st) {
+  if (w.chunks <= kFewChunks)   // the order of the sum in k_gradient_scale<true>
+    hipLaunchKernelGGL(k_gradient_norm<kThreads>, dim3(1), dim3(kThreads), 0, st, w.part, w.chunks, max_norm, norm,
+                       coef);
+  else
+    hipLaunchKernelGGL(k_gradient_norm<kSumThreads>, dim3(1), dim3(kSumThreads), 0, st, w.part, w.chunks, max_norm,
+                       norm, coef);
   return hipGetLastError();
 }
 
@@ -205,19 +261,25 @@ size_t gradient_ws_bytes(const moce_gradient* g, int count) {
 }
 
 hipError_t launch_gradient_norm(const moce_gradient* g, int count, float* norm, void* ws, hipStream_t st) {
-  return norm_of(g, count, 0.f, norm, nullptr, reinterpret_cast<double*>(static_cast<char*>(ws) + kPartAt),
-                 chunk_size(g, count), st);
+  const Work w(g, count, ws);
+  const hipError_t e = squares(g, count, w, st);
+  return e == hipSuccess ? norm_of(w, 0.f, norm, nullptr, st) : e;
 }
 
 hipError_t launch_gradient_clip(const moce_gradient* g, int count, float max_norm, float* norm, void* ws,
                                 hipStream_t st) {
-  const int64_t chunk = chunk_size(g, count);
-  float* coef = static_cast<float*>(ws);
-  const hipError_t e = norm_of(g, count, max_norm, norm, coef,
-                               reinterpret_cast<double*>(static_cast<char*>(ws) + kPartAt), chunk, st);
+  const Work w(g, count, ws);
+  hipError_t e = squares(g, count, w, st);
   if (e != hipSuccess) return e;
-  return each_list(g, count, chunk, [&](const List& l, int32_t chunks) {
-    hipLaunchKernelGGL(k_gradient_scale, dim3(chunks), dim3(kThreads), 0, st, l, chunk, coef);
+  const bool few = w.chunks > 0 && w.chunks <= kFewChunks;
+  if (!few && (e = norm_of(w, max_norm, norm, w.coef, st)) != hipSuccess) return e;
+  return each_list(g, count, w.chunk, [&](const List& l, int32_t chunks) {
+    if (few)
+      hipLaunchKernelGGL(k_gradient_scale<true>, dim3(chunks), dim3(kThreads), 0, st, l, w.chunk, w.part, w.chunks,
+                         max_norm, norm, w.coef);
+    else
+      hipLaunchKernelGGL(k_gradient_scale<false>, dim3(chunks), dim3(kThreads), 0, st, l, w.chunk, w.part, w.chunks,
+                         max_norm, norm, w.coef);
     return hipGetLastError();
   });
 }

@@ -757,7 +757,8 @@ k_project_few(GemmArgs g) {
   const T* x[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) x[b] = static_cast<const T*>(g.a.p) + (int64_t)min(16 * b + m, g.R - 1) * g.a.ld;
-  const int steps = (g.K + kStep - 1) / kStep, each = (steps + kFewWaves - 1) / kFewWaves;
+  // whole steps are shared out; what is left behind them is the last wave's
+  const int steps = g.K / kStep, each = (steps + kFewWaves - 1) / kFewWaves;
   const int s0 = wave * each, s1 = min(steps, s0 + each);
   f32x4 acc[NB];
 #pragma unroll
@@ -766,15 +767,22 @@ k_project_few(GemmArgs g) {
     u32x4 wv[kFewAhead], xv[kFewAhead][NB];
 #pragma unroll
     for (int i = 0; i < kFewAhead; ++i) {
-      const int k = s + i < s1 ? (s + i) * kStep + q * VE : g.K;   // past the share: zeros
-      wv[i] = load_row(w, k, g.K);
+      const int k = min(s + i, s1 - 1) * kStep + q * VE;   // past the share its last step again, not multiplied
+      __builtin_memcpy(&wv[i], w + k, 16);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) xv[i][b] = load_row(x[b], k, g.K);
+      for (int b = 0; b < NB; ++b) __builtin_memcpy(&xv[i][b], x[b] + k, 16);
     }
 #pragma unroll
     for (int i = 0; i < kFewAhead; ++i)
+      if (s + i < s1)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b] = multiply<T>(wv[i], xv[i][b], acc[b]);
+        for (int b = 0; b < NB; ++b) acc[b] = multiply<T>(wv[i], xv[i][b], acc[b]);
+  }
+  if (wave == kFewWaves - 1 && steps * kStep < g.K) {
+    const int k = steps * kStep + q * VE;
+    const u32x4 wv = load_row(w, k, g.K);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = multiply<T>(wv, load_row(x[b], k, g.K), acc[b]);
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
@@ -1291,7 +1299,7 @@ void output(GemmArgs* g, const Sizes& z, int64_t channels) {
 // Whether a tensor of so many channels has rows that the epilogue writes in pieces.
 bool ragged_rows(const Sizes& z, int64_t channels) { return (z.nhwc ? channels : z.s.HW) % 8 != 0; }
 
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 32;   // beyond, 64 x 64 tiles in splits are as fast (64 positions of 4096 x 4096: 17 us, not 25)
 bool few_rows(const Sizes& z) { return z.nhwc && z.P() <= kFewRows; }
 
 struct FwdLayout {
@@ -1327,10 +1335,8 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
     const dim3 grid((unsigned)ceil_div(s.O, 16)), block(kFewWaves * kWave);
     if (g.R <= 16)
       hipLaunchKernelGGL((k_project_few<T, 1>), grid, block, 0, st, g);
-    else if (g.R <= 32)
-      hipLaunchKernelGGL((k_project_few<T, 2>), grid, block, 0, st, g);
     else
-      hipLaunchKernelGGL((k_project_few<T, 4>), grid, block, 0, st, g);
+      hipLaunchKernelGGL((k_project_few<T, 2>), grid, block, 0, st, g);
     return hipGetLastError();
   }
   hipError_t e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import contextlib
 import math
+import operator
 from typing import Optional
 
 import numpy as np
@@ -282,6 +283,10 @@ def _on(device):
     return torch.cuda.device(device) if torch.cuda.current_device() != device.index else contextlib.nullcontext()
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _need(name: str, t: torch.Tensor, shape, dtype, device):
     """Raises unless t is a contiguous tensor of this shape, type and device: the library sees only its address."""
     if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
@@ -356,7 +361,7 @@ class ProjectLayer:
         with _on(self.device):
             ws, n = self._workspace(mb.moce_project_workspace_bytes(desc), ws)
             mb.moce_project(desc, x, self.weight, self.scale, self.shift, residual, y, z, ws, n,
-                            torch.cuda.current_stream(self.device))
+                            _raw_stream(self.device.index))
         return y
 
     def backward(self, x: torch.Tensor, dy: torch.Tensor, z: Optional[torch.Tensor] = None, residual: bool = False,
@@ -388,37 +393,44 @@ class ProjectLayer:
         with _on(dev):
             ws, n = self._workspace(mb.moce_project_backward_workspace_bytes(desc), ws)
             mb.moce_project_backward(desc, x, self.weight, self.scale, z, dy, mb.make_project_grads(**out), ws, n,
-                                     torch.cuda.current_stream(dev))
+                                     _raw_stream(dev.index))
         return out
 
 
-def _gradient_list(tensors, out):
+_dtype = operator.attrgetter("dtype")
+
+
+def _columns(name: str, tensors):
+    """Addresses, sizes and types of the tensors, a list each (hundreds of them: one pass a property is the fastest)."""
+    codes = list(map(_DTYPE_OF.get, map(_dtype, tensors)))
+    device = tensors[0].get_device()
+    if (device < 0 or None in codes or set(map(torch.Tensor.get_device, tensors)) != {device}
+            or not all(map(torch.Tensor.is_contiguous, tensors))):
+        raise ValueError(f"every {name} has to be a contiguous float32 or bfloat16 tensor on one GPU, got " +
+                         ", ".join(f"{t.dtype} {tuple(t.shape)} on {t.device}" for t in tensors)[:300])
+    return list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors)), codes, device
+
+
+def _gradient_call(tensors, out, ws, call):
     tensors = list(tensors)
     if not tensors:
         raise ValueError("no gradients")
-    device = tensors[0].device
+    src, sizes, codes, index = _columns("gradient", tensors)
+    dst = src
     if out is not None:
         out = list(out)
         if len(out) != len(tensors):
             raise ValueError(f"{len(tensors)} gradients, {len(out)} outputs")
-    for name, ts in (("gradient", tensors), ("output", out or ())):
-        for t, like in zip(ts, tensors):
-            if t.dtype not in _DTYPE_OF or not t.is_cuda or t.device != device or not t.is_contiguous():
-                raise ValueError(f"every {name} has to be a contiguous float32 or bfloat16 tensor on {device}, got "
-                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
-            if t.dtype != like.dtype or t.numel() != like.numel():
-                raise ValueError(f"an output is {t.dtype} {tuple(t.shape)}, its gradient {like.dtype} "
-                                 f"{tuple(like.shape)}")
-    return mb.make_gradients(tensors, out), len(tensors), device
-
-
-def _gradient_call(tensors, out, ws, call):
-    arr, n, device = _gradient_list(tensors, out)
+        dst, *rest = _columns("output", out)
+        if rest != [sizes, codes, index]:
+            raise ValueError("an output differs from its gradient in type, size or device")
+    device, n = tensors[0].device, len(tensors)
+    grads = mb.make_gradients(src, dst, sizes, codes)
     norm = torch.empty(1, dtype=torch.float32, device=device)
     with _on(device):
         if ws is None:
-            ws = torch.empty(mb.moce_gradient_workspace_bytes(arr, n), dtype=torch.uint8, device=device)
-        call(arr, n, norm, ws, ws.numel() * ws.element_size(), torch.cuda.current_stream(device))
+            ws = torch.empty(mb.moce_gradient_workspace_bytes(grads, n), dtype=torch.uint8, device=device)
+        call(grads, n, norm, ws, ws.numel() * ws.element_size(), _raw_stream(index))
     return norm
 
 

@@ -103,7 +103,7 @@ def test_zero_gradients_and_a_largest_norm_of_zero():
     assert float(gradient_norm([torch.empty(0, device="cuda")])) == 0.0
     e = torch.empty(1, device="cuda")
     ws = torch.empty(256, dtype=torch.uint8, device="cuda")
-    mb.moce_gradient_norm((mb.moce_gradient * 1)(), 0, e, ws, 256, torch.cuda.current_stream())
+    mb.moce_gradient_norm(mb.make_gradients([], [], [], []), 0, e, ws, 256, torch.cuda.current_stream())
     assert float(e) == 0.0
 
 
