@@ -48,7 +48,7 @@ struct GemmArgs {
   Operand a, b;
   int R, N, K;            // rows, columns, contraction
   int klen;               // contraction of one split, a multiple of the stage's
-  int tr, tc;             // tiles down and across
+  int tr, tc, splits;     // tiles down and across, parts of the contraction
   // output: row r at r ld, columns as an operand's line
   void *y, *z;
   const void* res;
@@ -117,8 +117,8 @@ __device__ __forceinline__ void stream8(float* p, const float (&v)[8]) {
 }
 
 // ---- activations -------------------------------------------------------------
-// The standard normal distribution function of z, and e^(-z^2 / 2) beside it.
-// float32 takes the library's complementary error function.  bfloat16 takes
+// The standard normal distribution function of z, and e^(-z^2 / 2) beside it
+// (the derivative of GELU, whose float32 sums keep its error).  float32 takes the library's complementary error function.  bfloat16 takes
 // the rational approximation of Abramowitz and Stegun 7.1.26 (error of the
 // error function below 1.5e-7), a quarter of the instructions.
 template <typename T>
@@ -151,8 +151,21 @@ template <typename T>
 __device__ __forceinline__ float act_value(float z, int act) {
   if (act == MOCE_ACT_RELU) return z < 0.f ? 0.f : z;
   if (act == MOCE_ACT_GELU) {
-    float e;
-    return fmaxf(z, -1e4f) * normal_cdf<T>(z, &e);
+    if constexpr (sizeof(T) == 4) {
+      float e;
+      return fmaxf(z, -1e4f) * normal_cdf<T>(z, &e);
+    }
+    // max(z, 0) - x Q(x) with x = |z| and Q(x) = P(Z > x) for a normal Z: log2
+    // Q is smooth, and this polynomial (a minimax fit weighted by x Q) leaves
+    // 6e-7 in x Q.  Half the instructions of the distribution function, which
+    // are a third of the time of a projection of 768 channels.
+    const float x = fabsf(z);
+    float p = fmaf(-4.87802085e-4f, x, 7.1974122e-3f);
+    p = fmaf(p, x, -5.21416664e-2f);
+    p = fmaf(p, x, -0.459609509f);
+    p = fmaf(p, x, -1.15098572f);
+    p = fmaf(p, x, -1.00000489f);
+    return fmaf(-fminf(x, 1e4f), __builtin_amdgcn_exp2f(p), fmaxf(z, 0.f));
   }
   if (act == MOCE_ACT_SILU) return fmaxf(z, -1e4f) * sigmoid<T>(z);
   return z;
@@ -335,17 +348,22 @@ __device__ __forceinline__ f32x4 multiply(u32x4 col, u32x4 row, f32x4 acc) {
   }
 }
 
-// The tile of a workgroup.  Workgroup u runs on XCD u mod 8 and takes the
-// (u / 8)-th of that XCD's eighth of the tiles, which go down kGroup rows of
-// tiles before they go across: the tiles that run together on an XCD share
-// the lines they read in its L2.  False past the last tile.
+// The tile and the split of a workgroup.  Workgroup u runs on XCD u mod 8 and
+// takes the (u / 8)-th of that XCD's eighth of the work, which goes through the
+// tiles of one split after the other, down kGroup rows of tiles before it goes
+// across: what runs together on an XCD shares the lines it reads in its L2.
+// (With a split's tiles spread over the XCDs each of them read both operands
+// whole: the weight's gradient of 50432 tokens, 768 by 768, took 114 us, not
+// 104.)  False past the last.
 constexpr int kGroup = 8;
-__device__ __forceinline__ bool tile_of(const GemmArgs& g, int& r, int& c) {
-  const int u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  if (u >= g.tr * g.tc) return false;
-  const int band = u / (kGroup * g.tc), r0 = band * kGroup, n = min(kGroup, g.tr - r0), v = u - r0 * g.tc;
-  r = r0 + v % n;
-  c = v / n;
+__device__ __forceinline__ bool tile_of(const GemmArgs& g, int& r, int& c, int& split) {
+  const int n = g.tr * g.tc, w = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  split = w / n;
+  if (split >= g.splits) return false;
+  const int u = w - split * n;
+  const int band = u / (kGroup * g.tc), r0 = band * kGroup, down = min(kGroup, g.tr - r0), v = u - r0 * g.tc;
+  r = r0 + v % down;
+  c = v / down;
   return true;
 }
 
@@ -405,7 +423,7 @@ struct Finish {
       v[4 + e] = hi[e];
     }
   }
-  __device__ __forceinline__ void run(f32x4 (&acc)[FR][FC], unsigned char* l, int lane) {
+  __device__ __forceinline__ void run(f32x4 (&acc)[FR][FC], unsigned char* l, int lane, int split) {
     float sc[8], sh[8];
     column_affine(g, c, sc, sh);
     T *y = static_cast<T*>(g.y), *z = static_cast<T*>(g.z);
@@ -468,7 +486,7 @@ struct Finish {
           float v[8];
           value(l, it, v);
           row_affine(g, row(f * kPer + it), sc, sh);
-          finish8<T>(g, row(f * kPer + it), c, blockIdx.y, v, sc, sh);
+          finish8<T>(g, row(f * kPer + it), c, split, v, sc, sh);
         }
       }
     }
@@ -606,10 +624,10 @@ k_project(GemmArgs g) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % WR * 16 * FR, wc = wave / WR * 16 * FC;
-  int r0, c0;
-  if (!tile_of(g, r0, c0)) return;
+  int r0, c0, split;
+  if (!tile_of(g, r0, c0, split)) return;
   r0 *= TR, c0 *= TC;
-  const int k0 = blockIdx.y * g.klen, length = min(g.K, k0 + g.klen) - k0;
+  const int k0 = split * g.klen, length = min(g.K, k0 + g.klen) - k0;
   const int n = (length + kDepth - 1) / kDepth;
 
   // a wave's part of LDS for its results
@@ -713,7 +731,7 @@ k_project(GemmArgs g) {
   __builtin_amdgcn_s_waitcnt(vm_wait(0));
   __syncthreads();
   const int w = wave / kEach;
-  fin.run(acc, (w == 0 ? a0 : w == 1 ? b0 : w == 2 ? a1 : b1) + wave % kEach * kPart, lane);
+  fin.run(acc, (w == 0 ? a0 : w == 1 ? b0 : w == 2 ? a1 : b1) + wave % kEach * kPart, lane, split);
 }
 
 // ---- few positions ---------------------------------------------------------------
@@ -1017,32 +1035,59 @@ __global__ void __launch_bounds__(kThreads)
 k_project_turn(DzArgs a, int across) {
   using E = Elem<T>;
   constexpr int kPitch = 64 + 4 / (int)sizeof(T) * 1;   // odd words: lanes down a column on different banks
-  __shared__ T s[64 * kPitch];
+  __shared__ __attribute__((aligned(16))) T s[64 * kPitch];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t u = blockIdx.x;                         // image and run of positions
   const int64_t b = u / across;
   const int p = (int)(u % across) * 64 + lane, c0 = blockIdx.y * 64;
   const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
   T* dz = static_cast<T*>(a.dz);
-  float v[16], q[16];
+  const int cw = c0 + 16 * wave;
+  float v[16];
+  T d[16], q[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int c = c0 + 16 * wave + i;
-    const int64_t e = (b * a.O + min(c, a.O - 1)) * a.hw + min(p, a.hw - 1);
-    v[i] = E::to_f(dy[e]);
-    q[i] = a.act != MOCE_ACT_NONE ? E::to_f(z[e]) : 0.f;
+    const int64_t e = (b * a.O + min(cw + i, a.O - 1)) * a.hw + min(p, a.hw - 1);
+    d[i] = dy[e];
+    if (a.act != MOCE_ACT_NONE) q[i] = z[e];
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int c = c0 + 16 * wave + i;
-    const bool there = c < a.O && p < a.hw;
-    v[i] = there ? act_gradient<T>(q[i], v[i], a.act) : 0.f;
-    if (dz && there) dz[(b * a.O + c) * a.hw + p] = E::from_f(v[i]);
-    if (a.part) {
-      const float t = wave_sum(v[i]);
-      if (lane == 0 && c < a.O) a.part[u * a.O + c] = t;
+    const bool there = cw + i < a.O && p < a.hw;
+    const float f = E::to_f(d[i]);
+    v[i] = there ? (a.act != MOCE_ACT_NONE ? act_gradient<T>(E::to_f(q[i]), f, a.act) : f) : 0.f;
+    if (dz && there) dz[(b * a.O + cw + i) * a.hw + p] = E::from_f(v[i]);
+  }
+  if (a.pack) {
+    float w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = a.scale ? v[i] * a.scale[min(cw + i, a.O - 1)] : v[i];
+    T* to = s + lane * kPitch + 16 * wave;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint32_t*>(to + i) = pack_bf16x2(w[i], w[i + 1]);
+      } else {
+        to[i] = w[i];
+        to[i + 1] = w[i + 1];
+      }
     }
-    if (a.pack) s[lane * kPitch + 16 * wave + i] = E::from_f(a.scale ? v[i] * a.scale[min(c, a.O - 1)] : v[i]);
+  }
+  if (a.part) {
+    // the 16 channels' sums over the lanes: each step gives half the channels
+    // away and adds what it gets for the others
+#pragma unroll
+    for (int h = 8; h > 0; h >>= 1) {
+      const bool up = lane & h;
+#pragma unroll
+      for (int i = 0; i < h; ++i) {
+        const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+        v[i] = keep + __shfl_xor(give, h, kWave);
+      }
+    }
+    v[0] += __shfl_xor(v[0], 16, kWave);
+    v[0] += __shfl_xor(v[0], 32, kWave);
+    if (lane < 16 && cw + lane < a.O) a.part[u * a.O + cw + lane] = v[0];
   }
   if (!a.pack) return;
   __syncthreads();
@@ -1066,6 +1111,7 @@ k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* _
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6, o = blockIdx.x * 64 + x;
   float t = 0.f;
   if (o < O)
+#pragma unroll 8
     for (int64_t i = y; i < groups; i += 16) t += part[i * O + o];
   s[y][x] = t;
   __syncthreads();
@@ -1158,7 +1204,8 @@ size_t part_bytes(int64_t R, int64_t N, const Plan& p) { return (size_t)p.splits
 template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC, int D>
 void launch_tiles(GemmArgs g, int splits, hipStream_t st) {
   g.tr = (int)ceil_div(g.R, 16 * WR * FR), g.tc = (int)ceil_div(g.N, 16 * WC * FC);
-  const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc, 8) * 8), splits);
+  g.splits = splits;
+  const dim3 grid((unsigned)(ceil_div((int64_t)g.tr * g.tc * splits, 8) * 8));
   hipLaunchKernelGGL((k_project<T, AK, BK, IMG, WR, WC, FR, FC, D>), grid, dim3(64 * WR * WC), 0, st, g);
 }
 
