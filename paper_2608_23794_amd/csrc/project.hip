@@ -76,6 +76,14 @@ struct Elem<float> {
   static __device__ __forceinline__ float from_f(float v) { return v; }
 };
 
+// Two values rounded to bfloat16 by one conversion (of one value each they
+// take two, and two more to join).
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
 // 8 elements at any alignment (the hardware's unaligned vector accesses)
 __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
   u32x4 u;
@@ -88,8 +96,8 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
 }
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) { __builtin_memcpy(v, p, 32); }
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  const u32x4 u = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                   pack_bf16x2(v[6], v[7])};
+  const u32x4 u = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]),
+                   pack2(v[6], v[7])};
   __builtin_memcpy(p, &u, 16);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
@@ -101,14 +109,14 @@ __device__ __forceinline__ void load4(const uint16_t* p, float* v) {
 }
 __device__ __forceinline__ void load4(const float* p, float* v) { __builtin_memcpy(v, p, 16); }
 __device__ __forceinline__ void store4(uint16_t* p, const float* v) {
-  const uint32_t u[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  const uint32_t u[2] = {pack2(v[0], v[1]), pack2(v[2], v[3])};
   __builtin_memcpy(p, u, 8);
 }
 __device__ __forceinline__ void store4(float* p, const float* v) { __builtin_memcpy(p, v, 16); }
 
 // The same past the caches, for results in whole aligned rows.
 __device__ __forceinline__ void stream8(uint16_t* p, const float (&v)[8]) {
-  const u32x4 u = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  const u32x4 u = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
   __builtin_nontemporal_store(u, reinterpret_cast<u32x4*>(p));
 }
 __device__ __forceinline__ void stream8(float* p, const float (&v)[8]) {
@@ -170,11 +178,17 @@ __device__ __forceinline__ float act_value(float z, int act) {
   if (act == MOCE_ACT_SILU) return fmaxf(z, -1e4f) * sigmoid<T>(z);
   return z;
 }
-template <typename T>
-__device__ __forceinline__ void act_values(float (&v)[8], int act) {
-  if (act == MOCE_ACT_NONE) return;
+template <typename T, int N>
+__device__ __forceinline__ void act_values(float (&v)[N][8], int act) {
+  auto all = [&](int a) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = act_value<T>(v[i], act);
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u][i] = act_value<T>(v[u][i], a);
+  };
+  if (act == MOCE_ACT_RELU) all(MOCE_ACT_RELU);
+  if (act == MOCE_ACT_GELU) all(MOCE_ACT_GELU);
+  if (act == MOCE_ACT_SILU) all(MOCE_ACT_SILU);
 }
 // act'(z) dy; ReLU selects, so that an upstream value that is not finite stays on its own positions
 template <typename T>
@@ -441,38 +455,56 @@ struct Finish {
           *reinterpret_cast<f32x4*>(l + r * kPitch + ((ch ^ (r & 7)) << 4)) = acc[f + i][j];
         }
       if (!g.part && fit) {
+        // each step over the whole batch: one decision for 8 kBatch values,
+        // and as many independent chains
         auto batch = [&](int it) __attribute__((always_inline)) {
+          const int i0 = f * kPer + it;
+          float v[kBatch][8];
           T8 q[kBatch];
-          float rsc[kBatch], rsh[kBatch];
+          if (g.res)
 #pragma unroll
-          for (int u = 0; u < kBatch; ++u) {
-            const int i = f * kPer + it + u, r = min(row(i), g.R - 1);
-            rsc[u] = g.per_row && g.scale ? g.scale[r] : 1.f;
-            rsh[u] = g.per_row && g.shift ? g.shift[r] : 0.f;
-            if (g.res) {
+            for (int u = 0; u < kBatch; ++u) {
               if constexpr (kAhead)
-                q[u] = ahead[i];
+                q[u] = ahead[i0 + u];
               else
-                q[u] = residual(i);
+                q[u] = residual(i0 + u);
+            }
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) value(l, it + u, v[u]);
+          if (!g.per_row) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[u][e] = fmaf(v[u][e], sc[e], sh[e]);
+          } else {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              const int r = min(row(i0 + u), g.R - 1);
+              const float a = g.scale ? g.scale[r] : 1.f, b = g.shift ? g.shift[r] : 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[u][e] = fmaf(v[u][e], a, b);
             }
           }
+          if (g.res)
 #pragma unroll
-          for (int u = 0; u < kBatch; ++u) {
-            const int r = row(f * kPer + it + u);
-            float v[8];
-            value(l, it + u, v);
+            for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], g.per_row ? rsc[u] : sc[e], g.per_row ? rsh[u] : sh[e]);
-            if (g.res)
+              for (int e = 0; e < 8; ++e) v[u][e] += Elem<T>::to_f(q[u][e]);
+          auto store = [&](T* to) __attribute__((always_inline)) {
+            T* p = to + at + row(i0) * g.ld;
+            if (stream) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += Elem<T>::to_f(q[u][e]);
-            if (r < g.R) {
-              T *yr = y + r * g.ld + at, *zr = z + r * g.ld + at;
-              if (z) stream ? stream8(zr, v) : store8(zr, v);
-              act_values<T>(v, g.act);
-              stream ? stream8(yr, v) : store8(yr, v);
+              for (int u = 0; u < kBatch; ++u)
+                if (row(i0 + u) < g.R) stream8(p + u * kDown * g.ld, v[u]);
+            } else {
+#pragma unroll
+              for (int u = 0; u < kBatch; ++u)
+                if (row(i0 + u) < g.R) store8(p + u * kDown * g.ld, v[u]);
             }
-          }
+          };
+          if (z) store(z);
+          act_values<T>(v, g.act);
+          store(y);
         };
         if constexpr (kAhead) {   // the residual's registers by constant places
 #pragma unroll
@@ -932,8 +964,13 @@ __device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, float (&v
     if (a.act != MOCE_ACT_NONE) {
       float q[8];
       load8(z + e, q);
+      auto all = [&](int act) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = act_gradient<T>(q[i], v[i], a.act);
+        for (int i = 0; i < 8; ++i) v[i] = act_gradient<T>(q[i], v[i], act);
+      };
+      if (a.act == MOCE_ACT_RELU) all(MOCE_ACT_RELU);
+      if (a.act == MOCE_ACT_GELU) all(MOCE_ACT_GELU);
+      if (a.act == MOCE_ACT_SILU) all(MOCE_ACT_SILU);
     }
     if (dz) store8(dz + e, v);
     return;
@@ -1066,7 +1103,7 @@ k_project_turn(DzArgs a, int across) {
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint32_t*>(to + i) = pack_bf16x2(w[i], w[i + 1]);
+        *reinterpret_cast<uint32_t*>(to + i) = pack2(w[i], w[i + 1]);
       } else {
         to[i] = w[i];
         to[i + 1] = w[i + 1];
