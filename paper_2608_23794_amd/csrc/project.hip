@@ -1065,66 +1065,36 @@ k_project_dz_planes(DzArgs a, int lanes) {
 }
 
 // Channels-first to lines of channels: a workgroup turns 64 channels by 64
-// positions of an image through LDS, a wave 16 channels, a lane a position;
-// pack: [position][ld], zeros behind O.  part: a group per 64 positions.
+// positions of an image through LDS, a thread eight positions of a channel at
+// a time; pack: [position][ld], zeros behind O.  part: a group per 64
+// positions.  (A lane a position, two bytes a load, took 52 us at 64 images of
+// 1024 channels by 14 x 14, not 31.)
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_project_turn(DzArgs a, int across) {
   using E = Elem<T>;
-  constexpr int kPitch = 64 + 4 / (int)sizeof(T) * 1;   // odd words: lanes down a column on different banks
+  constexpr int kPitch = 64 + 4 / (int)sizeof(T);   // odd words: positions on different banks
   __shared__ __attribute__((aligned(16))) T s[64 * kPitch];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t u = blockIdx.x;                         // image and run of positions
+  const int64_t u = blockIdx.x;                     // image and run of positions
   const int64_t b = u / across;
-  const int p = (int)(u % across) * 64 + lane, c0 = blockIdx.y * 64;
-  const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
-  T* dz = static_cast<T*>(a.dz);
-  const int cw = c0 + 16 * wave;
-  float v[16];
-  T d[16], q[16];
+  const int p0 = (int)(u % across) * 64, c0 = blockIdx.y * 64;
+  const int pc = threadIdx.x % 8 * 8, p = p0 + pc, n = min(8, a.hw - p);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int64_t e = (b * a.O + min(cw + i, a.O - 1)) * a.hw + min(p, a.hw - 1);
-    d[i] = dy[e];
-    if (a.act != MOCE_ACT_NONE) q[i] = z[e];
-  }
+  for (int h = 0; h < 2; ++h) {
+    const int cl = h * 32 + threadIdx.x / 8, c = c0 + cl;
+    float v[8] = {};
+    if (c < a.O && n > 0) dz8<T>(a, (b * a.O + c) * a.hw + p, n, v);
+    if (a.part) {
+      float t = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const bool there = cw + i < a.O && p < a.hw;
-    const float f = E::to_f(d[i]);
-    v[i] = there ? (a.act != MOCE_ACT_NONE ? act_gradient<T>(E::to_f(q[i]), f, a.act) : f) : 0.f;
-    if (dz && there) dz[(b * a.O + cw + i) * a.hw + p] = E::from_f(v[i]);
-  }
-  if (a.pack) {
-    float w[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = a.scale ? v[i] * a.scale[min(cw + i, a.O - 1)] : v[i];
-    T* to = s + lane * kPitch + 16 * wave;
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint32_t*>(to + i) = pack2(w[i], w[i + 1]);
-      } else {
-        to[i] = w[i];
-        to[i + 1] = w[i + 1];
-      }
+      for (int o = 4; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
+      if (pc == 0 && c < a.O) a.part[u * a.O + c] = t;
     }
-  }
-  if (a.part) {
-    // the 16 channels' sums over the lanes: each step gives half the channels
-    // away and adds what it gets for the others
+    if (a.pack) {
+      const float f = a.scale ? a.scale[min(c, a.O - 1)] : 1.f;
 #pragma unroll
-    for (int h = 8; h > 0; h >>= 1) {
-      const bool up = lane & h;
-#pragma unroll
-      for (int i = 0; i < h; ++i) {
-        const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
-        v[i] = keep + __shfl_xor(give, h, kWave);
-      }
+      for (int i = 0; i < 8; ++i) s[(pc + i) * kPitch + cl] = E::from_f(v[i] * f);
     }
-    v[0] += __shfl_xor(v[0], 16, kWave);
-    v[0] += __shfl_xor(v[0], 32, kWave);
-    if (lane < 16 && cw + lane < a.O) a.part[u * a.O + cw + lane] = v[0];
   }
   if (!a.pack) return;
   __syncthreads();
@@ -1132,12 +1102,12 @@ k_project_turn(DzArgs a, int across) {
   constexpr int kVec = E::kVec, kLanes = 64 / kVec;
 #pragma unroll
   for (int i = threadIdx.x; i < 64 * kLanes; i += kThreads) {
-    const int row = i / kLanes, c = i % kLanes * kVec, at = (int)(u % across) * 64 + row;
-    if (at >= a.hw || c0 + c >= a.ld) continue;
+    const int row = i / kLanes, c = i % kLanes * kVec;
+    if (p0 + row >= a.hw || c0 + c >= a.ld) continue;
     T w[kVec];
 #pragma unroll
     for (int j = 0; j < kVec; ++j) w[j] = s[row * kPitch + c + j];
-    __builtin_memcpy(static_cast<T*>(a.pack) + (b * a.hw + at) * a.ld + c0 + c, w, 16);
+    __builtin_memcpy(static_cast<T*>(a.pack) + (b * a.hw + p0 + row) * a.ld + c0 + c, w, 16);
   }
 }
 
