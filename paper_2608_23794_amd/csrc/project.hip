@@ -1145,26 +1145,28 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The tiles there are: tr x tc, stages in LDS, workgroups a CU, and the
 // microseconds of a bfloat16 stage on a CU that is full (a workgroup's share)
-// and on one of its own.  The times and those of plan() are fitted to 3000
+// and on one of its own.  These times and those of plan() are fitted to 3000
 // measured cuts of 165 products (forward, dx and dW from one position to
-// 360000, 32 to 4096 channels): the cut they pick is 4% slower than the best
-// one measured on average, 28% at worst.
+// 360000, 32 to 4096 channels): the cut they pick is 1.4% slower than the best
+// one measured on average, 20% at worst.
 struct Tile {
   int tr, tc, stages, per_cu;
   double busy, alone;
 };
 enum { kT256, kT128, kT128x64, kT64x128, kT128x64Deep, kT64x128Deep, kT64, kT128x64Once, kT64x128Once, kTiles };
 constexpr Tile kTile[kTiles] = {
-    {256, 256, 2, 1, 1.80, 1.50},  // the most products for an LDS read: 1300 TFLOP/s where it fills the GPU
-    {128, 128, 2, 2, 0.46, 0.72},  // 1130
-    {128, 64, 2, 3, 0.30, 0.64},   // 890; three workgroups a CU hide each other's ends
-    {64, 128, 2, 3, 0.30, 0.64},
-    {128, 64, 3, 2, 0.30, 0.42},   // few tiles, long contractions: 1024 x 2048 over 2048 in 15 us, not 20
-    {64, 128, 3, 2, 0.30, 0.42},
-    {64, 64, 3, 3, 0.23, 0.29},    // few outputs
-    {128, 64, 1, 4, 0.30, 0.55},   // contractions of one stage: 56 x 56 x 64, 64 to 256 channels, 61 us, not 74
-    {64, 128, 1, 4, 0.30, 0.55},
+    {256, 256, 2, 1, 1.81, 1.45},  // the most products for an LDS read: 1350 TFLOP/s where it fills the GPU
+    {128, 128, 2, 2, 0.48, 0.70},  // 1130
+    {128, 64, 2, 3, 0.30, 0.69},   // 890; three workgroups a CU hide each other's ends
+    {64, 128, 2, 3, 0.30, 0.69},
+    {128, 64, 3, 2, 0.36, 0.34},   // few tiles, long contractions: 1024 x 2048 over 2048 in 15 us, not 20
+    {64, 128, 3, 2, 0.36, 0.34},
+    {64, 64, 3, 3, 0.20, 0.24},    // few outputs
+    {128, 64, 1, 4, 0.30, 0.86},   // contractions of one stage: 56 x 56 x 64, 64 to 256 channels, 54 us, not 66
+    {64, 128, 1, 4, 0.30, 0.86},
 };
+// Parts of the contraction: above eight in multiples of the dies.
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 16, 24, 32, 48, 64, 96, 128, 192, 256};
 
 // How a product is cut: its tile and, where the tiles are too few for the GPU,
 // the contraction in `splits` lengths whose sums are joined by another kernel.
@@ -1172,14 +1174,14 @@ struct Plan {
   int tile, splits, klen;
 };
 // ragged: the output's rows are not whole chunks; turned: both operands lie
-// across the contraction (twice the LDS reads).
+// across the contraction (more LDS reads).
 Plan plan(int64_t R, int64_t N, int64_t K, int elem, bool ragged, bool turned) {
   constexpr int kCUs = 256;
   const int depth = kLine / (elem == MOCE_F32 ? 4 : 2), stages = (int)ceil_div(K, depth);
   // sweep
   // The time of a cut: rounds of workgroups over the CUs, each as long as its
   // stages and its ends (the way of the first operands and of the results,
-  // 12.6 KB a microsecond and CU); then the join.
+  // 12.9 KB a microsecond and CU); then the join.
   Plan best{};
   double least = 1e300;
   for (int t = 0; t < kTiles; ++t) {
@@ -1187,17 +1189,21 @@ Plan plan(int64_t R, int64_t N, int64_t K, int elem, bool ragged, bool turned) {
     if (c.stages == 1 ? stages != 1 : elem == MOCE_F32 && (t == kT256 || c.stages == 3) && t != kT64) continue;
     const int64_t tiles = ceil_div(R, c.tr) * ceil_div(N, c.tc), slots = (int64_t)kCUs * c.per_cu;
     // float32: bound by its matrix instructions
-    const double busy = elem == MOCE_F32 ? 0.36 / 4096 * c.tr * c.tc : turned ? 1.25 * c.busy : c.busy;
-    const double alone = std::max(c.alone, elem == MOCE_F32 ? 1.13 * busy : busy);
-    for (int64_t s = 1; s <= 256; s += s < 8 ? 1 : s / 4) {
-      if (s > 1 && (stages / s < 6 || tiles * (s - 1) >= 2 * slots)) break;
+    const double busy = elem == MOCE_F32 ? 0.68 / 4096 * c.tr * c.tc : turned ? 1.16 * c.busy : c.busy;
+    const double alone = std::max(c.alone, elem == MOCE_F32 ? 1.03 * busy : busy);
+    for (const int s : kSplits) {
+      if (s > 1 && (stages / s < 2 || tiles * (s - 1) >= 2 * slots)) break;
       const int64_t each = ceil_div(stages, s), splits = ceil_div(stages, each);
       const int64_t rounds = tiles * splits / slots, k = ceil_div(tiles * splits % slots, kCUs);
-      const int bytes = splits > 1 || elem == MOCE_F32 ? 4 : ragged ? 2 * 2 : 2;
-      const double end = c.tr * c.tc * bytes / 12600., begin = 7. / c.per_cu;
+      // rows in pieces; short runs of memory
+      const double pieces = splits > 1 ? 1. : ragged ? 2.65 : c.tc == 64 ? 1.05 : 1.;
+      const double end = c.tr * c.tc * (splits > 1 || elem == MOCE_F32 ? 4 : 2) * pieces / 12900., begin = 4.7 / c.per_cu;
       double time = rounds * (each * c.per_cu * busy + begin + end * c.per_cu);
       if (k > 0) time += each * std::max(alone, k * busy) + begin + end * k;
-      if (splits > 1) time += 3 + (double)splits * R * N * 4 / 2e6;
+      if (splits > 1) {
+        if (splits % 8) time *= 1.125;   // splits that lie on two dies are read by both
+        time += 6.8 + (double)splits * R * N * 4 / 2.9e6;
+      }
       if (time < least) {
         least = time;
         best = Plan{t, (int)splits, (int)(each * depth)};
