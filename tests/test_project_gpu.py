@@ -379,3 +379,43 @@ def test_tiles(size, dtype):
     y = t["layer"].forward(t["x"], residual=res, z=z)
     check_forward(t, dtype, layout, act, res, y, z)
     check_backward(t, dtype, layout, act, t["layer"].backward(t["x"], t["dy"], z=t["z"], residual=residual))
+
+
+@pytest.mark.parametrize("size", [(1, 96, 64, 300, 1, "nhwc"), (2, 512, 512, 20, 16, "nchw"), (1, 33, 20, 70, 1, "nhwc"),
+                                  (1, 300, 24, 6, 1, "nhwc")], ids=str)
+@pytest.mark.parametrize("scale", [1e-35, 1e-20, 1e18])
+def test_float32_keeps_its_bits_at_any_size_of_the_values(size, scale):
+    """float32 products at the ends of the range, and beside values of ordinary size."""
+    B, C, O, H, W, layout = size
+    t = make(B, C, O, H, W, "f32", layout, "none", seed=11)
+    t["x"].mul_(scale)
+    t["dy"].mul_(scale)
+    if layout == "nhwc":
+        t["x"][..., : C // 2].div_(scale)
+    else:
+        t["x"][:, : C // 2].div_(scale)
+    check_forward(t, "f32", layout, "none", None, t["layer"].forward(t["x"]), None)
+    out = t["layer"].backward(t["x"], t["dy"])
+    dx, mag = rows(t["dy"], layout) @ t["w"].double(), rows(t["dy"], layout).abs() @ t["w"].double().abs()
+    check("dx", rows(out["dx"], layout), dx, HALF["f32"] * 1.01 * dx.abs() + (O + 8) * STEP32 * mag + 2.0 ** -149)
+
+
+def test_float32_values_that_are_not_finite():
+    """Infinities meet weights without lower bits, zeros and each other as in float32 arithmetic."""
+    x = torch.randn(200, 64, device="cuda")
+    w = torch.randn(72, 64, device="cuda")
+    w[5], w[6, 3] = 1.0, 0.0
+    x[7, 3], x[8, 3], x[9, 3], x[9, 4] = float("inf"), float("-inf"), float("inf"), float("-inf")
+    x[150, 10] = float("nan")
+    x[30], w[8] = 3e38, 1.5
+    y = ProjectLayer(w).forward(x)
+    want = x.cpu() @ w.cpu().t()
+    kind = torch.where(torch.isnan(want), 2.0, torch.where(torch.isinf(want), want.sign() * 1.0, torch.zeros_like(want)))
+    got = y.cpu()
+    kind_got = torch.where(torch.isnan(got), 2.0, torch.where(torch.isinf(got), got.sign() * 1.0, torch.zeros_like(got)))
+    rest = torch.ones(200, dtype=torch.bool)
+    rest[30] = False          # sums that overflow on the way go by their order
+    assert torch.equal(kind_got[rest], kind[rest])
+    fine = rest[:, None] & torch.isfinite(want)
+    mag = x.cpu().abs().nan_to_num(0.0, 0.0, 0.0).double() @ w.cpu().abs().double().t()
+    assert ((got.double() - want.double()).abs()[fine] <= (80 * STEP32 * mag + 1e-30)[fine]).all()
