@@ -379,7 +379,8 @@ typedef struct moce_project_desc {
 } moce_project_desc;
 
 /* Bytes of device workspace moce_project needs (0: none, or an invalid
- * descriptor).  It holds the partial products of shapes with few outputs,
+ * descriptor).  It holds operands whose lines are not whole 16 bytes, packed
+ * into lines that are, and the partial products of shapes with few outputs,
  * whose contraction is divided. */
 size_t moce_project_workspace_bytes(const moce_project_desc* desc);
 
@@ -395,8 +396,8 @@ size_t moce_project_workspace_bytes(const moce_project_desc* desc);
  * Errors: MOCE_ERR_NULL (desc, x, weight, y), MOCE_ERR_SHAPE (a size below 1,
  * an unknown act, z == y), MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN,
  * MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED when C or O
- * exceeds 2^20, B H W 2^29, C H W or O H W 2^31 - 1, or B C H W or B O H W
- * 2^33. */
+ * exceeds 2^20, C O 2^35, B H W 2^29, C H W or O H W 2^31 - 1, or B C H W or
+ * B O H W 2^33. */
 moce_status moce_project(const moce_project_desc* desc, const void* x, const void* weight, const float* scale,
                          const float* shift, const void* residual, void* y, void* z, void* ws, size_t ws_bytes,
                          hipStream_t stream);

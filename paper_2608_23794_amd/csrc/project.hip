@@ -96,8 +96,7 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
 }
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) { __builtin_memcpy(v, p, 32); }
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  const u32x4 u = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]),
-                   pack2(v[6], v[7])};
+  const u32x4 u = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
   __builtin_memcpy(p, &u, 16);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
@@ -126,9 +125,10 @@ __device__ __forceinline__ void stream8(float* p, const float (&v)[8]) {
 
 // ---- activations -------------------------------------------------------------
 // The standard normal distribution function of z, and e^(-z^2 / 2) beside it
-// (the derivative of GELU, whose float32 sums keep its error).  float32 takes the library's complementary error function.  bfloat16 takes
-// the rational approximation of Abramowitz and Stegun 7.1.26 (error of the
-// error function below 1.5e-7), a quarter of the instructions.
+// (the derivative of GELU, whose float32 sums keep its error).  float32 takes
+// the library's complementary error function; bfloat16 the rational
+// approximation of Abramowitz and Stegun 7.1.26 (error of the error function
+// below 1.5e-7), a quarter of the instructions.
 template <typename T>
 __device__ __forceinline__ float normal_cdf(float z, float* e) {
   if constexpr (sizeof(T) == 4) {
@@ -1111,21 +1111,22 @@ k_project_turn(DzArgs a, int across) {
   }
 }
 
-// dshift[o] = sum over the groups' partial sums
+// out[y][o] = sum over the y-th of gridDim.y runs of the groups' partial sums
 __global__ void __launch_bounds__(1024)
-k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* __restrict__ dshift) {
+k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* __restrict__ out) {
   __shared__ float s[16][64];
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6, o = blockIdx.x * 64 + x;
+  const int64_t each = (groups + gridDim.y - 1) / gridDim.y, g0 = blockIdx.y * each, g1 = min(groups, g0 + each);
   float t = 0.f;
   if (o < O)
 #pragma unroll 8
-    for (int64_t i = y; i < groups; i += 16) t += part[i * O + o];
+    for (int64_t i = g0 + y; i < g1; i += 16) t += part[i * O + o];
   s[y][x] = t;
   __syncthreads();
   if (y == 0 && o < O) {
     t = s[0][x];
     for (int i = 1; i < 16; ++i) t += s[i][x];
-    dshift[o] = t;
+    out[(int64_t)blockIdx.y * O + o] = t;
   }
 }
 
@@ -1421,6 +1422,22 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
   return launch_whole<T, true, false>(g, l.p, part, st);
 }
 
+// dshift from the groups' sums; many of them (small planes) by way of
+// kManyRuns runs behind them.
+constexpr int kManyGroups = 4096, kManyRuns = 256;
+hipError_t sum_groups(float* part, int64_t groups, int64_t O, float* dshift, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(O, 64)), block(1024);
+  if (groups > kManyGroups) {
+    float* runs = part + groups * O;
+    hipLaunchKernelGGL(k_project_dshift, dim3(grid.x, kManyRuns), block, 0, st, part, groups, (int)O, runs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    part = runs, groups = kManyRuns;
+  }
+  hipLaunchKernelGGL(k_project_dshift, grid, block, 0, st, part, groups, (int)O, dshift);
+  return hipGetLastError();
+}
+
 // Groups of positions whose sums of dz lie apart: rows (channels-last) in up
 // to 1024 workgroups, images or 64 positions of them (channels-first).
 struct DzPlan {
@@ -1444,6 +1461,7 @@ bool project_limits(const ProjectShape& s) {
   constexpr int64_t kCh = 1 << 20;
   if (s.C > kCh || s.O > kCh || s.HW > INT_MAX / std::max(s.C, s.O)) return false;
   // positions and elements whose threads one launch holds
+  if (s.O > ((int64_t)1 << 35) / s.C) return false;
   return s.B <= ((int64_t)1 << 29) / s.HW && s.B <= ((int64_t)1 << 33) / (std::max(s.C, s.O) * s.HW);
 }
 
@@ -1478,7 +1496,8 @@ BwdLayout bwd_layout(const ProjectShape& s) {
   l.dz = take(s.act != MOCE_ACT_NONE || z.rows(s.O) ? z.packed(s.O) : 0);
   l.x = take(z.rows(s.C) ? z.packed(s.C) : 0);
   l.weight = take((size_t)std::max(s.O * z.up(s.C), z.up(s.O) * s.C) * z.el());
-  l.shift = take((size_t)dz_plan(z).groups * s.O * sizeof(float));
+  const int64_t groups = dz_plan(z).groups;
+  l.shift = take((size_t)(groups + (groups > kManyGroups ? kManyRuns : 0)) * s.O * sizeof(float));
   // one after the other on the stream, so both products' partial sums share their place
   l.part = take(std::max(l.px.splits > 1 ? part_bytes(g.R, g.N, l.px) : 0, part_bytes(s.O, s.C, l.pw)));
   l.total = at;
@@ -1534,9 +1553,8 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
       if (e != hipSuccess) return e;
     }
     if (gr.dshift) {
-      hipLaunchKernelGGL(k_project_dshift, dim3((unsigned)ceil_div(s.O, 64)), dim3(1024), 0, st, a.part, dp.groups,
-                         (int)s.O, gr.dshift);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      e = sum_groups(a.part, dp.groups, s.O, gr.dshift, st);
+      if (e != hipSuccess) return e;
     }
   }
   float* part = reinterpret_cast<float*>(ws + l.part);

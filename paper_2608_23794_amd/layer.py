@@ -294,6 +294,12 @@ def _need(name: str, t: torch.Tensor, shape, dtype, device):
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', strided'}")
 
 
+def _given_workspace(ws: torch.Tensor, device):
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"the workspace has to be a contiguous tensor on {device}, got one on {ws.device}")
+    return ws, ws.numel() * ws.element_size()
+
+
 class ProjectLayer:
     """A dense pointwise projection: y = act(scale x W^T + shift + residual) over the channels.
 
@@ -343,7 +349,7 @@ class ProjectLayer:
 
     def _workspace(self, n: int, ws: Optional[torch.Tensor]):
         if ws is not None:
-            return ws, ws.numel() * ws.element_size()
+            return _given_workspace(ws, self.device)
         return (torch.empty(n, dtype=torch.uint8, device=self.device) if n else None), n
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
@@ -430,7 +436,7 @@ def _gradient_call(tensors, out, ws, call):
     with _on(device):
         if ws is None:
             ws = torch.empty(mb.moce_gradient_workspace_bytes(grads, n), dtype=torch.uint8, device=device)
-        call(grads, n, norm, ws, ws.numel() * ws.element_size(), _raw_stream(index))
+        call(grads, n, norm, *_given_workspace(ws, device), _raw_stream(index))
     return norm
 
 

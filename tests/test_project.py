@@ -45,7 +45,7 @@ def backward(d, x=FAKE, weight=FAKE, scale=None, z=FAKE, dy=FAKE, ws=FAKE, n=GIB
     (dict(B=0), -2), (dict(C=0), -2), (dict(H=0), -2), (dict(W=-3), -2), (dict(O=0), -2), (dict(act=4), -2),
     (dict(act=-1), -2), (dict(dtype=2), -3), (dict(layout=2), -4), (dict(C=(1 << 20) + 1), -10),
     (dict(O=(1 << 20) + 1), -10), (dict(B=(1 << 29) + 1, H=1, W=1, C=1, O=1), -10), (dict(H=1 << 20, W=1 << 11), -10),
-    (dict(C=1 << 16, H=1 << 8, W=1 << 8), -10), (dict(B=1 << 20, C=1 << 10, H=4, W=4), -10),
+    (dict(C=1 << 16, H=1 << 8, W=1 << 8), -10), (dict(C=1 << 18, O=(1 << 17) + 1, B=1, H=1, W=1), -10), (dict(B=1 << 20, C=1 << 10, H=4, W=4), -10),
 ])
 def test_descriptor(lib, change, code):
     d = desc(**change)

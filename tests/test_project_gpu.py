@@ -126,6 +126,7 @@ SIZES = [
     (1, 7, 300, 130, 1, "nhwc"), (5, 72, 40, 8, 8, "nchw"), (3, 33, 31, 7, 7, "nchw"), (9, 64, 128, 2, 1, "nchw"),
     (2, 130, 66, 14, 14, "nchw"), (70, 16, 8, 3, 5, "nchw"), (1, 2048, 16, 4, 4, "nchw"), (2, 24, 16, 61, 64, "nchw"),
     (2, 16, 24, 97, 101, "nhwc"), (16, 4096, 72, 1, 1, "nhwc"), (17, 513, 1030, 1, 1, "nhwc"),
+    (5000, 8, 16, 2, 1, "nchw"), (4200, 8, 72, 4, 2, "nchw"), (33, 264, 40, 1, 1, "nhwc"), (20, 777, 90, 1, 1, "nhwc"),
 ]
 KINDS = [("none", False, False, False), ("relu", True, True, True), ("gelu", False, True, False),
          ("silu", False, True, True), ("none", True, False, True), ("gelu", True, True, True)]
@@ -345,6 +346,8 @@ def test_layer_refusals():
         ProjectLayer(t["w"], shift=t["shift"][:-1])
     with pytest.raises(mb.MoceError):
         layer.backward(x, t["dy"], z=t["z"], ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        layer.forward(x, ws=torch.empty(1 << 20, dtype=torch.uint8))
     odd = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
     with pytest.raises(mb.MoceError):
         layer.forward(odd)                               # not 16-byte aligned
