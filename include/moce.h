@@ -390,11 +390,13 @@ size_t moce_project_workspace_bytes(const moce_project_desc* desc);
  * [O].  y is fully overwritten, and so is z where it is given (the
  * pre-activation that moce_project_backward reads, rounded to the type; y
  * itself comes from the unrounded one).  residual may be y or z (in place);
- * y, z and the other inputs may not overlap.  Sums are float32.
+ * y, z, ws and the other inputs may not overlap.  Sums are float32.
  * ws: as sized above, 256-byte aligned, contents on return unspecified; may
- * be NULL where no bytes are needed.  Asynchronous on `stream`.
+ * be NULL where no bytes are needed; calls that can run at the same time need
+ * one each, captured calls that are replayed so too.  Rows of channels of any
+ * grouping are MOCE_NHWC with B rows and H = W = 1.  Asynchronous on `stream`.
  * Errors: MOCE_ERR_NULL (desc, x, weight, y), MOCE_ERR_SHAPE (a size below 1,
- * an unknown act, z == y), MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN,
+ * an unknown act, memory that overlaps), MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN,
  * MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED when C or O
  * exceeds 2^20, C O 2^35, B H W 2^29, C H W or O H W 2^31 - 1, or B C H W or
  * B O H W 2^33. */
@@ -424,8 +426,8 @@ size_t moce_project_backward_workspace_bytes(const moce_project_desc* desc);
  * type of y).  x, weight, scale as in the forward; z: the pre-activation that
  * the forward wrote (for MOCE_ACT_RELU its y serves as well; not read for
  * MOCE_ACT_NONE).  act' of ReLU is 0 where z <= 0.  All tensors contiguous
- * and 16-byte aligned; dresidual may be dy (in place), no other output may
- * overlap an input or another output.  For bfloat16, dz enters the products
+ * and 16-byte aligned; dresidual may be dy (in place), no other output,
+ * and not ws, may overlap an input or another output.  For bfloat16, dz enters the products
  * rounded to its type (exact for MOCE_ACT_NONE and MOCE_ACT_RELU), and so does
  * the scaled weight of dx; sums are float32.  ws as sized above, 256-byte
  * aligned.  Errors: those of moce_project; MOCE_ERR_NULL for a missing dy or
@@ -470,8 +472,9 @@ moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float*
  * float32, rounded to the tensor's type.  *norm is the norm before clipping.
  * Errors: those of moce_gradient_norm; MOCE_ERR_NULL for a missing dst;
  * MOCE_ERR_SHAPE when max_norm is negative or not finite, when two tensors
- * overlap (a tensor listed twice would be scaled twice), or when a dst
- * overlaps any src but its own, or its own partly. */
+ * overlap (a tensor listed twice would be scaled twice), when a dst overlaps
+ * any src but its own, or its own partly, or when norm or ws overlaps a
+ * tensor. */
 moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float max_norm, float* norm, void* ws,
                                size_t ws_bytes, hipStream_t stream);
 

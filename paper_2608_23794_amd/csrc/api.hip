@@ -5,6 +5,7 @@
 #include <climits>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <utility>
@@ -603,6 +604,33 @@ moce_status check_project(const moce_project_desc* d, moce::ProjectShape* s) {
   return moce::project_limits(*s) ? MOCE_OK : MOCE_ERR_UNSUPPORTED;
 }
 
+// A call's memory: what it reads, then what it writes (the workspace too).
+// NULL and no bytes are apart from everything.
+struct Range {
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Range& a, const Range& b) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+  return p && q && a.bytes && b.bytes && p < q + b.bytes && q < p + a.bytes;
+}
+bool outputs_apart(std::initializer_list<Range> in, std::initializer_list<Range> out) {
+  for (const Range* o = out.begin(); o != out.end(); ++o) {
+    for (const Range& r : in)
+      if (overlap(*o, r)) return false;
+    for (const Range* q = out.begin(); q != o; ++q)
+      if (overlap(*o, *q)) return false;
+  }
+  return true;
+}
+struct ProjectBytes {
+  size_t x, y, weight, rows;   // rows: float32 [O]
+  explicit ProjectBytes(const moce::ProjectShape& s) {
+    const size_t el = s.elem == MOCE_F32 ? 4 : 2, P = (size_t)s.B * s.HW;
+    x = P * s.C * el, y = P * s.O * el, weight = (size_t)s.O * s.C * el, rows = (size_t)s.O * 4;
+  }
+};
+
 }  // namespace
 
 size_t moce_project_workspace_bytes(const moce_project_desc* desc) {
@@ -625,6 +653,11 @@ moce_status moce_project(const moce_project_desc* desc, const void* x, const voi
   const size_t need = moce::project_ws_bytes(s);
   if (need > 0 && (!ws || ws_bytes < need)) return MOCE_ERR_WORKSPACE;
   if (need > 0 && !aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const ProjectBytes n(s);
+  if (!outputs_apart({{x, n.x}, {weight, n.weight}, {scale, n.rows}, {shift, n.rows},
+                      {residual == y || residual == z ? nullptr : residual, n.y}},
+                     {{y, n.y}, {z, n.y}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
   return device_status(moce::launch_project(s, x, weight, scale, shift, residual, y, z, ws, stream));
 }
 
@@ -647,8 +680,15 @@ moce_status moce_project_backward(const moce_project_desc* desc, const void* x, 
       !aligned(grads->dweight, 16) || !aligned(grads->dresidual, 16) || !aligned(scale, 4) ||
       !aligned(grads->dscale, 4) || !aligned(grads->dshift, 4))
     return MOCE_ERR_ALIGN;
-  if (!ws || ws_bytes < moce::project_backward_ws_bytes(s)) return MOCE_ERR_WORKSPACE;
+  const size_t need = moce::project_backward_ws_bytes(s);
+  if (!ws || ws_bytes < need) return MOCE_ERR_WORKSPACE;
   if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const ProjectBytes n(s);
+  if (!outputs_apart({{x, n.x}, {weight, n.weight}, {scale, n.rows}, {s.act != MOCE_ACT_NONE ? z : nullptr, n.y},
+                      {grads->dresidual == dy ? nullptr : dy, n.y}},
+                     {{grads->dx, n.x}, {grads->dweight, n.weight}, {grads->dscale, n.rows}, {grads->dshift, n.rows},
+                      {grads->dresidual, n.y}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
   return device_status(moce::launch_project_backward(s, x, weight, scale, z, dy, *grads, ws, stream));
 }
 
@@ -719,10 +759,14 @@ moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float 
   if (st == MOCE_OK) st = check_gradient_ws(grads, count, norm, ws, ws_bytes);
   if (st != MOCE_OK) return st;
   if (!std::isfinite(max_norm) || max_norm < 0.f) return MOCE_ERR_SHAPE;
+  const size_t need = moce::gradient_ws_bytes(grads, count);
   for (int32_t i = 0; i < count; ++i) {
     if (grads[i].n == 0) continue;
     if (!grads[i].dst) return MOCE_ERR_NULL;
     if (!aligned(grads[i].dst, grads[i].dtype == MOCE_F32 ? 4 : 2)) return MOCE_ERR_ALIGN;
+    // the norm and the workspace are written before the gradients are read again
+    const size_t bytes = (size_t)grads[i].n * (grads[i].dtype == MOCE_F32 ? 4 : 2);
+    if (!outputs_apart({{grads[i].src, bytes}, {grads[i].dst, bytes}}, {{norm, 4}, {ws, need}})) return MOCE_ERR_SHAPE;
   }
   try {
     if (!ranges_apart(grads, count)) return MOCE_ERR_SHAPE;

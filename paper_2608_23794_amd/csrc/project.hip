@@ -1179,7 +1179,6 @@ struct Plan {
 Plan plan(int64_t R, int64_t N, int64_t K, int elem, bool ragged, bool turned) {
   constexpr int kCUs = 256;
   const int depth = kLine / (elem == MOCE_F32 ? 4 : 2), stages = (int)ceil_div(K, depth);
-  // sweep
   // The time of a cut: rounds of workgroups over the CUs, each as long as its
   // stages and its ends (the way of the first operands and of the results,
   // 12.9 KB a microsecond and CU); then the join.

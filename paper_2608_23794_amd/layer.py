@@ -337,7 +337,7 @@ class ProjectLayer:
         else:
             if len(s) < 2 or s[-1] != self.C:
                 raise ValueError(f"x has to be [..., {self.C}], got {tuple(s)}")
-            B, H, W = s[0], math.prod(s[1:-1]), 1
+            B, H, W = math.prod(s[:-1]), 1, 1      # rows of channels, however they are grouped
         return mb.moce_project_desc(B, self.C, H, W, self.O, _DTYPE_OF[self.dtype], _LAYOUT[self.layout],
                                     _ACT[self.act], 0)
 

@@ -86,6 +86,42 @@ def test_backward_pointers(lib):
     assert backward(d, ws=None) == -7 and backward(d, n=need - 1) == -7 and backward(d, ws=FAKE + 16) == -8
 
 
+def test_overlapping_tensors(lib):
+    """No output, and no workspace, over another tensor: the first and the last of its bytes."""
+    d = desc(act=mb.MOCE_ACT_NONE, C=60)          # x packed: a workspace
+    M = 2 * 64
+    size = {"x": M * 60 * 2, "y": M * 48 * 2, "weight": 48 * 60 * 2, "row": 48 * 4}
+    size.update(z=size["y"], residual=size["y"], dy=size["y"], dresidual=size["y"], dx=size["x"], dweight=size["weight"])
+    need, bneed = (f(ctypes.byref(d)) for f in (lib.moce_project_workspace_bytes, lib.moce_project_backward_workspace_bytes))
+    apart = {n: FAKE + (i << 20) for i, n in enumerate(("x", "weight", "scale", "shift", "residual", "y", "z", "dy", "dx",
+                                                         "dweight", "dscale", "dshift", "dresidual"))}
+    ws = FAKE + (100 << 20)
+    fwd = {n: apart[n] for n in ("x", "weight", "scale", "shift", "residual", "y", "z")}
+    for out in ("y", "z"):
+        for other in fwd:
+            if other != out:
+                assert need > 0
+                last = size.get(other, size["row"]) - 1 & ~15
+                if other != "residual":           # residual may be y or z, but only as a whole
+                    assert project(d, ws=ws, n=need, **{**fwd, out: fwd[other]}) == -2, (out, other)
+                assert project(d, ws=ws, n=need, **{**fwd, out: fwd[other] + last}) == -2, (out, other)
+    for other in fwd:
+        assert project(d, n=need, **{**fwd, "ws": fwd[other]}) == -2, other
+    ins = {n: apart[n] for n in ("x", "weight", "scale", "dy")}
+    outs = {n: apart[n] for n in ("dx", "dweight", "dscale", "dshift", "dresidual")}
+    for out in outs:
+        for other in {**ins, **outs}:
+            if other != out:
+                last = size.get(other, size["row"]) - 1 & ~15
+                place = {**ins, **outs}[other]
+                if (out, other) != ("dresidual", "dy"):
+                    assert backward(d, ws=ws, n=bneed, **ins, **{**outs, out: place}) == -2, (out, other)
+                assert backward(d, ws=ws, n=bneed, **ins, **{**outs, out: place + last}) == -2, (out, other)
+    for other, place in {**ins, **outs}.items():
+        assert backward(d, ws=place, n=bneed, **ins, **outs) == -2, other
+    assert backward(desc(C=60), ws=ws, z=outs["dx"], **ins, **outs) == -2
+
+
 def test_one_position_an_image_is_the_same_in_both_layouts(lib):
     sizes = {lib.moce_project_backward_workspace_bytes(ctypes.byref(desc(B=300, H=1, W=1, layout=l))) for l in (0, 1)}
     assert len(sizes) == 1
@@ -144,6 +180,11 @@ def test_overlapping_gradients():
     assert clip(gradients((a, a + 32, 16, F32)), 1) == -2                        # its own, partly
     assert clip(gradients((a, b, 16, F32), (b, a, 16, F32)), 2) == -2            # each other's
     assert clip(gradients((a, b, 16, F32), (a + 64, b + 60, 16, F32)), 2) == -2  # destinations
+    far = FAKE << 8
+    assert clip(gradients((a, b, 16, F32)), 1, out=a + 60, ws=far) == -2         # the norm in a tensor
+    assert clip(gradients((a, b, 16, F32)), 1, out=b, ws=far) == -2
+    assert clip(gradients((a, b, 16, F32)), 1, out=far, ws=a) == -2
+    assert clip(gradients((a, b + 256, 16, F32)), 1, out=far, ws=b) == -2        # the workspace's end
 
 
 def test_layers_refuse_what_is_not_on_the_gpu():

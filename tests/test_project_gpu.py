@@ -365,6 +365,29 @@ def test_many_positions(layout):
     check_backward(t, "bf16", layout, "relu", t["layer"].backward(t["x"], t["dy"], z=z, residual=True))
 
 
+def test_rows_of_one_image_beyond_two_gigabytes():
+    """2^21 rows of 1024 channels as one sequence, offsets past 32 bits: rows at the ends, and the sums over all."""
+    n, C, O, part = (1 << 21) + 3, 1024, 24, 1 << 18
+    g = torch.Generator(device="cuda").manual_seed(5)
+    # whole numbers: the sums over rows stay below 2^23 and are exact
+    x = torch.empty(1, n, C, dtype=torch.bfloat16, device="cuda").random_(-2, 3, generator=g)
+    w = (torch.randn(O, C, generator=g, device="cuda") * C ** -0.5).bfloat16()
+    dy = torch.empty(1, n, O, dtype=torch.bfloat16, device="cuda").random_(-1, 2, generator=g)
+    layer = ProjectLayer(w)
+    y, out = layer.forward(x), layer.backward(x, dy)
+    wd = w.double()
+    for rows in (slice(0, 40), slice(n // 2, n // 2 + 40), slice(n - 40, n)):
+        xd, dyd = x[0, rows].double(), dy[0, rows].double()
+        want, mag = xd @ wd.t(), xd.abs() @ wd.abs().t()
+        check("y", y[0, rows], want, HALF["bf16"] * want.abs() + 2 * C * STEP32 * mag)
+        want, mag = dyd @ wd, dyd.abs() @ wd.abs()
+        check("dx", out["dx"][0, rows], want, HALF["bf16"] * want.abs() + 2 * O * STEP32 * mag)
+    want = torch.zeros(O, C, dtype=torch.float64, device="cuda")
+    for i in range(0, n, part):
+        want += dy[0, i:i + part].double().t().contiguous() @ x[0, i:i + part].double()
+    check("dweight", out["dweight"], want, HALF["bf16"] * want.abs())
+
+
 # aligned shapes that take each tile with edges in it, contractions that end inside a stage, images shorter and longer
 # than a stage
 TILES = [(1, 200, 328, 700, 1, "nhwc"), (3, 136, 264, 40, 24, "nchw"), (2, 1096, 520, 33, 16, "nhwc"),
