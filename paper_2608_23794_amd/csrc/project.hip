@@ -902,14 +902,46 @@ k_project_join(GemmArgs g, int splits, int down) {
 
 // ---- the gradients' other passes -------------------------------------------------
 
+// out[o] = sum of the groups' partial sums part[group][o], of 16 channels o from
+// o0 on and the groups g0..g1, by a workgroup; s: an element per thread.
+__device__ __forceinline__ void sum_channels(const float* __restrict__ part, int64_t g0, int64_t g1, int O, int o0,
+                                             float* __restrict__ out, float* s) {
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, o = o0 + x;
+  float t = 0.f;
+  if (o < O)
+#pragma unroll 8
+    for (int64_t i = g0 + y; i < g1; i += kThreads / 16) t += part[i * O + o];
+  s[threadIdx.x] = t;
+  __syncthreads();
+  if (y == 0 && o < O) {
+#pragma unroll
+    for (int i = 1; i < kThreads / 16; ++i) t += s[16 * i + x];
+    out[o] = t;
+  }
+}
+
+// dshift, or the y-th of gridDim.y runs of its groups.
+__global__ void __launch_bounds__(kThreads)
+k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* __restrict__ out) {
+  __shared__ float s[kThreads];
+  const int64_t each = (groups + gridDim.y - 1) / gridDim.y, g0 = blockIdx.y * each;
+  sum_channels(part, g0, min(groups, g0 + each), O, blockIdx.x * 16, out + (int64_t)blockIdx.y * O, s);
+}
+
 // Row o of the weight's gradient from the splits' G: dweight = scale G, dscale
 // = <weight, G>.  `across` threads (a power of two) take the columns, the
-// others of a workgroup their share of the splits.
+// others of a workgroup their share of the splits.  Workgroups behind the O
+// rows sum dshift, 16 channels each, from `groups` partial sums.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_project_dweight(const float* __restrict__ part, int splits, int O, int C, const float* __restrict__ scale,
-                  const T* __restrict__ weight, T* __restrict__ dweight, float* __restrict__ dscale, int across) {
-  __shared__ float s[kThreads], sums[kThreads / kWave];
+                  const T* __restrict__ weight, T* __restrict__ dweight, float* __restrict__ dscale, int across,
+                  const float* __restrict__ sums, int64_t groups, float* __restrict__ dshift) {
+  __shared__ float s[kThreads], dots[kThreads / kWave];
+  if ((int)blockIdx.x >= O) {
+    sum_channels(sums, 0, groups, O, (blockIdx.x - O) * 16, dshift, s);
+    return;
+  }
   const int o = blockIdx.x, x = threadIdx.x % across, down = kThreads / across;
   const float sc = scale ? scale[o] : 1.f;
   float dot = 0.f;
@@ -935,9 +967,9 @@ k_project_dweight(const float* __restrict__ part, int splits, int O, int C, cons
   }
   if (!dscale) return;
   dot = wave_sum(dot);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = dot;
+  if ((threadIdx.x & 63) == 0) dots[threadIdx.x >> 6] = dot;
   __syncthreads();
-  if (threadIdx.x == 0) dscale[o] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  if (threadIdx.x == 0) dscale[o] = (dots[0] + dots[1]) + (dots[2] + dots[3]);
 }
 
 // The passes over dy (and z) before the products; packing x or the weight is
@@ -949,32 +981,50 @@ struct DzArgs {
   const float* scale;     // by channel
   float* part;            // [groups][O] partial sums of dz over positions (nullptr: none)
   int act, O, hw, ld;     // O channels; hw positions of a plane (channels-first)
+  int rows;               // k_project_lines: not turned
   int64_t n;              // rows of positions (channels-last), images or planes (channels-first)
   int64_t per;            // rows of one group
 };
 
-// act'(z) dy of eight neighbouring elements (n of them there) at e, stored to dz
+// act'(z) dy of N times eight neighbouring elements, at e[.] where there[.],
+// stored to dz: all loads before the first store.
+template <typename T, int N>
+__device__ __forceinline__ void dz_whole(const DzArgs& a, const int64_t (&e)[N], const bool (&there)[N], float (&v)[N][8]) {
+  const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
+  T* dz = static_cast<T*>(a.dz);
+  float q[N][8];
+#pragma unroll
+  for (int u = 0; u < N; ++u) load8(dy + e[u], v[u]);
+  if (a.act != MOCE_ACT_NONE) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) load8(z + e[u], q[u]);
+    auto all = [&](int act) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = act_gradient<T>(q[u][i], v[u][i], act);
+    };
+    if (a.act == MOCE_ACT_RELU) all(MOCE_ACT_RELU);
+    if (a.act == MOCE_ACT_GELU) all(MOCE_ACT_GELU);
+    if (a.act == MOCE_ACT_SILU) all(MOCE_ACT_SILU);
+  }
+  if (dz)
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (there[u]) store8(dz + e[u], v[u]);
+}
+// The same of the n elements at e (up to eight), zeros behind them.
 template <typename T>
 __device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, float (&v)[8]) {
   using E = Elem<T>;
-  const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
-  T* dz = static_cast<T*>(a.dz);
   if (n == 8) {
-    load8(dy + e, v);
-    if (a.act != MOCE_ACT_NONE) {
-      float q[8];
-      load8(z + e, q);
-      auto all = [&](int act) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act_gradient<T>(q[i], v[i], act);
-      };
-      if (a.act == MOCE_ACT_RELU) all(MOCE_ACT_RELU);
-      if (a.act == MOCE_ACT_GELU) all(MOCE_ACT_GELU);
-      if (a.act == MOCE_ACT_SILU) all(MOCE_ACT_SILU);
-    }
-    if (dz) store8(dz + e, v);
+    const int64_t at[1] = {e};
+    const bool there[1] = {true};
+    dz_whole<T, 1>(a, at, there, reinterpret_cast<float(&)[1][8]>(v));
     return;
   }
+  const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
+  T* dz = static_cast<T*>(a.dz);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     v[i] = 0.f;
@@ -1064,80 +1114,99 @@ k_project_dz_planes(DzArgs a, int lanes) {
   if (plane < a.n && threadIdx.x % lanes == 0) a.part[plane] = sum;
 }
 
-// Channels-first to lines of channels: a workgroup turns 64 channels by 64
-// positions of an image through LDS, a thread eight positions of a channel at
-// a time; pack: [position][ld], zeros behind O.  part: a group per 64
-// positions.  (A lane a position, two bytes a load, took 52 us at 64 images of
-// 1024 channels by 14 x 14, not 31.)
+// Up to three tensors brought into whole lines by one launch: planes of
+// positions turned into lines of channels, [position][ld], or (rows) lines of
+// hw elements, O of them, copied to lines of ld; zeros behind the elements.
+// Bound by memory: the backward of 64 images of 256 to 1024 channels at 14 x
+// 14 (z, dy, dz, their copies: 117 MB) takes 29 us, 4.0 TB/s; of three
+// launches 45.
+struct Lines {
+  DzArgs job[3];
+  int across[3];        // runs of kRun positions of an image
+  unsigned end[3];      // patches of the jobs up to this one
+  int jobs;
+};
+
+// A workgroup takes a patch of 64 channels by kRun positions of an image, a
+// thread eight positions of a channel (a lane a position, two bytes a load,
+// had taken 52 us, not 31, for the turn of dy); a patch that is turned goes
+// through LDS.  Runs of 32: of 64, the last one of 196 positions is nearly
+// empty (33 us for the above, not 29).  The patches of an XCD lie side by
+// side, so that the lines which two of them share meet in one L2 (with every
+// eighth patch 36 us, not 33).  part: a group per kRun positions.
+constexpr int kRun = 32;
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-k_project_turn(DzArgs a, int across) {
+k_project_lines(Lines t) {
   using E = Elem<T>;
   constexpr int kPitch = 64 + 4 / (int)sizeof(T);   // odd words: positions on different banks
-  __shared__ __attribute__((aligned(16))) T s[64 * kPitch];
-  const int64_t u = blockIdx.x;                     // image and run of positions
-  const int64_t b = u / across;
-  const int p0 = (int)(u % across) * 64, c0 = blockIdx.y * 64;
-  const int pc = threadIdx.x % 8 * 8, p = p0 + pc, n = min(8, a.hw - p);
+  constexpr int kLanes = kRun / 8, kDown = kThreads / kLanes, kPer = 64 / kDown;   // of a channel; channels at a time
+  __shared__ __attribute__((aligned(16))) T s[kRun * kPitch];
+  const unsigned each = (t.end[2] + 7) / 8;
+  for (unsigned i = blockIdx.x; i < 8 * each; i += gridDim.x) {
+    const unsigned v0 = (i & 7) * each + (i >> 3);
+    if (v0 >= t.end[2]) continue;
+    const int j = v0 >= t.end[1] ? 2 : v0 >= t.end[0] ? 1 : 0;
+    const DzArgs& a = t.job[j];
+    const unsigned first = v0 - (j ? t.end[j - 1] : 0), across = t.across[j], runs = (unsigned)a.n * across;
+    const unsigned u = first % runs, b = u / across;
+    const int p0 = (int)(u - b * across) * kRun, c0 = (int)(first / runs) * 64;
+    const int pc = threadIdx.x % kLanes * 8, p = p0 + pc, n = min(8, a.hw - p), cl = threadIdx.x / kLanes;
+    int64_t e[kPer];
+    bool there[kPer];
+    float v[kPer][8];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int cl = h * 32 + threadIdx.x / 8, c = c0 + cl;
-    float v[8] = {};
-    if (c < a.O && n > 0) dz8<T>(a, (b * a.O + c) * a.hw + p, n, v);
-    if (a.part) {
-      float t = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
-      if (pc == 0 && c < a.O) a.part[u * a.O + c] = t;
+    for (int h = 0; h < kPer; ++h) {
+      const int c = c0 + cl + h * kDown;
+      there[h] = c < a.O;
+      e[h] = ((int64_t)b * a.O + min(c, a.O - 1)) * a.hw + p;
     }
-    if (a.pack) {
+    if (n == 8) {
+      dz_whole<T, kPer>(a, e, there, v);
+    } else {
+#pragma unroll
+      for (int h = 0; h < kPer; ++h) dz8<T>(a, e[h], there[h] ? n : 0, v[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
+      const int c = c0 + cl + h * kDown;
+      if (a.part) {
+        float sum = ((v[h][0] + v[h][1]) + (v[h][2] + v[h][3])) + ((v[h][4] + v[h][5]) + (v[h][6] + v[h][7]));
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+        if (pc == 0 && there[h]) a.part[(int64_t)u * a.O + c] = sum;
+      }
+      if (!a.pack) continue;
       const float f = a.scale ? a.scale[min(c, a.O - 1)] : 1.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[(pc + i) * kPitch + cl] = E::from_f(v[i] * f);
+      for (int i = 0; i < 8; ++i) v[h][i] = there[h] ? v[h][i] * f : 0.f;
+      if (!a.rows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[(pc + i) * kPitch + c - c0] = E::from_f(v[h][i]);
+      } else if (there[h]) {
+        T* q = static_cast<T*>(a.pack) + ((int64_t)b * a.O + c) * a.ld + p;
+        if (p + 8 <= a.ld)
+          store8(q, v[h]);
+        else if (p < a.ld)   // float32: a line may end after four
+          store4(q, v[h]);
+      }
     }
-  }
-  if (!a.pack) return;
-  __syncthreads();
-  // a thread writes 16 bytes of a position's line at a time
-  constexpr int kVec = E::kVec, kLanes = 64 / kVec;
+    if (a.pack && !a.rows) {
+      __syncthreads();
+      // a thread writes 16 bytes of a position's line at a time
+      constexpr int kVec = E::kVec, kAcross = 64 / kVec;
 #pragma unroll
-  for (int i = threadIdx.x; i < 64 * kLanes; i += kThreads) {
-    const int row = i / kLanes, c = i % kLanes * kVec;
-    if (p0 + row >= a.hw || c0 + c >= a.ld) continue;
-    T w[kVec];
+      for (int i = threadIdx.x; i < kRun * kAcross; i += kThreads) {
+        const int row = i / kAcross, c = i % kAcross * kVec;
+        if (p0 + row >= a.hw || c0 + c >= a.ld) continue;
+        T w[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) w[j] = s[row * kPitch + c + j];
-    __builtin_memcpy(static_cast<T*>(a.pack) + (b * a.hw + p0 + row) * a.ld + c0 + c, w, 16);
+        for (int x = 0; x < kVec; ++x) w[x] = s[row * kPitch + c + x];
+        __builtin_memcpy(static_cast<T*>(a.pack) + ((int64_t)b * a.hw + p0 + row) * a.ld + c0 + c, w, 16);
+      }
+    }
+    if (i + gridDim.x < 8 * each) __syncthreads();
   }
-}
-
-// out[y][o] = sum over the y-th of gridDim.y runs of the groups' partial sums
-__global__ void __launch_bounds__(1024)
-k_project_dshift(const float* __restrict__ part, int64_t groups, int O, float* __restrict__ out) {
-  __shared__ float s[16][64];
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6, o = blockIdx.x * 64 + x;
-  const int64_t each = (groups + gridDim.y - 1) / gridDim.y, g0 = blockIdx.y * each, g1 = min(groups, g0 + each);
-  float t = 0.f;
-  if (o < O)
-#pragma unroll 8
-    for (int64_t i = g0 + y; i < g1; i += 16) t += part[i * O + o];
-  s[y][x] = t;
-  __syncthreads();
-  if (y == 0 && o < O) {
-    t = s[0][x];
-    for (int i = 1; i < 16; ++i) t += s[i][x];
-    out[(int64_t)blockIdx.y * O + o] = t;
-  }
-}
-
-// scale[o] weight[o][c] (scale may be nullptr), rounded to the weight's type, in lines of ld, zeros behind C
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-k_project_weight(const T* __restrict__ weight, const float* __restrict__ scale, int C, int ld, T* __restrict__ out) {
-  const int o = blockIdx.x;
-  const float s = scale ? scale[o] : 1.f;
-  for (int c = threadIdx.x; c < ld; c += kThreads)
-    out[(int64_t)o * ld + c] = c < C ? Elem<T>::from_f(s * Elem<T>::to_f(weight[(int64_t)o * C + c])) : (T)0;
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -1270,6 +1339,7 @@ hipError_t launch_whole(GemmArgs g, const Plan& p, float* part, hipStream_t st) 
 
 // ---- which operands are packed ---------------------------------------------------
 
+constexpr int64_t kMaxPatches = 1 << 23;   // workgroups of k_project_lines; they go on beyond
 constexpr int64_t kSpan = INT_MAX;   // bytes that a tile's offsets reach
 
 struct Sizes {
@@ -1306,47 +1376,49 @@ hipError_t pack_rows(const void* src, int64_t rows, int64_t channels, void* out,
                      dim3(kThreads), 0, st, a, tx);
   return hipGetLastError();
 }
+// The jobs of one launch; none is no launch.
 template <typename T>
-hipError_t launch_turn(const DzArgs& a, hipStream_t st) {
-  const int across = (int)ceil_div(a.hw, 64);
-  return image_slices(a.n, (int64_t)across * kThreads, 1, [&](int64_t b, int64_t n) {
-    DzArgs p = a;
-    const int64_t at = b * a.O * a.hw;
-    auto on = [&](const void* q) { return const_cast<T*>(static_cast<const T*>(q) + at); };
-    p.dy = on(a.dy);
-    if (a.z) p.z = on(a.z);
-    if (a.dz) p.dz = on(a.dz);
-    if (a.pack) p.pack = static_cast<T*>(a.pack) + b * a.hw * a.ld;
-    if (a.part) p.part = a.part + b * across * a.O;
-    hipLaunchKernelGGL(k_project_turn<T>, dim3((unsigned)(n * across), (unsigned)ceil_div(a.O, 64)), dim3(kThreads), 0,
-                       st, p, across);
+struct LinesLaunch {
+  Lines t{};
+  int64_t patches = 0;
+  void add(const DzArgs& a) {
+    t.job[t.jobs] = a;
+    t.across[t.jobs] = (int)ceil_div(std::max(a.hw, a.rows ? a.ld : 0), kRun);
+    patches += a.n * t.across[t.jobs] * ceil_div(a.O, 64);
+    for (int j = t.jobs++; j < 3; ++j) t.end[j] = (unsigned)patches;
+  }
+  // images of channels planes of hw positions into lines of channels, times scale (may be nullptr)
+  void turn(const void* src, int64_t images, int64_t channels, int64_t hw, const float* scale, void* out, int64_t ld) {
+    DzArgs a{};
+    a.dy = src, a.pack = out, a.scale = scale, a.O = (int)channels, a.hw = (int)hw, a.ld = (int)ld, a.n = images;
+    add(a);
+  }
+  // the weight as the products read it: packed into `out` where its lines are ragged or a scale goes into them
+  void weight(const Sizes& z, const void** w, const float* scale, void* out) {
+    if (!z.weight() && !scale) return;
+    DzArgs a{};
+    a.dy = *w, a.pack = out, a.scale = scale, a.O = (int)z.s.O, a.hw = (int)z.s.C, a.ld = (int)z.up(z.s.C);
+    a.n = 1, a.rows = 1;
+    add(a);
+    *w = out;
+  }
+  hipError_t launch(hipStream_t st) {
+    if (t.jobs == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_project_lines<T>, dim3((unsigned)std::min<int64_t>(ceil_div(patches, 8) * 8, kMaxPatches)), dim3(kThreads), 0,
+                       st, t);
     return hipGetLastError();
-  });
-}
-// Images of channels planes of hw positions into lines of channels, times scale (may be nullptr).
+  }
+};
+// x as the products read it: packed into `out` where its lines are ragged, by
+// a launch of its own (rows) or a job of `lines`.
 template <typename T>
-hipError_t turn(const void* src, int64_t images, int64_t channels, int64_t hw, const float* scale, void* out,
-                int64_t ld, hipStream_t st) {
-  DzArgs a{};
-  a.dy = src, a.pack = out, a.scale = scale, a.O = (int)channels, a.hw = (int)hw, a.ld = (int)ld, a.n = images;
-  return launch_turn<T>(a, st);
-}
-// x (or dy) as the products read it: packed into `out` where its lines are ragged.
-template <typename T>
-hipError_t pack_tensor(const Sizes& z, const void** t, int64_t channels, void* out, hipStream_t st) {
-  if (!z.rows(channels)) return hipSuccess;
-  const void* src = *t;
-  *t = out;
-  return z.nhwc ? pack_rows<T>(src, z.P(), channels, out, z.up(channels), st)
-                : turn<T>(src, z.s.B, channels, z.s.HW, nullptr, out, z.up(channels), st);
-}
-template <typename T>
-hipError_t pack_weight(const Sizes& z, const void** w, const float* scale, void* out, hipStream_t st) {
-  if (!z.weight() && !scale) return hipSuccess;
-  hipLaunchKernelGGL(k_project_weight<T>, dim3((unsigned)z.s.O), dim3(kThreads), 0, st, static_cast<const T*>(*w), scale,
-                     (int)z.s.C, (int)z.up(z.s.C), static_cast<T*>(out));
-  *w = out;
-  return hipGetLastError();
+hipError_t pack_x(const Sizes& z, const void** x, void* out, LinesLaunch<T>* lines, hipStream_t st) {
+  if (!z.rows(z.s.C)) return hipSuccess;
+  const void* src = *x;
+  *x = out;
+  if (z.nhwc) return pack_rows<T>(src, z.P(), z.s.C, out, z.up(z.s.C), st);
+  lines->turn(src, z.s.B, z.s.C, z.s.HW, nullptr, out, z.up(z.s.C));
+  return hipSuccess;
 }
 
 // Rows and columns of the output, of `channels` channels, as the products write it
@@ -1399,8 +1471,10 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
       hipLaunchKernelGGL((k_project_few<T, 2>), grid, block, 0, st, g);
     return hipGetLastError();
   }
-  hipError_t e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);
-  if (e == hipSuccess) e = pack_weight<T>(z, &w, nullptr, ws + l.weight, st);
+  LinesLaunch<T> lines;
+  lines.weight(z, &w, nullptr, ws + l.weight);
+  hipError_t e = pack_x(z, &x, ws + l.x, &lines, st);
+  if (e == hipSuccess) e = lines.launch(st);
   if (e != hipSuccess) return e;
   GemmArgs g{};
   output(&g, z, s.O);
@@ -1421,31 +1495,27 @@ hipError_t forward(const ProjectShape& s, const void* x, const void* w, const fl
   return launch_whole<T, true, false>(g, l.p, part, st);
 }
 
-// dshift from the groups' sums; many of them (small planes) by way of
-// kManyRuns runs behind them.
+// Many groups' sums (small planes) are added up in kManyRuns runs, behind
+// them, first.  Returns where the sums that make dshift lie, and how many.
 constexpr int kManyGroups = 4096, kManyRuns = 256;
-hipError_t sum_groups(float* part, int64_t groups, int64_t O, float* dshift, hipStream_t st) {
-  const dim3 grid((unsigned)ceil_div(O, 64)), block(1024);
-  if (groups > kManyGroups) {
-    float* runs = part + groups * O;
-    hipLaunchKernelGGL(k_project_dshift, dim3(grid.x, kManyRuns), block, 0, st, part, groups, (int)O, runs);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    part = runs, groups = kManyRuns;
-  }
-  hipLaunchKernelGGL(k_project_dshift, grid, block, 0, st, part, groups, (int)O, dshift);
+hipError_t fewer_groups(float** part, int64_t* groups, int64_t O, hipStream_t st) {
+  if (*groups <= kManyGroups) return hipSuccess;
+  float* runs = *part + *groups * O;
+  hipLaunchKernelGGL(k_project_dshift, dim3((unsigned)ceil_div(O, 16), kManyRuns), dim3(kThreads), 0, st, *part, *groups,
+                     (int)O, runs);
+  *part = runs, *groups = kManyRuns;
   return hipGetLastError();
 }
 
 // Groups of positions whose sums of dz lie apart: rows (channels-last) in up
-// to 1024 workgroups, images or 64 positions of them (channels-first).
+// to 1024 workgroups, images or kRun positions of them (channels-first).
 struct DzPlan {
   int tx;
   int64_t per, groups;
 };
 DzPlan dz_plan(const Sizes& z) {
   const ProjectShape& s = z.s;
-  if (!z.nhwc) return DzPlan{0, 0, z.planes() ? s.B * ceil_div(s.HW, 64) : s.B};
+  if (!z.nhwc) return DzPlan{0, 0, z.planes() ? s.B * ceil_div(s.HW, kRun) : s.B};
   int tx = 1;
   while (tx < 32 && tx * 8 < s.O) tx *= 2;
   const int64_t M = z.P(), across = ceil_div(s.O, tx * 8), down = kThreads / tx;
@@ -1518,6 +1588,10 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
   const bool products = gr.dx || gr.dweight || gr.dscale;
   const bool ragged = z.rows(s.O);
   const void* dz = dy;
+  const DzPlan dp = dz_plan(z);
+  float* sums = reinterpret_cast<float*>(ws + l.shift);   // of dz, by groups of positions
+  int64_t groups = dp.groups;
+  LinesLaunch<T> lines;
   hipError_t e = hipSuccess;
   {
     DzArgs a{};
@@ -1530,8 +1604,7 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
       if (!a.dz) a.dz = ws + l.dz;
       dz = a.dz;
     }
-    a.part = gr.dshift ? reinterpret_cast<float*>(ws + l.shift) : nullptr;
-    const DzPlan dp = dz_plan(z);
+    a.part = gr.dshift ? sums : nullptr;
     if (a.dz || a.pack || a.part) {
       if (z.nhwc) {
         a.n = z.P(), a.per = dp.per;
@@ -1540,7 +1613,7 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
         e = hipGetLastError();
       } else if (turned) {
         a.n = s.B;
-        e = launch_turn<T>(a, st);
+        lines.add(a);
       } else {
         int lanes = 1;
         while (lanes < 64 && lanes * 8 < s.HW) lanes *= 2;
@@ -1551,44 +1624,43 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
       }
       if (e != hipSuccess) return e;
     }
-    if (gr.dshift) {
-      e = sum_groups(a.part, dp.groups, s.O, gr.dshift, st);
-      if (e != hipSuccess) return e;
-    }
   }
+  // what else the products read in lines of their own
+  const bool dw = gr.dweight || gr.dscale;
+  const void* wp = w;
+  if (gr.dx && turned) {   // the weight turned too, so that both operands run along the outputs
+    lines.turn(w, 1, s.O, s.C, row_scale, ws + l.weight, z.up(s.O));
+    wp = ws + l.weight;
+  } else if (gr.dx) {
+    lines.weight(z, &wp, row_scale, ws + l.weight);
+  }
+  if (dw) e = pack_x(z, &x, ws + l.x, &lines, st);
+  if (e == hipSuccess) e = lines.launch(st);
+  if (e == hipSuccess && gr.dshift) e = fewer_groups(&sums, &groups, s.O, st);
+  if (e != hipSuccess) return e;
   float* part = reinterpret_cast<float*>(ws + l.part);
   const Operand dzo{dz, z.up(s.O), 0, 0}, dzp{dz, s.HW, s.O * s.HW, z.images()};   // lines of channels, of positions
   if (gr.dx) {
     GemmArgs g{};
     output(&g, z, s.C);
     g.K = (int)s.O, g.y = gr.dx;
+    const Operand wo{wp, z.up(turned ? s.O : s.C), 0, 0};
     if (turned) {
-      // the weight turned too, so that both operands run along the outputs
-      e = turn<T>(w, 1, s.O, s.C, row_scale, ws + l.weight, z.up(s.O), st);
-      if (e != hipSuccess) return e;
-      g.a = Operand{ws + l.weight, z.up(s.O), 0, 0}, g.b = dzo;
+      g.a = wo, g.b = dzo;
       e = launch_whole<T, true, true>(g, l.px, part, st);
+    } else if (z.nhwc) {
+      g.a = dzo, g.b = wo;
+      e = launch_whole<T, true, false>(g, l.px, part, st);
     } else {
-      const void* wp = w;
-      e = pack_weight<T>(z, &wp, row_scale, ws + l.weight, st);
-      if (e != hipSuccess) return e;
-      const Operand wo{wp, z.up(s.C), 0, 0};
-      if (z.nhwc) {
-        g.a = dzo, g.b = wo;
-        e = launch_whole<T, true, false>(g, l.px, part, st);
-      } else {
-        g.a = wo, g.b = dzp;
-        e = launch_whole<T, false, false>(g, l.px, part, st);
-      }
+      g.a = wo, g.b = dzp;
+      e = launch_whole<T, false, false>(g, l.px, part, st);
     }
     if (e != hipSuccess) return e;
   }
-  if (gr.dweight || gr.dscale) {
-    e = pack_tensor<T>(z, &x, s.C, ws + l.x, st);
-    if (e != hipSuccess) return e;
+  const bool join = dw && (row_scale || l.pw.splits > 1);
+  if (dw) {
     GemmArgs g{};
     g.R = (int)s.O, g.N = (int)s.C, g.K = (int)z.P(), g.ld = s.C, g.y = gr.dweight, g.klen = l.pw.klen;
-    const bool join = row_scale || l.pw.splits > 1;
     if (join) g.part = part;
     if (z.nhwc || turned) {
       g.a = dzo, g.b = Operand{x, z.up(s.C), 0, 0};
@@ -1598,15 +1670,18 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
       e = launch_product<T, true, true>(g, l.pw, st);
     }
     if (e != hipSuccess) return e;
-    if (join) {
-      int across = 32;
-      while (across < kThreads && across < s.C) across *= 2;
-      hipLaunchKernelGGL(k_project_dweight<T>, dim3((unsigned)s.O), dim3(kThreads), 0, st, part, l.pw.splits, (int)s.O,
-                         (int)s.C, row_scale, static_cast<const T*>(w), static_cast<T*>(gr.dweight), gr.dscale, across);
-      e = hipGetLastError();
-    }
   }
-  return e;
+  const unsigned shifts = gr.dshift ? (unsigned)ceil_div(s.O, 16) : 0;
+  if (join) {
+    int across = 32;
+    while (across < kThreads && across < s.C) across *= 2;
+    hipLaunchKernelGGL(k_project_dweight<T>, dim3((unsigned)s.O + shifts), dim3(kThreads), 0, st, part, l.pw.splits,
+                       (int)s.O, (int)s.C, row_scale, static_cast<const T*>(w), static_cast<T*>(gr.dweight), gr.dscale,
+                       across, sums, groups, gr.dshift);
+  } else if (shifts) {
+    hipLaunchKernelGGL(k_project_dshift, dim3(shifts), dim3(kThreads), 0, st, sums, groups, (int)s.O, gr.dshift);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
