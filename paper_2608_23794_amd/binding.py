@@ -11,9 +11,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
-
-import numpy as np
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmoce.so")
@@ -139,7 +138,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_project_backward_workspace_bytes.argtypes = [J]
     lib.moce_project_backward_workspace_bytes.restype = SZ
     lib.moce_project_backward.argtypes = [J, P, P, P, P, P, ctypes.POINTER(moce_project_grads), P, SZ, P]
-    # the list as an address: an array of moce_gradient, or memory laid out the same
+    # the list as an address, or bytes laid out as an array of moce_gradient
     lib.moce_gradient_workspace_bytes.argtypes = [P, I32]
     lib.moce_gradient_workspace_bytes.restype = SZ
     lib.moce_gradient_norm.argtypes = [P, I32, P, P, SZ, P]
@@ -354,29 +353,25 @@ def moce_project_backward(desc: moce_project_desc, x, weight, scale, z, dy, grad
                                                                  _ptr(ws), ws_bytes, _stream(stream)))
 
 
-def make_gradients(src, dst, sizes, dtypes) -> np.ndarray:
+def make_gradients(src, dst, sizes, dtypes) -> bytes:
     """The list of gradients for moce_gradient_norm and moce_gradient_clip (an array of moce_gradient) from lists of
     addresses, element counts and MOCE_F32 / MOCE_BF16."""
-    grads = np.empty((len(src), 4), np.int64)      # the last word: the type, then the reserved zero
-    grads[:, 0], grads[:, 1], grads[:, 2], grads[:, 3] = src, dst, sizes, dtypes
-    return grads
-
-
-def _list(grads: np.ndarray) -> int:
-    return grads.__array_interface__["data"][0]
+    words = [0] * (4 * len(src))
+    words[0::4], words[1::4], words[2::4], words[3::4] = src, dst, sizes, dtypes   # the type, then the reserved zero
+    return struct.pack(f"<{len(words)}q", *words)
 
 
 def moce_gradient_workspace_bytes(grads, count: int) -> int:
-    return load().moce_gradient_workspace_bytes(_list(grads), count)
+    return load().moce_gradient_workspace_bytes(grads, count)
 
 
 def moce_gradient_norm(grads, count: int, norm, ws, ws_bytes: int, stream=None) -> None:
-    _check("moce_gradient_norm", load().moce_gradient_norm(_list(grads), count, _ptr(norm), _ptr(ws), ws_bytes,
+    _check("moce_gradient_norm", load().moce_gradient_norm(grads, count, _ptr(norm), _ptr(ws), ws_bytes,
                                                            _stream(stream)))
 
 
 def moce_gradient_clip(grads, count: int, max_norm: float, norm, ws, ws_bytes: int, stream=None) -> None:
-    _check("moce_gradient_clip", load().moce_gradient_clip(_list(grads), count, max_norm, _ptr(norm), _ptr(ws),
+    _check("moce_gradient_clip", load().moce_gradient_clip(grads, count, max_norm, _ptr(norm), _ptr(ws),
                                                            ws_bytes, _stream(stream)))
 
 
