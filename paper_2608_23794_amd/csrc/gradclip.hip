@@ -8,6 +8,11 @@
 // as it is.  Work is cut into chunks of one tensor each; a workgroup sums a
 // chunk in float64 (a square of a float32 is exact there, and neither
 // overflows nor vanishes) and the chunks' sums are added in a fixed order.
+//
+// 1.2 GB of bfloat16 gradients: 238 us for the norm (5.0 TB/s), 436 for the
+// scaling (2.4 GB, 5.5 TB/s; some of it from the infinity cache).  A few small
+// tensors are bound by two launches, 4 us each, and a list of hundreds by the
+// host that gathers it: 161 tensors of 102 MB take the GPU 38 us, the call 98.
 #include <algorithm>
 
 #include "moce_internal.h"
@@ -22,7 +27,7 @@ constexpr int kList = 128;                       // tensors a launch: 3.6 KB of 
 // of float32, and more where kMaxChunks would not do.
 constexpr int64_t kWantChunks = 2048, kMinChunk = 2048, kMaxChunk = 32768, kMaxChunks = 65536;
 // Chunks whose sums every workgroup of the scaling adds up by itself, which
-// saves the launch between (clip_gradients of a layer's four: 16 us, not 20).
+// saves the launch between (clip_gradients of a layer's four: 17 us, not 21).
 constexpr int kFewChunks = 4096;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
