@@ -999,10 +999,12 @@ struct DzArgs {
   int64_t per;            // rows of one group
 };
 
-// act'(z) dy of N times eight neighbouring elements, at e[.] where there[.],
-// stored to dz: all loads before the first store.
+// act'(z) dy of N times n neighbouring elements (up to eight; zeros behind
+// them), at e[.] where there[.], stored to dz: all loads before the first
+// store.  Eight are read: what lies behind a line is the next one.
 template <typename T, int N>
-__device__ __forceinline__ void dz_whole(const DzArgs& a, const int64_t (&e)[N], const bool (&there)[N], float (&v)[N][8]) {
+__device__ __forceinline__ void dz_whole(const DzArgs& a, const int64_t (&e)[N], const bool (&there)[N], int n,
+                                         float (&v)[N][8]) {
   const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
   T* dz = static_cast<T*>(a.dz);
   float q[N][8];
@@ -1021,19 +1023,35 @@ __device__ __forceinline__ void dz_whole(const DzArgs& a, const int64_t (&e)[N],
     if (a.act == MOCE_ACT_GELU) all(MOCE_ACT_GELU);
     if (a.act == MOCE_ACT_SILU) all(MOCE_ACT_SILU);
   }
-  if (dz)
+  if (n < 8) {
 #pragma unroll
     for (int u = 0; u < N; ++u)
-      if (there[u]) store8(dz + e[u], v[u]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u][i] = i < n ? v[u][i] : 0.f;
+  }
+  if (!dz) return;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    if (!there[u]) continue;
+    if (n == 8) {
+      store8(dz + e[u], v[u]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) dz[e[u] + i] = Elem<T>::from_f(v[u][i]);
+    }
+  }
 }
-// The same of the n elements at e (up to eight), zeros behind them.
+// The same of n elements at e, of a tensor of `total`.  (Its last ones go one
+// by one; where every line's did, each took longer than all before it: 35972
+// rows of 541, z, dy and a copy: 68 us, not 33.)
 template <typename T>
-__device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, float (&v)[8]) {
+__device__ __forceinline__ void dz8(const DzArgs& a, int64_t e, int n, int64_t total, float (&v)[8]) {
   using E = Elem<T>;
-  if (n == 8) {
+  if (n > 0 && e + 8 <= total) {
     const int64_t at[1] = {e};
     const bool there[1] = {true};
-    dz_whole<T, 1>(a, at, there, reinterpret_cast<float(&)[1][8]>(v));
+    dz_whole<T, 1>(a, at, there, n, reinterpret_cast<float(&)[1][8]>(v));
     return;
   }
   const T *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(a.dy);
@@ -1061,11 +1079,11 @@ k_project_dz_rows(DzArgs a, int tx) {
   float sum[8] = {}, sc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sc[i] = a.pack && a.scale ? a.scale[min(c + i, a.O - 1)] : 1.f;
-  if (n > 0) {
+  if (n > 0 && (int)threadIdx.x < down * tx) {
     const int64_t end = min(a.n, (blockIdx.x + (int64_t)1) * a.per);
     for (int64_t r = blockIdx.x * a.per + threadIdx.x / tx; r < end; r += down) {
       float v[8];
-      dz8<T>(a, r * a.O + c, n, v);
+      dz8<T>(a, r * a.O + c, n, a.n * a.O, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += v[i];
       if (a.pack) {
@@ -1108,7 +1126,7 @@ k_project_dz_planes(DzArgs a, int lanes) {
       float v[8];
       const int64_t e = plane * a.hw + p;
       const int n = min(8, a.hw - p);
-      dz8<T>(a, e, n, v);
+      dz8<T>(a, e, n, a.n * a.hw, v);
       sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
       if (a.pack) {
         T* q = static_cast<T*>(a.pack) + e;
@@ -1176,11 +1194,12 @@ k_project_lines(Lines t) {
       there[h] = c < a.O;
       e[h] = ((int64_t)b * a.O + min(c, a.O - 1)) * a.hw + p;
     }
-    if (n == 8) {
-      dz_whole<T, kPer>(a, e, there, v);
+    const int64_t total = a.n * a.O * a.hw;
+    if (n > 0 && e[kPer - 1] + 8 <= total) {
+      dz_whole<T, kPer>(a, e, there, min(n, 8), v);
     } else {
 #pragma unroll
-      for (int h = 0; h < kPer; ++h) dz8<T>(a, e[h], there[h] ? n : 0, v[h]);
+      for (int h = 0; h < kPer; ++h) dz8<T>(a, e[h], there[h] ? n : 0, total, v[h]);
     }
 #pragma unroll
     for (int h = 0; h < kPer; ++h) {
@@ -1380,13 +1399,26 @@ struct Sizes {
   int images() const { return !nhwc && s.B > 1 ? (int)s.HW : 0; }
 };
 
+// Threads across a row of k_project_dz_rows: of the ways to share its chunks
+// out evenly, the first that leaves no more than a
+// twentieth of the threads idle (35972 rows of 544, z, dy and dz: 31 us, not 36
+// with 32 across).
+int row_lanes(int64_t channels) {
+  const int64_t chunks = ceil_div(channels, 8);
+  int best = 1, most = 0;
+  for (int64_t parts = ceil_div(chunks, 128); parts <= ceil_div(chunks, 8); ++parts) {
+    const int tx = (int)ceil_div(chunks, parts), used = (int)(chunks * (kThreads / tx) * 256 / (parts * kThreads));
+    if (used > most) best = tx, most = used;
+    if (used >= 243) break;
+  }
+  return best;
+}
 template <typename T>
 hipError_t pack_rows(const void* src, int64_t rows, int64_t channels, void* out, int64_t ld, hipStream_t st) {
   DzArgs a{};
   a.dy = src, a.pack = out, a.O = (int)channels, a.ld = (int)ld, a.n = rows;
-  int tx = 1;
-  while (tx < 32 && tx * 8 < channels) tx *= 2;
-  a.per = ceil_div(ceil_div(rows, 2048), kThreads / tx) * (kThreads / tx);
+  const int tx = row_lanes(channels), down = kThreads / tx;
+  a.per = ceil_div(ceil_div(rows, 2048), down) * down;
   hipLaunchKernelGGL(k_project_dz_rows<T>, dim3((unsigned)ceil_div(rows, a.per), (unsigned)ceil_div(channels, tx * 8)),
                      dim3(kThreads), 0, st, a, tx);
   return hipGetLastError();
@@ -1531,8 +1563,7 @@ struct DzPlan {
 DzPlan dz_plan(const Sizes& z) {
   const ProjectShape& s = z.s;
   if (!z.nhwc) return DzPlan{0, 0, z.planes() ? s.B * ceil_div(s.HW, kRun) : s.B};
-  int tx = 1;
-  while (tx < 32 && tx * 8 < s.O) tx *= 2;
+  const int tx = row_lanes(s.O);
   const int64_t M = z.P(), across = ceil_div(s.O, tx * 8), down = kThreads / tx;
   const int64_t want = std::max<int64_t>(1, 1024 / across);
   const int64_t per = ceil_div(ceil_div(M, want), down) * down;
