@@ -1475,8 +1475,9 @@ void output(GemmArgs* g, const Sizes& z, int64_t channels) {
   g->ld = z.nhwc ? channels : z.s.HW, g->hw = z.images(), g->img = channels * z.s.HW;
 }
 
-// Whether a tensor of so many channels has rows that the epilogue writes in pieces.
-bool ragged_rows(const Sizes& z, int64_t channels) { return (z.nhwc ? channels : z.s.HW) % 8 != 0; }
+// Whether a tensor of so many channels has rows that are not whole 16 bytes,
+// which the epilogue writes in pieces.
+bool ragged_rows(const Sizes& z, int64_t channels) { return (z.nhwc ? channels : z.s.HW) % z.vec != 0; }
 
 constexpr int kFewRows = 32;   // beyond, 64 x 64 tiles in splits are as fast (64 positions of 4096 x 4096: 17 us, not 25)
 bool few_rows(const Sizes& z) { return z.nhwc && z.P() <= kFewRows; }
@@ -1566,7 +1567,8 @@ DzPlan dz_plan(const Sizes& z) {
   const int tx = row_lanes(s.O);
   const int64_t M = z.P(), across = ceil_div(s.O, tx * 8), down = kThreads / tx;
   const int64_t want = std::max<int64_t>(1, 1024 / across);
-  const int64_t per = ceil_div(ceil_div(M, want), down) * down;
+  // few rows are one group's, whose sums are dshift
+  const int64_t per = M <= 4 * down ? M : ceil_div(ceil_div(M, want), down) * down;
   return DzPlan{tx, per, ceil_div(M, per)};
 }
 
@@ -1601,7 +1603,7 @@ BwdLayout bwd_layout(const ProjectShape& s) {
   GemmArgs g{};
   output(&g, z, s.C);
   l.px = plan(g.R, g.N, s.O, s.elem, ragged_rows(z, s.C), false);
-  l.pw = plan(s.O, s.C, z.P(), s.elem, s.C % 8 != 0, z.nhwc || z.planes());
+  l.pw = plan(s.O, s.C, z.P(), s.elem, s.C % z.vec != 0, z.nhwc || z.planes());
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -1650,7 +1652,7 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
       if (!a.dz) a.dz = ws + l.dz;
       dz = a.dz;
     }
-    a.part = gr.dshift ? sums : nullptr;
+    a.part = !gr.dshift ? nullptr : groups == 1 ? gr.dshift : sums;
     if (a.dz || a.pack || a.part) {
       if (z.nhwc) {
         a.n = z.P(), a.per = dp.per;
@@ -1682,7 +1684,8 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
   }
   if (dw) e = pack_x(z, &x, ws + l.x, &lines, st);
   if (e == hipSuccess) e = lines.launch(st);
-  if (e == hipSuccess && gr.dshift) e = fewer_groups(&sums, &groups, s.O, st);
+  const bool shift = gr.dshift && groups > 1;   // to be summed
+  if (e == hipSuccess && shift) e = fewer_groups(&sums, &groups, s.O, st);
   if (e != hipSuccess) return e;
   float* part = reinterpret_cast<float*>(ws + l.part);
   const Operand dzo{dz, z.up(s.O), 0, 0}, dzp{dz, s.HW, s.O * s.HW, z.images()};   // lines of channels, of positions
@@ -1717,7 +1720,7 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
     }
     if (e != hipSuccess) return e;
   }
-  const unsigned shifts = gr.dshift ? (unsigned)ceil_div(s.O, 16) : 0;
+  const unsigned shifts = shift ? (unsigned)ceil_div(s.O, 16) : 0;
   if (join) {
     int across = 32;
     while (across < kThreads && across < s.C) across *= 2;
