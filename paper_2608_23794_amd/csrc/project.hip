@@ -644,10 +644,10 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // WR x WC waves of FR x FC fragments, D stages in LDS.
 //
 // Bound by the matrix cores where the contraction is long (16384 positions of
-// 4096 by 4096: 423 us, 1300 TFLOP/s, of the 1421 that a large product of the
+// 4096 by 4096: 418 us, 1315 TFLOP/s, of the 1421 that a large product of the
 // library reaches here), by memory where it is short (64 to 256 channels over
 // 64 images of 56 x 56 with their residual: 50 us, 4.6 TB/s).  Between (50432
-// positions of 768 by 768, GELU, z written too: 84 us, for 46 of memory and 42
+// positions of 768 by 768, GELU, z written too: 82 us, for 46 of memory and 42
 // of products) the two do not overlap: a workgroup's results leave while only
 // its neighbours on the CU multiply.  Tried and slower there: a wave of its
 // own that only copies, stages ahead of the product's end (persistent
@@ -1151,7 +1151,7 @@ k_project_dz_planes(DzArgs a, int lanes) {
 // positions turned into lines of channels, [position][ld], or (rows) lines of
 // hw elements, O of them, copied to lines of ld; zeros behind the elements.
 // Bound by memory: the backward of 64 images of 256 to 1024 channels at 14 x
-// 14 (z, dy, dz, their copies: 117 MB) takes 29 us, 4.0 TB/s; of three
+// 14 (z, dy, dz, their copies: 117 MB) takes 26 us, 4.5 TB/s; of three
 // launches 45.
 struct Lines {
   DzArgs job[3];
