@@ -257,6 +257,27 @@ def test_values_that_are_not_finite_stay_at_their_position(dtype, layout):
     assert all(torch.isfinite(v.float()).all() for v in out.values())
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(3, 21, 13, 40, 1, "nhwc"), (3, 21, 541, 40, 1, "nhwc"), (2, 21, 13, 7, 7, "nchw"),
+                                  (3, 13, 70, 5, 7, "nchw"), (1, 5, 3, 1, 2, "nhwc")], ids=str)
+def test_lines_of_any_length_end_where_they_end(size, dtype, act):
+    """Upstream values that are not finite at the first element of a line leave the line before it alone."""
+    B, C, O, H, W, layout = size
+    t = make(B, C, O, H, W, dtype, layout, act, shift=True)
+    clean = t["layer"].backward(t["x"], t["dy"], z=t["z"], residual=True)
+    dy, z = t["dy"].clone(), t["z"].clone()
+    z[B - 1] = 1.0      # open for every activation
+    want = t["layer"].backward(t["x"], dy, z=z, residual=True)
+    dy[B - 1] = float("nan")
+    got = t["layer"].backward(t["x"], dy, z=z, residual=True)
+    for name in ("dx", "dresidual"):
+        if B > 1:
+            assert torch.equal(got[name][:B - 1], clean[name][:B - 1]), name
+        assert torch.isnan(got[name][B - 1]).all() and torch.isfinite(want[name].float()).all(), name
+    assert torch.isnan(got["dshift"]).all() and torch.isnan(got["dweight"]).all()
+
+
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_activations_over_their_range(dtype, act):
