@@ -466,3 +466,25 @@ def test_float32_values_that_are_not_finite():
     fine = rest[:, None] & torch.isfinite(want)
     mag = x.cpu().abs().nan_to_num(0.0, 0.0, 0.0).double() @ w.cpu().abs().double().t()
     assert ((got.double() - want.double()).abs()[fine] <= (80 * STEP32 * mag + 1e-30)[fine]).all()
+
+
+def test_gelu_relative_to_its_value():
+    """bfloat16 GELU and its slope at every bfloat16 argument down to where the values leave the normal numbers: half a
+    step of the value and 2^-12 of it for the evaluation (the slope, which passes through zero, 3e-7 beside that)."""
+    bits = torch.arange(1 << 15, dtype=torch.int32)
+    v = (bits << 16).view(torch.float32)
+    v = v[(v >= 2.0 ** -60) & (v <= 12.9)]
+    v = torch.cat([-v, v])
+    v = v[: v.numel() // 8 * 8].cuda().bfloat16()
+    want = act64(v.double(), "gelu")
+    tol = (HALF["bf16"] * 1.01 + 2.0 ** -12) * want.abs() + 2.0 ** -122
+    one = ProjectLayer(torch.ones(1, 1, dtype=v.dtype, device="cuda"), act="gelu")
+    eye = ProjectLayer(torch.eye(8, dtype=v.dtype, device="cuda"), act="gelu")
+    check("tiles", eye.forward(v.view(-1, 8)).view(-1), want, tol)
+    check("elements", one.forward(v.view(-1, 1)).view(-1), want, tol)
+    few = v.view(-1, 8)[:: v.numel() // 8 // 30][:30].contiguous()
+    w = act64(few.double(), "gelu")
+    check("few rows", eye.forward(few), w, (HALF["bf16"] * 1.01 + 2.0 ** -12) * w.abs() + 2.0 ** -122)
+    slope = eye.backward(v.view(-1, 8), torch.ones_like(v).view(-1, 8), z=v.view(-1, 8), residual=True)["dresidual"]
+    w = act_grad64(v.double(), "gelu")
+    check("slope", slope.view(-1), w, (HALF["bf16"] * 1.01 + 2.0 ** -12) * w.abs() + 3e-7)
