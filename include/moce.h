@@ -414,7 +414,8 @@ moce_status moce_project(const moce_project_desc* desc, const void* x, const voi
 typedef struct moce_project_grads {
     void* dx;             /* layout and type of x */
     void* dweight;        /* [O][C], type of weight */
-    float* dscale;        /* [O]; needs scale; only for MOCE_ACT_NONE and MOCE_ACT_RELU */
+    float* dscale;        /* [O]; needs scale; MOCE_ACT_NONE and MOCE_ACT_RELU (the others: with
+                           * dresidual of one call as dy of another with MOCE_ACT_NONE) */
     float* dshift;        /* [O] */
     void* dresidual;      /* layout and type of y */
 } moce_project_grads;

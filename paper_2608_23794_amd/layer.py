@@ -372,8 +372,9 @@ class ProjectLayer:
 
     def backward(self, x: torch.Tensor, dy: torch.Tensor, z: Optional[torch.Tensor] = None, residual: bool = False,
                  dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> dict:
-        """moce_project_backward: dx, dweight, dscale and dshift where the layer has them (no dscale with "gelu"
-        and "silu"), and with residual=True dresidual."""
+        """moce_project_backward: dx, dweight, dscale and dshift where the layer has them, and with residual=True
+        dresidual.  The scale of a "gelu" or "silu" layer takes a second call over the dz of the first: dweight and
+        dscale then come from sums over dz as it is, not scaled before its rounding."""
         desc, shape = self.desc(x.shape), self.y_shape(x.shape)
         f32, dev = torch.float32, self.device
         _need("x", x, x.shape, self.dtype, dev)
@@ -386,7 +387,7 @@ class ProjectLayer:
             dx = torch.empty_like(x)
         _need("dx", dx, x.shape, self.dtype, dev)
         out = {"dx": dx, "dweight": torch.empty_like(self.weight)}
-        if self.scale is not None and self.act in ("none", "relu"):
+        if self.scale is not None:
             out["dscale"] = torch.empty(self.O, dtype=f32, device=dev)
         if self.shift is not None:
             out["dshift"] = torch.empty(self.O, dtype=f32, device=dev)
@@ -398,8 +399,18 @@ class ProjectLayer:
             return out
         with _on(dev):
             ws, n = self._workspace(mb.moce_project_backward_workspace_bytes(desc), ws)
-            mb.moce_project_backward(desc, x, self.weight, self.scale, z, dy, mb.make_project_grads(**out), ws, n,
-                                     _raw_stream(dev.index))
+            stream, first = _raw_stream(dev.index), out
+            two = self.scale is not None and self.act in ("gelu", "silu")
+            if two:
+                first = {k: v for k, v in out.items() if k not in ("dweight", "dscale")}
+                first["dresidual"] = dz = out["dresidual"] if residual else torch.empty_like(dy)
+            mb.moce_project_backward(desc, x, self.weight, self.scale, z, dy, mb.make_project_grads(**first), ws, n,
+                                     stream)
+            if two:
+                desc.act = mb.MOCE_ACT_NONE    # needs no more workspace than the activation
+                mb.moce_project_backward(desc, x, self.weight, self.scale, None, dz,
+                                         mb.make_project_grads(dweight=out["dweight"], dscale=out["dscale"]), ws, n,
+                                         stream)
         return out
 
 

@@ -488,3 +488,51 @@ def test_gelu_relative_to_its_value():
     slope = eye.backward(v.view(-1, 8), torch.ones_like(v).view(-1, 8), z=v.view(-1, 8), residual=True)["dresidual"]
     w = act_grad64(v.double(), "gelu")
     check("slope", slope.view(-1), w, (HALF["bf16"] * 1.01 + 2.0 ** -12) * w.abs() + 3e-7)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 8, 8, 1, 1, "nhwc"), (2, 65, 63, 33, 1, "nhwc"), (4, 128, 256, 16, 9, "nhwc"),
+                                  (3, 33, 31, 7, 7, "nchw"), (5, 72, 40, 8, 8, "nchw"), (1, 7, 300, 130, 1, "nhwc")], ids=str)
+def test_the_scale_of_a_smooth_activation_has_its_gradient(size, dtype, act):
+    B, C, O, H, W, layout = size
+    t = make(B, C, O, H, W, dtype, layout, act, scale=True, shift=True, seed=3)
+    layer = t["layer"]
+    out = layer.backward(t["x"], t["dy"], z=t["z"], residual=True)
+    assert set(out) == {"dx", "dweight", "dscale", "dshift", "dresidual"}
+    check_backward(t, dtype, layout, act, out)
+    # the same bits without dresidual, in a workspace of the size that the layer gives, and captured
+    ws = torch.empty(layer.backward_workspace_bytes(t["x"].shape), dtype=torch.uint8, device="cuda")
+    again = layer.backward(t["x"], t["dy"], z=t["z"], ws=ws)
+    assert set(again) == {"dx", "dweight", "dscale", "dshift"}
+    assert all(torch.equal(again[n], out[n]) for n in again)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = layer.backward(t["x"], t["dy"], z=t["z"], ws=ws)
+    for f in (1.0, -0.5, 2.0):
+        t["dy"].mul_(f)
+        want = layer.backward(t["x"], t["dy"], z=t["z"])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(held[n], want[n]) for n in want)
+
+
+def test_the_scale_of_a_smooth_activation_against_differences():
+    t = make(2, 12, 10, 3, 4, "f32", "nchw", "gelu", scale=True, shift=True)
+
+    def loss(scale):
+        y = ProjectLayer(t["w"], scale, t["shift"], act="gelu", layout="nchw").forward(t["x"])
+        return float((y.double() * t["dy"].double()).sum())
+
+    z = torch.empty_like(t["dy"])
+    t["layer"].forward(t["x"], z=z)
+    got = t["layer"].backward(t["x"], t["dy"], z=z)["dscale"]
+    h = 2.0 ** -6      # as above: off by h^2 / 6 of a third derivative and by roundings over h
+    for i in range(10):
+        a, b = t["scale"].clone(), t["scale"].clone()
+        a[i] += h
+        b[i] -= h
+        d = (loss(a) - loss(b)) / (2 * h)
+        assert abs(d - float(got[i])) <= 2e-3 * max(1.0, float(got.abs().max())), i
