@@ -314,6 +314,8 @@ class ProjectLayer:
         if weight.dim() != 2 or weight.dtype not in _DTYPE_OF or not weight.is_cuda:
             raise ValueError(f"weight has to be a float32 or bfloat16 [O, C] tensor on the GPU, got {weight.dtype} "
                              f"{tuple(weight.shape)} on {weight.device}")
+        if weight.numel() == 0:
+            raise ValueError(f"weight has to have outputs and channels, got {tuple(weight.shape)}")
         self.O, self.C = weight.shape
         self.dtype, self.device = weight.dtype, weight.device
         _need("weight", weight, weight.shape, self.dtype, self.device)

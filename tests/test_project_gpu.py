@@ -536,3 +536,10 @@ def test_the_scale_of_a_smooth_activation_against_differences():
         b[i] -= h
         d = (loss(a) - loss(b)) / (2 * h)
         assert abs(d - float(got[i])) <= 2e-3 * max(1.0, float(got.abs().max())), i
+
+
+@pytest.mark.parametrize("O,C", [(4, 0), (0, 4), (0, 0)])
+def test_a_weight_without_channels_is_refused(O, C):
+    """A sum over no channels is none that the kernels form: the call would have to return act(shift + residual)."""
+    with pytest.raises(ValueError):
+        ProjectLayer(torch.empty(O, C, device="cuda"))
