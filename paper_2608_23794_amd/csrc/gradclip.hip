@@ -143,15 +143,27 @@ __device__ __forceinline__ double norm_of_parts(const double* __restrict__ part,
   for (int w = 1; w < NT / kWave; ++w) a += s[w];
   return sqrt(a);
 }
-__device__ __forceinline__ float coefficient(double norm, float max_norm) {
-  return norm > (double)max_norm && __builtin_isfinite((float)norm) ? (float)((double)max_norm / norm) : 1.f;
+// 1 or max_norm / norm, as two factors to be multiplied one after the other: a
+// quotient below the normal float32 numbers would have lost bits, or be zero,
+// where a gradient near the largest ones times it is an ordinary number.  The
+// first is below 1 there, so that its product cannot overflow; what that makes
+// subnormal the second, 2^-126, makes zero.  One more multiplication a value,
+// which the memory hides.
+struct Coef {
+  float first, second;
+  __device__ __forceinline__ float times(float v) const { return v * first * second; }
+};
+__device__ __forceinline__ Coef coefficient(double norm, float max_norm) {
+  if (!(norm > (double)max_norm && __builtin_isfinite((float)norm))) return {1.f, 1.f};
+  const double c = (double)max_norm / norm;
+  return c < 0x1p-126 ? Coef{(float)(c * 0x1p126), 0x1p-126f} : Coef{(float)c, 1.f};
 }
 
-// The norm, and the coefficient 1 or max_norm / norm (coef may be nullptr).
+// The norm, and the coefficient (coef may be nullptr).
 template <int NT>
 __global__ void __launch_bounds__(NT)
 k_gradient_norm(const double* __restrict__ part, int chunks, float max_norm, float* __restrict__ norm,
-                float* __restrict__ coef) {
+                Coef* __restrict__ coef) {
   const double a = norm_of_parts<NT>(part, chunks);
   if (threadIdx.x != 0) return;
   *norm = (float)a;
@@ -163,8 +175,8 @@ k_gradient_norm(const double* __restrict__ part, int chunks, float max_norm, flo
 template <bool FEW>
 __global__ void __launch_bounds__(kThreads)
 k_gradient_scale(List l, int64_t chunk, const double* __restrict__ part, int chunks, float max_norm,
-                 float* __restrict__ norm, const float* __restrict__ coef) {
-  float c;
+                 float* __restrict__ norm, const Coef* __restrict__ coef) {
+  Coef c;
   if constexpr (FEW) {
     const double a = norm_of_parts<kThreads>(part, chunks);
     if (l.base + (int)blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)a;
@@ -173,23 +185,23 @@ k_gradient_scale(List l, int64_t chunk, const double* __restrict__ part, int chu
     c = *coef;
   }
   const Part r = part_of(l, gridDim.x - 1 - blockIdx.x, chunk);
-  if (c == 1.f && l.src[r.t] == l.dst[r.t]) return;
+  if (c.first == 1.f && l.src[r.t] == l.dst[r.t]) return;
   if (r.bf16) {
     const uint16_t* p = static_cast<const uint16_t*>(l.src[r.t]);
     uint16_t* d = static_cast<uint16_t*>(l.dst[r.t]);
     each_vector(p, r, [&](int64_t i, u32x4 v) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = pack_bf16x2(bf16_lo(v[e]) * c, bf16_hi(v[e]) * c);
+      for (int e = 0; e < 4; ++e) v[e] = pack_bf16x2(c.times(bf16_lo(v[e])), c.times(bf16_hi(v[e])));
       __builtin_memcpy(d + i, &v, 16);
-    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = f32_to_bf16(bf16_to_f32(p[i]) * c); });
+    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = f32_to_bf16(c.times(bf16_to_f32(p[i]))); });
   } else {
     const float* p = static_cast<const float*>(l.src[r.t]);
     float* d = static_cast<float*>(l.dst[r.t]);
     each_vector(p, r, [&](int64_t i, u32x4 v) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * c);
+      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(c.times(__uint_as_float(v[e])));
       __builtin_memcpy(d + i, &v, 16);
-    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = p[i] * c; });
+    }, [&](int64_t i) __attribute__((always_inline)) { d[i] = c.times(p[i]); });
   }
 }
 
@@ -236,10 +248,10 @@ constexpr size_t kPartAt = 256;   // the workspace: the coefficient, then the ch
 struct Work {
   int64_t chunk;
   int chunks;
-  float* coef;
+  Coef* coef;
   double* part;
   Work(const moce_gradient* g, int count, void* ws)
-      : chunk(chunk_size(g, count)), chunks((int)chunk_count(g, count, chunk)), coef(static_cast<float*>(ws)),
+      : chunk(chunk_size(g, count)), chunks((int)chunk_count(g, count, chunk)), coef(static_cast<Coef*>(ws)),
         part(reinterpret_cast<double*>(static_cast<char*>(ws) + kPartAt)) {}
 };
 
@@ -249,7 +261,7 @@ hipError_t squares(const moce_gradient* g, int count, const Work& w, hipStream_t
     return hipGetLastError();
   });
 }
-hipError_t norm_of(const Work& w, float max_norm, float* norm, float* coef, hipStream_t st) {
+hipError_t norm_of(const Work& w, float max_norm, float* norm, Coef* coef, hipStream_t st) {
   if (w.chunks <= kFewChunks)   // the order of the sum in k_gradient_scale<true>
     hipLaunchKernelGGL(k_gradient_norm<kThreads>, dim3(1), dim3(kThreads), 0, st, w.part, w.chunks, max_norm, norm,
                        coef);

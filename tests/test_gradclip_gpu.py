@@ -194,3 +194,23 @@ def test_training_step_of_the_layers_together(layout):
     dW = scale.double()[:, None] * G
     tol = 2.0 ** -8 * 1.01 * dW.abs() + scale.double()[:, None] * (hr.shape[0] + 8) * 2.0 ** -24 * Gm
     assert ((before[0].double() - dW).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("count", [3, 4200])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-12, 1e-30])
+def test_a_coefficient_below_the_normal_numbers(max_norm, count):
+    """Gradients near the largest float32: max_norm / norm has fewer bits as a float32, or is none, the products have all
+    of theirs.  Few chunks, and more than one workgroup adds up by itself."""
+    ts = normals([500, 501] + [1] * (count - 2), [F, H] + [F, H] * (count // 2 - 1) + [F] * (count % 2), scale=3e36)
+    want = norm64(ts)
+    assert 1e37 < want < 3.4e38
+    outs = [torch.empty_like(t) for t in ts]
+    norm = clip_gradients(ts, max_norm, out=outs)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    coef = max_norm / want
+    for t, o in zip(ts[:40], outs[:40]):
+        half = 2.0 ** -24 if t.dtype == F else 2.0 ** -8
+        exact = t.double() * coef
+        assert ((o.double() - exact).abs() <= (2.0 ** -22 + half) * exact.abs() + 2.0 ** -133).all()
+    clip_gradients(ts, max_norm)
+    assert all(torch.equal(t, o) for t, o in zip(ts, outs))
