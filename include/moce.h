@@ -461,8 +461,9 @@ size_t moce_gradient_workspace_bytes(const moce_gradient* grads, int32_t count);
  * list is host memory, read before the call returns; count == 0 gives 0.  The
  * order of the sum depends on the sizes alone: the same gradients give the
  * same bits.  Errors: MOCE_ERR_NULL (norm, the list, a tensor's src with
- * n > 0), MOCE_ERR_SHAPE (count < 0, n < 0), MOCE_ERR_DTYPE, MOCE_ERR_ALIGN,
- * MOCE_ERR_WORKSPACE; MOCE_ERR_UNSUPPORTED when the sizes sum to over 2^40.
+ * n > 0), MOCE_ERR_SHAPE (count < 0, n < 0, norm or ws over a tensor or each
+ * other), MOCE_ERR_DTYPE, MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE;
+ * MOCE_ERR_UNSUPPORTED when the sizes sum to over 2^40.
  * Asynchronous on `stream`. */
 moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float* norm, void* ws, size_t ws_bytes,
                                hipStream_t stream);
@@ -475,8 +476,7 @@ moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float*
  * Errors: those of moce_gradient_norm; MOCE_ERR_NULL for a missing dst;
  * MOCE_ERR_SHAPE when max_norm is negative or not finite, when two tensors
  * overlap (a tensor listed twice would be scaled twice), when a dst overlaps
- * any src but its own, or its own partly, or when norm or ws overlaps a
- * tensor. */
+ * any src but its own, or its own partly, or when norm or ws overlaps a dst. */
 moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float max_norm, float* norm, void* ws,
                                size_t ws_bytes, hipStream_t stream);
 

@@ -738,6 +738,18 @@ moce_status check_gradient_ws(const moce_gradient* g, int32_t count, const float
   return MOCE_OK;
 }
 
+// Whether the norm and the workspace lie apart and over no tensor: the
+// workspace is written before the gradients are all read.
+bool norm_apart(const moce_gradient* g, int32_t count, const float* norm, const void* ws, bool dst) {
+  const Range n{norm, 4}, w{ws, moce::gradient_ws_bytes(g, count)};
+  if (!outputs_apart({}, {n, w})) return false;
+  for (int32_t i = 0; i < count; ++i) {
+    const size_t bytes = (size_t)g[i].n * (g[i].dtype == MOCE_F32 ? 4 : 2);
+    if (!outputs_apart({{g[i].src, bytes}, {dst ? g[i].dst : nullptr, bytes}}, {n, w})) return false;
+  }
+  return true;
+}
+
 }  // namespace
 
 size_t moce_gradient_workspace_bytes(const moce_gradient* grads, int32_t count) {
@@ -750,6 +762,7 @@ moce_status moce_gradient_norm(const moce_gradient* grads, int32_t count, float*
   moce_status st = check_gradients(grads, count);
   if (st == MOCE_OK) st = check_gradient_ws(grads, count, norm, ws, ws_bytes);
   if (st != MOCE_OK) return st;
+  if (!norm_apart(grads, count, norm, ws, false)) return MOCE_ERR_SHAPE;
   return device_status(moce::launch_gradient_norm(grads, count, norm, ws, stream));
 }
 
@@ -759,15 +772,12 @@ moce_status moce_gradient_clip(const moce_gradient* grads, int32_t count, float 
   if (st == MOCE_OK) st = check_gradient_ws(grads, count, norm, ws, ws_bytes);
   if (st != MOCE_OK) return st;
   if (!std::isfinite(max_norm) || max_norm < 0.f) return MOCE_ERR_SHAPE;
-  const size_t need = moce::gradient_ws_bytes(grads, count);
   for (int32_t i = 0; i < count; ++i) {
     if (grads[i].n == 0) continue;
     if (!grads[i].dst) return MOCE_ERR_NULL;
     if (!aligned(grads[i].dst, grads[i].dtype == MOCE_F32 ? 4 : 2)) return MOCE_ERR_ALIGN;
-    // the norm and the workspace are written before the gradients are read again
-    const size_t bytes = (size_t)grads[i].n * (grads[i].dtype == MOCE_F32 ? 4 : 2);
-    if (!outputs_apart({{grads[i].src, bytes}, {grads[i].dst, bytes}}, {{norm, 4}, {ws, need}})) return MOCE_ERR_SHAPE;
   }
+  if (!norm_apart(grads, count, norm, ws, true)) return MOCE_ERR_SHAPE;
   try {
     if (!ranges_apart(grads, count)) return MOCE_ERR_SHAPE;
   } catch (const std::bad_alloc&) {

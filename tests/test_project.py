@@ -194,3 +194,15 @@ def test_layers_refuse_what_is_not_on_the_gpu():
         gradient_norm([])
     with pytest.raises(ValueError):
         clip_gradients([torch.zeros(4)], 1.0)
+
+
+def test_the_norm_over_a_tensor():
+    """The workspace is written while the gradients are read, and the norm is no gradient."""
+    a, far = FAKE, FAKE << 8
+    arr = gradients((a, None, 4096, F32))
+    need = 512                                       # the two chunks' sums, rounded up
+    assert norm(arr, 1, out=far, ws=a) == -2
+    assert norm(arr, 1, out=far, ws=a + 4096 * 4 - 256) == -2
+    assert norm(arr, 1, out=far, ws=a - 256, nb=need) == -2
+    assert norm(arr, 1, out=a + 4096 * 4 - 4, ws=far) == -2
+    assert norm(arr, 1, out=far + 256, ws=far, nb=need) == -2
