@@ -214,3 +214,81 @@ def test_a_coefficient_below_the_normal_numbers(max_norm, count):
         assert ((o.double() - exact).abs() <= (2.0 ** -22 + half) * exact.abs() + 2.0 ** -133).all()
     clip_gradients(ts, max_norm)
     assert all(torch.equal(t, o) for t, o in zip(ts, outs))
+
+
+def clipped_as_expected(ts, outs, max_norm, want):
+    coef = min(1.0, max_norm / want)
+    for t, o in zip(ts, outs):
+        half = 2.0 ** -24 if t.dtype == F else 2.0 ** -8
+        assert ((o.double() - t.double() * coef).abs() <= (2.0 ** -22 + half) * (t.double().abs() * coef)).all()
+
+
+@pytest.mark.parametrize("count", [4096, 4097, 8192 + 129])
+def test_many_chunks(count):
+    """A chunk per tensor: the last count whose sums every workgroup adds up by itself, and the first of a launch between."""
+    ts = normals([1] * count, [F, H] * (count // 2) + [H] * (count % 2), seed=count)
+    want = norm64(ts)
+    got = gradient_norm(ts)
+    assert abs(float(got) - want) <= 2.0 ** -23 * want
+    keep, outs = [t.clone() for t in ts], [torch.full_like(t, 7.0) for t in ts]
+
+    def flat(v):
+        return [torch.cat([t for t in v if t.dtype == d]) for d in (F, H)]
+
+    for max_norm in (want * 0.3, want * 3):
+        assert torch.equal(clip_gradients(ts, max_norm, out=outs), got)
+        clipped_as_expected(flat(keep), flat(outs), max_norm, want)
+        assert all(torch.equal(a, b) for a, b in zip(flat(ts), flat(keep)))
+        assert torch.equal(clip_gradients(ts, max_norm), got)
+        assert all(torch.equal(a, b) for a, b in zip(flat(ts), flat(outs)))
+        for t, k in zip(ts, keep):
+            t.copy_(k)
+    for at, bad in ((0, float("nan")), (count - 1, float("inf"))):
+        ts[at].fill_(bad)
+        before = flat(ts)
+        assert not torch.isfinite(clip_gradients(ts, 1e-3)).any()
+        assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(flat(ts), before))
+        ts[at].copy_(keep[at])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = clip_gradients(ts, 1.0)
+    for f in (1.0, 0.001, 3.0):
+        for t, k in zip(ts, keep):
+            t.copy_(k * f)
+        want = clip_gradients(ts, 1.0, out=outs)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want) and all(torch.equal(a, b) for a, b in zip(flat(ts), flat(outs)))
+
+
+@pytest.mark.parametrize("n", [(1 << 27) + 32771, (1 << 31) + (1 << 16) + 7], ids=str)
+def test_large_lists(n):
+    """Chunks of the largest size and above it, one tensor past 2^31 elements, odd ends, small tensors around it."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ts = [torch.randn(1001, generator=g, device="cuda"), torch.empty(n, dtype=H, device="cuda"),
+          torch.randn(33, generator=g, device="cuda").bfloat16()]
+    ts[1].random_(-3, 4, generator=g)
+    piece = 1 << 27
+
+    def pieces(t):
+        return t.split(piece)
+
+    def squares(t):
+        return sum(float((p.double() ** 2).sum()) for p in pieces(t))
+
+    want = sum(squares(t) for t in ts) ** 0.5
+    got = gradient_norm(ts)
+    assert abs(float(got) - want) <= 2.0 ** -23 * want
+    outs = [torch.full_like(t, 7.0) for t in ts]
+    for max_norm in (want * 3, want * 0.3):
+        assert torch.equal(clip_gradients(ts, max_norm, out=outs), got)
+        for t, o in zip(ts, outs):
+            for a, b in zip(pieces(t), pieces(o)):
+                clipped_as_expected([a], [b], max_norm, want)
+        assert torch.equal(clip_gradients(ts, max_norm), got)
+        assert all(torch.equal(t, o) for t, o in zip(ts, outs))
+    ts[1][-1] = float("inf")
+    assert not torch.isfinite(clip_gradients(ts, 1e-3)).any()
+    assert all(torch.equal(t[:-1], o[:-1]) for t, o in zip(ts[1:2], outs[1:2]))
