@@ -543,3 +543,39 @@ def test_a_weight_without_channels_is_refused(O, C):
     """A sum over no channels is none that the kernels form: the call would have to return act(shift + residual)."""
     with pytest.raises(ValueError):
         ProjectLayer(torch.empty(O, C, device="cuda"))
+
+
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(4, 24, 16, 257, 257, "nchw"), (4, 24, 16, 256, 260, "nchw"), (7, 40, 24, 200, 200, "nchw"),
+                                  (1, 24, 16, 512, 520, "nchw"), (4, 24, 16, 257, 257, "nhwc"), (9, 23, 13, 181, 163, "nhwc"),
+                                  (9000, 23, 13, 4, 7, "nchw")], ids=str)
+def test_sums_of_whole_numbers_over_many_positions(size, dtype, act):
+    """Every partial sum is a whole number below 2^24 (a half of one for dscale and dx) and so exact in float32: a
+    position that is lost or counted twice shows, and the gradients are the exact ones rounded once."""
+    B, C, O, H, W, layout = size
+    g = torch.Generator(device="cuda").manual_seed(B + C)
+    dt, xs, ys = TYPES[dtype], (B, C, H, W), (B, O, H, W)
+    if layout == "nhwc":
+        xs, ys = (B, H, W, C), (B, H, W, O)
+
+    def whole(shape, lo, hi, t):
+        return torch.empty(shape, device="cuda").random_(lo, hi + 1, generator=g).to(t)
+
+    # means that are not zero, so that no part of the positions adds up to nothing
+    x, dy, z = whole(xs, -1, 3, dt), whole(ys, -1, 2, dt), whole(ys, -1, 1, dt)
+    w, shift = whole((O, C), -2, 2, dt), whole((O,), -3, 3, torch.float32)
+    scale = 2.0 ** whole((O,), -1, 1, torch.float32) * torch.where(whole((O,), 0, 1, torch.float32) > 0, 1.0, -1.0)
+    layer = ProjectLayer(w, scale, shift, act=act, layout=layout)
+    out = layer.backward(x, dy, z=z if act == "relu" else None, residual=True)
+    xd, wd, dz = rows(x, layout), w.double(), rows(dy, layout)
+    if act == "relu":
+        dz = torch.where(rows(z, layout) > 0, dz, torch.zeros_like(dz))
+    assert float((dz.abs().t() @ xd.abs()).max()) < 2.0 ** 24
+    G = dz.t() @ xd
+    assert float((wd.abs() * G.abs()).sum(1).max()) < 2.0 ** 24
+    assert torch.equal(out["dshift"], dz.sum(0).float())
+    assert torch.equal(out["dscale"], (wd * G).sum(1).float())
+    assert torch.equal(out["dweight"], (scale.double()[:, None] * G).to(dt))
+    assert torch.equal(rows(out["dresidual"], layout), dz)
+    assert torch.equal(rows(out["dx"], layout), ((dz * scale.double()) @ wd).to(dt).double())
