@@ -439,6 +439,24 @@ moce_status moce_project_backward(const moce_project_desc* desc, const void* x, 
                                   const float* scale, const void* z, const void* dy,
                                   const moce_project_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* How one of the products of this descriptor is cut, for tests and timing (the
+ * results do not depend on it but for the order of float32 sums). */
+enum { MOCE_PRODUCT_FORWARD = 0, MOCE_PRODUCT_DX = 1, MOCE_PRODUCT_DWEIGHT = 2 };
+
+typedef struct moce_project_cut {
+    int32_t rows, columns; /* a tile of the product; 0: the forward of up to 32 rows, which has none */
+    int32_t stages;        /* of the contraction in LDS */
+    int32_t splits;        /* parts of the contraction, joined by another kernel (1: none) */
+    int32_t a_along;       /* whether the rows' operand runs along the contraction in memory */
+    int32_t b_along;       /* and the columns' */
+    int32_t images;        /* whether lines along the contraction pass from image to image */
+    int32_t reserved;
+} moce_project_cut;
+
+/* A query on the host.  Errors: MOCE_ERR_NULL (desc, cut), MOCE_ERR_SHAPE for
+ * an unknown product, and those of moce_project for the descriptor. */
+moce_status moce_project_path(const moce_project_desc* desc, int32_t product, moce_project_cut* cut);
+
 /* ---- the global norm of a list of gradients, and clipping ------------------ */
 
 /* One gradient: n elements of `dtype` at src (aligned to its element; n == 0

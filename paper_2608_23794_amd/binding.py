@@ -21,6 +21,7 @@ MOCE_F32, MOCE_BF16 = 0, 1
 MOCE_NCHW, MOCE_NHWC = 0, 1
 MOCE_GATE_SOFTPLUS_LINEAR, MOCE_GATE_MLP_SIGMOID = 0, 1
 MOCE_ACT_NONE, MOCE_ACT_RELU, MOCE_ACT_GELU, MOCE_ACT_SILU = 0, 1, 2, 3
+MOCE_PRODUCT_FORWARD, MOCE_PRODUCT_DX, MOCE_PRODUCT_DWEIGHT = 0, 1, 2
 
 STATUS = {
     0: "MOCE_OK", -1: "MOCE_ERR_NULL", -2: "MOCE_ERR_SHAPE", -3: "MOCE_ERR_DTYPE",
@@ -34,8 +35,8 @@ ENTRY_POINTS = (
     "moce_forward_workspace_bytes", "moce_forward_path", "moce_forward", "moce_forward_ex", "moce_forward_static",
     "moce_forward_dynamic_workspace_bytes", "moce_forward_dynamic", "moce_backward_workspace_bytes",
     "moce_backward", "moce_logit_backward_workspace_bytes", "moce_logit_backward", "moce_project_workspace_bytes",
-    "moce_project", "moce_project_backward_workspace_bytes", "moce_project_backward", "moce_gradient_workspace_bytes",
-    "moce_gradient_norm", "moce_gradient_clip", "moce_status_str", "moce_abi_version",
+    "moce_project", "moce_project_backward_workspace_bytes", "moce_project_backward", "moce_project_path",
+    "moce_gradient_workspace_bytes", "moce_gradient_norm", "moce_gradient_clip", "moce_status_str", "moce_abi_version",
 )
 
 MOCE_STATIC_SCRATCH_BYTES = 16 << 20
@@ -85,6 +86,11 @@ class moce_project_desc(ctypes.Structure):
 class moce_project_grads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p), ("dscale", ctypes.c_void_p),
                 ("dshift", ctypes.c_void_p), ("dresidual", ctypes.c_void_p)]
+
+
+class moce_project_cut(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "columns", "stages", "splits", "a_along", "b_along", "images",
+                                              "reserved")]
 
 
 class moce_gradient(ctypes.Structure):
@@ -138,6 +144,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_project_backward_workspace_bytes.argtypes = [J]
     lib.moce_project_backward_workspace_bytes.restype = SZ
     lib.moce_project_backward.argtypes = [J, P, P, P, P, P, ctypes.POINTER(moce_project_grads), P, SZ, P]
+    lib.moce_project_path.argtypes = [J, I32, ctypes.POINTER(moce_project_cut)]
     # the list as an address, or bytes laid out as an array of moce_gradient
     lib.moce_gradient_workspace_bytes.argtypes = [P, I32]
     lib.moce_gradient_workspace_bytes.restype = SZ
@@ -148,7 +155,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_abi_version.restype = ctypes.c_int
     for name in ("moce_support_prepare", "moce_support_prepare16", "moce_pool", "moce_gate", "moce_gate_mix", "moce_mix", "moce_forward", "moce_forward_ex",
                  "moce_forward_static", "moce_forward_dynamic", "moce_backward", "moce_logit_backward",
-                 "moce_project", "moce_project_backward", "moce_gradient_norm", "moce_gradient_clip"):
+                 "moce_project", "moce_project_backward", "moce_project_path", "moce_gradient_norm",
+                 "moce_gradient_clip"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -351,6 +359,13 @@ def moce_project_backward(desc: moce_project_desc, x, weight, scale, z, dy, grad
     _check("moce_project_backward", load().moce_project_backward(ctypes.byref(desc), _ptr(x), _ptr(weight),
                                                                  _ptr(scale), _ptr(z), _ptr(dy), ctypes.byref(grads),
                                                                  _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moce_project_path(desc: moce_project_desc, product: int) -> moce_project_cut:
+    """How the product MOCE_PRODUCT_* of this descriptor is cut."""
+    cut = moce_project_cut()
+    _check("moce_project_path", load().moce_project_path(ctypes.byref(desc), product, ctypes.byref(cut)))
+    return cut
 
 
 def make_gradients(src, dst, sizes, dtypes) -> bytes:

@@ -692,6 +692,16 @@ moce_status moce_project_backward(const moce_project_desc* desc, const void* x, 
   return device_status(moce::launch_project_backward(s, x, weight, scale, z, dy, *grads, ws, stream));
 }
 
+moce_status moce_project_path(const moce_project_desc* desc, int32_t product, moce_project_cut* cut) {
+  moce::ProjectShape s;
+  const moce_status st = check_project(desc, &s);
+  if (st != MOCE_OK) return st;
+  if (!cut) return MOCE_ERR_NULL;
+  if (product < MOCE_PRODUCT_FORWARD || product > MOCE_PRODUCT_DWEIGHT) return MOCE_ERR_SHAPE;
+  *cut = moce::project_path(s, product);
+  return MOCE_OK;
+}
+
 // ---- gradient norm and clipping --------------------------------------------------
 
 namespace {

@@ -310,6 +310,7 @@ size_t project_ws_bytes(const ProjectShape& s);   // packed operands, partial pr
 hipError_t launch_project(const ProjectShape& s, const void* x, const void* w, const float* scale, const float* shift,
                           const void* res, void* y, void* z, void* ws, hipStream_t st);
 size_t project_backward_ws_bytes(const ProjectShape& s);
+moce_project_cut project_path(const ProjectShape& s, int product);
 hipError_t launch_project_backward(const ProjectShape& s, const void* x, const void* w, const float* scale,
                                    const void* z, const void* dy, const moce_project_grads& gr, void* ws,
                                    hipStream_t st);

@@ -1742,6 +1742,22 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
 
 size_t project_backward_ws_bytes(const ProjectShape& s) { return bwd_layout(s).total; }
 
+// What forward() and backward() launch, by the table at the file's head
+// (planes that are turned are lines of channels, as channels-last ones).
+moce_project_cut project_path(const ProjectShape& s, int product) {
+  const Sizes z(s);
+  const bool forward = product == MOCE_PRODUCT_FORWARD, turned = !z.nhwc && z.planes(), lines = z.nhwc || turned;
+  moce_project_cut c{};
+  c.splits = 1;
+  c.a_along = forward || (product == MOCE_PRODUCT_DX ? lines : !lines);
+  c.b_along = forward ? lines : product == MOCE_PRODUCT_DX ? turned : !lines;
+  if (forward && few_rows(z)) return c;
+  const Plan p = forward ? fwd_layout(s).p : product == MOCE_PRODUCT_DX ? bwd_layout(s).px : bwd_layout(s).pw;
+  c.rows = kTile[p.tile].tr, c.columns = kTile[p.tile].tc, c.stages = kTile[p.tile].stages, c.splits = p.splits;
+  c.images = product == MOCE_PRODUCT_DWEIGHT && !lines && z.images() > 0;
+  return c;
+}
+
 hipError_t launch_project_backward(const ProjectShape& s, const void* x, const void* w, const float* scale,
                                    const void* z, const void* dy, const moce_project_grads& gr, void* ws,
                                    hipStream_t st) {

@@ -409,8 +409,8 @@ def test_rows_of_one_image_beyond_two_gigabytes():
     check("dweight", out["dweight"], want, HALF["bf16"] * want.abs())
 
 
-# aligned shapes that take each tile with edges in it, contractions that end inside a stage, images shorter and longer
-# than a stage
+# aligned shapes with edges in their tiles, contractions that end inside a stage, images shorter and longer than a
+# stage (every kernel that the products can take: test_project_tiles.py)
 TILES = [(1, 200, 328, 700, 1, "nhwc"), (3, 136, 264, 40, 24, "nchw"), (2, 1096, 520, 33, 16, "nhwc"),
          (5, 64, 72, 8, 9, "nchw"), (300, 328, 264, 1, 1, "nhwc"), (64, 24, 2056, 72, 1, "nhwc"), (40, 2056, 24, 8, 10, "nchw"),
          (9, 1032, 1544, 1000, 1, "nhwc"), (10, 1544, 1032, 24, 25, "nchw")]
