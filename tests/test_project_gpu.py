@@ -579,3 +579,43 @@ def test_sums_of_whole_numbers_over_many_positions(size, dtype, act):
     assert torch.equal(out["dweight"], (scale.double()[:, None] * G).to(dt))
     assert torch.equal(rows(out["dresidual"], layout), dz)
     assert torch.equal(rows(out["dx"], layout), ((dz * scale.double()) @ wd).to(dt).double())
+
+
+def arena(nbytes, guard=4096):
+    """nbytes of device memory between guards of a fixed pattern, aligned to 256 bytes: the whole, and the middle."""
+    whole = torch.full((nbytes + 2 * guard + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    at = guard + -(whole.data_ptr() + guard) % 256
+    return whole, whole[at:at + nbytes], at
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 72, 50, 37, 1, "nhwc"), (3, 72, 48, 7, 9, "nchw"), (2, 40, 64, 8, 4, "nchw"),
+                                  (1, 1030, 13, 3, 1, "nhwc"), (2, 45, 541, 19, 1, "nhwc"), (5000, 9, 17, 2, 3, "nchw"),
+                                  (4100, 8, 16, 4, 2, "nchw"), (1, 100, 700, 1, 1, "nhwc"), (2, 700, 20, 13, 11, "nchw"),
+                                  (3, 260, 68, 60, 70, "nhwc"), (1, 1036, 516, 40, 1, "nhwc")], ids=str)
+def test_every_output_and_the_workspace_end_where_they_end(size, dtype):
+    """The calls themselves, with every output in memory of its own size and the workspace in what the query says."""
+    B, C, O, H, W, layout = size
+    for act, scale in (("relu", True), ("gelu", False), ("none", True), ("silu", True)):
+        t = make(B, C, O, H, W, dtype, layout, act, scale, True, seed=2)
+        layer, x, st = t["layer"], t["x"], torch.cuda.current_stream()
+        d = layer.desc(x.shape)
+        smooth = act in ("gelu", "silu")
+        like = {"y": t["dy"], "z": t["dy"], "dx": x, "dweight": t["w"], "dshift": t["shift"], "dresidual": t["dy"]}
+        if scale and not smooth:
+            like["dscale"] = t["scale"]
+        sizes = {n: v.numel() * v.element_size() for n, v in like.items()}
+        sizes.update(ws=layer.workspace_bytes(x.shape), bws=layer.backward_workspace_bytes(x.shape))
+        held = {n: arena(b) for n, b in sizes.items()}
+        out = {n: held[n][1].view(v.dtype).view(v.shape) for n, v in like.items()}
+        ws, bws = held["ws"][1], held["bws"][1]
+        mb.moce_project(d, x, t["w"], t["scale"], t["shift"], t["residual"], out["y"], out["z"], ws if sizes["ws"] else None,
+                        sizes["ws"], st)
+        grads = {n: out[n] for n in out if n not in ("y", "z")}
+        mb.moce_project_backward(d, x, t["w"], t["scale"], t["z"], t["dy"], mb.make_project_grads(**grads), bws,
+                                 sizes["bws"], st)
+        torch.cuda.synchronize()
+        for n, (whole, _, at) in held.items():
+            assert (whole[:at] == 0xA5).all() and (whole[at + sizes[n]:] == 0xA5).all(), n
+        check_forward(t, dtype, layout, act, t["residual"], out["y"], out["z"])
+        check_backward(t, dtype, layout, act, grads)

@@ -109,14 +109,39 @@ def test_the_kernel_of_a_product(lib):
     assert few.rows == 0 and few.splits == 1
 
 
+# the last planes whose tiles' offsets have 31 bits, and the first that are turned for that although their lines are whole
+SPANS = [(2, 256, 256, 8, 174762, "bf16", "nchw"), (2, 256, 256, 8, 174763, "bf16", "nchw"),
+         (3, 8, 8, 8, 493447, "bf16", "nchw"), (3, 8, 8, 8, 493448, "bf16", "nchw"),
+         (2, 72, 80, 8, 161319, "f32", "nchw"), (2, 72, 80, 8, 161320, "f32", "nchw")]
+
+
+def turned(size):
+    return {k[4:6] for k in kernels(*size)} == {(1, 1), (0, 0)}
+
+
+def test_the_planes_that_are_turned_for_their_offsets(lib):
+    assert [turned(s) for s in SPANS] == [False, True] * 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", SPANS, ids=str)
+def test_planes_at_the_limit_of_a_tiles_offsets(size):
+    check_products(size, "relu", True)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_products_of_whole_numbers(size):
+    i = SIZES.index(size)
+    check_products(size, ("none", "relu")[i % 2], i % 3 != 0)
+
+
+def check_products(size, act, affine):
     """Small whole numbers, scales that are powers of two: every sum is exact in float32, so y, z and the gradients are
     the exact ones rounded once, whatever the tile."""
     B, C, O, H, W, dtype, layout = size
     g = torch.Generator(device="cuda").manual_seed(C + O)
-    dt, act, affine = TYPES[dtype], ("none", "relu")[SIZES.index(size) % 2], SIZES.index(size) % 3 != 0
+    dt = TYPES[dtype]
     xs, ys = ((B, C, H, W), (B, O, H, W)) if layout == "nchw" else ((B, H, W, C), (B, H, W, O))
 
     def whole(shape, lo, hi, t):
