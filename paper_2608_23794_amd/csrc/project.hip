@@ -553,9 +553,8 @@ __device__ __align__(16) unsigned int zero_chunk[4];
 
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
-// s_waitcnt operands
+// the operand of s_waitcnt for at most n memory accesses in flight
 constexpr int vm_wait(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
-constexpr int kLgkmWait0 = 0xc07f;
 
 // 16 bytes from a scalar base and the lane's 32-bit offset (a buffer without
 // bounds), to `to` and the lanes' places behind it.  With 64-bit addresses of
