@@ -366,8 +366,8 @@ moce_status moce_logit_backward(int32_t R, int64_t C, int32_t k, const float* L,
  * scale, shift and residual are optional (NULL: 1, 0, 0). */
 
 /* Activations: z; max(z, 0); z (1 + erf(z / sqrt 2)) / 2; z / (1 + e^-z).
- * A NaN stays one, and infinities give the limits.  In bfloat16 the value is
- * evaluated to within 2^-12 of itself before its rounding. */
+ * A NaN stays one, and infinities give the limits.  In bfloat16 a value of
+ * 2^-119 or more is evaluated to within 2^-12 of itself before its rounding. */
 enum { MOCE_ACT_NONE = 0, MOCE_ACT_RELU = 1, MOCE_ACT_GELU = 2, MOCE_ACT_SILU = 3 };
 
 typedef struct moce_project_desc {

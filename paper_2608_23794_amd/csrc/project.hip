@@ -648,12 +648,13 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // WR x WC waves of FR x FC fragments, D stages in LDS.
 //
 // Bound by the matrix cores where the contraction is long (16384 positions of
-// 4096 by 4096: 418 us, 1315 TFLOP/s, of the 1421 that a large product of the
-// library reaches here), by memory where it is short (64 to 256 channels over
+// 4096 by 4096: 429 us, 1281 TFLOP/s, of the 1466 that a large product of the
+// library reaches here; the cores are busy 62% of the cycles of a burst, whose
+// clock falls to 2 GHz), by memory where it is short (64 to 256 channels over
 // 64 images of 56 x 56 with their residual: 50 us, 4.6 TB/s).  Between (50432
-// positions of 768 by 768, GELU, z written too: 82 us, for 46 of memory and 42
-// of products) the two do not overlap: a workgroup's results leave while only
-// its neighbours on the CU multiply.  Tried and slower there: a wave of its
+// positions of 768 by 768, GELU, z written too: 86 us, for 46 of memory and 41
+// of products; cores busy 26%, 125 MB read for 79) the two do not overlap: a
+// workgroup's results leave while only its neighbours on the CU multiply.  Tried and slower there: a wave of its
 // own that only copies, stages ahead of the product's end (persistent
 // workgroups), and prefetches of the stage after next into L2 (86 to 89 us).
 template <typename T, bool AK, bool BK, bool IMG, int WR, int WC, int FR, int FC, int D>
@@ -1155,7 +1156,7 @@ k_project_dz_planes(DzArgs a, int lanes) {
 // positions turned into lines of channels, [position][ld], or (rows) lines of
 // hw elements, O of them, copied to lines of ld; zeros behind the elements.
 // Bound by memory: the backward of 64 images of 256 to 1024 channels at 14 x
-// 14 (z, dy, dz, their copies: 117 MB) takes 26 us, 4.5 TB/s; of three
+// 14 (z, dy, dz, their copies: 120 MB counted) takes 28 us, 4.3 TB/s; of three
 // launches 45.
 struct Lines {
   DzArgs job[3];
@@ -1253,10 +1254,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The tiles there are: tr x tc, stages in LDS, workgroups a CU, and the
 // microseconds of a bfloat16 stage on a CU that is full (a workgroup's share)
-// and on one of its own.  These times and those of plan() are fitted to 3000
-// measured cuts of 165 products (forward, dx and dW from one position to
-// 360000, 32 to 4096 channels): the cut they pick is 1.4% slower than the best
-// one measured on average, 20% at worst.
+// and on one of its own.  These times and those of plan() are fitted to
+// measured cuts (forward, dx and dW from one position to 360000, 32 to 4096
+// channels).  Of 225 products in both types, 5657 cuts measured again, the cut
+// they pick is 1.6% slower than the best one on average, 22% at worst, and more
+// than 5% for 20 of them.
 struct Tile {
   int tr, tc, stages, per_cu;
   double busy, alone;
@@ -1634,7 +1636,13 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
   const bool turned = !z.nhwc && z.planes();
   // Where dz is rounded anyway, the scale goes into it before the rounding
   // (one rounding, not two); where dz is dy or 0, into the weight of dx and
-  // the rows of dW.
+  // the rows of dW.  So each bfloat16 product has one rounded operand at most,
+  // whose error is as large as the result's own rounding: dx (and, of GELU and
+  // SiLU, dweight) is 2.35e-3 off in the 2-norm where exact operands leave
+  // 1.66e-3.  Operands in two bfloat16 parts would leave that, for products
+  // twice as long: the dx of 64 images of 256 to 1024 channels at 14 x 14 takes
+  // 48 us and not 31, both products of 50432 tokens of 768 by 768 another 140
+  // beside a backward of 203.
   const bool fold = scale && smooth;
   const float* row_scale = fold ? nullptr : scale;
   const bool products = gr.dx || gr.dweight || gr.dscale;
