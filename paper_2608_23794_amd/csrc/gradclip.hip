@@ -185,7 +185,7 @@ k_gradient_scale(List l, int64_t chunk, const double* __restrict__ part, int chu
     c = *coef;
   }
   const Part r = part_of(l, gridDim.x - 1 - blockIdx.x, chunk);
-  if (c.first == 1.f && l.src[r.t] == l.dst[r.t]) return;
+  if (c.first == 1.f && c.second == 1.f && l.src[r.t] == l.dst[r.t]) return;
   if (r.bf16) {
     const uint16_t* p = static_cast<const uint16_t*>(l.src[r.t]);
     uint16_t* d = static_cast<uint16_t*>(l.dst[r.t]);

@@ -292,3 +292,16 @@ def test_large_lists(n):
     ts[1][-1] = float("inf")
     assert not torch.isfinite(clip_gradients(ts, 1e-3)).any()
     assert all(torch.equal(t[:-1], o[:-1]) for t, o in zip(ts[1:2], outs[1:2]))
+
+
+@pytest.mark.parametrize("count", [2, 4200])
+def test_a_coefficient_just_below_the_normal_numbers(count):
+    """Its first factor rounds to 1; the gradients are scaled all the same, in place too."""
+    ts = [torch.tensor([2.0 ** 100], device="cuda"), torch.tensor([2.0 ** 87.5], device="cuda").bfloat16()]
+    ts += [torch.zeros(1, device="cuda") for _ in range(count - 2)]
+    want, max_norm = norm64(ts), 2.0 ** -26
+    assert 1 - 2.0 ** -25 < max_norm / want * 2.0 ** 126 < 1
+    outs = [torch.empty_like(t) for t in ts]
+    clip_gradients(ts, max_norm, out=outs)
+    clip_gradients(ts, max_norm)
+    assert float(ts[0]) == 2.0 ** -26 and all(torch.equal(t, o) for t, o in zip(ts, outs))
