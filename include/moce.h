@@ -457,6 +457,163 @@ typedef struct moce_project_cut {
  * an unknown product, and those of moce_project for the descriptor. */
 moce_status moce_project_path(const moce_project_desc* desc, int32_t product, moce_project_cut* cut);
 
+/* ---- group norm with an activation -------------------------------------------
+ *
+ * x holds B images of C channels over H*W positions; the channels form G groups
+ * of C / G neighbours.  Per image b and group g, over the n = (C / G) H W
+ * elements of the group:
+ *   mean = sum x / n,   rstd = 1 / sqrt(sum (x - mean)^2 / n + eps),
+ *   h = (x - mean) rstd,   z = scale[c] h + shift[c],   y = act(z)
+ * (scale and shift optional: NULL is 1 and 0).  G = 1 takes all channels of an
+ * image together, G = C each by itself. */
+typedef struct moce_group_norm_desc {
+    int64_t B, C, H, W;
+    int64_t G;            /* groups, a divisor of C */
+    int32_t dtype;        /* of x, y and their gradients: MOCE_F32 or MOCE_BF16 */
+    int32_t layout;       /* MOCE_NCHW or MOCE_NHWC (tokens: H of them, W = 1) */
+    int32_t act;          /* MOCE_ACT_* */
+    float eps;            /* finite, >= 0 */
+} moce_group_norm_desc;
+
+/* Bytes of device workspace moce_group_norm needs (0 on an invalid descriptor). */
+size_t moce_group_norm_workspace_bytes(const moce_group_norm_desc* desc);
+
+/* The normalisation.  x, y: contiguous, 16-byte aligned; scale, shift: float32
+ * [C]; stats (optional): float32 [2][B][G], the means, then the rstd, which the
+ * backward reads.  y is fully overwritten and may be x (in place); nothing else
+ * may overlap.  Sums are float32 about values of the group, so that a mean that
+ * is large against the deviation costs no digits of it; their order depends on
+ * the descriptor alone.  A NaN or infinity makes its group NaN, and no other.
+ * ws: as sized above, 256-byte aligned; calls that can run at the same time
+ * need one each, captured calls that are replayed so too.  Asynchronous on
+ * `stream`.  Errors: MOCE_ERR_NULL (desc, x, y), MOCE_ERR_SHAPE (a size below
+ * 1, C not a multiple of G, an unknown act, eps, memory that overlaps),
+ * MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE,
+ * MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED when C exceeds 2^20, C H W 2^31 - 1, B
+ * 2^29 or B C H W 2^38. */
+moce_status moce_group_norm(const moce_group_norm_desc* desc, const void* x, const float* scale, const float* shift,
+                            void* y, float* stats, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of moce_group_norm, each optional (NULL: not computed) and fully
+ * overwritten; t = scale dz, means over the group:
+ *   dz = act'(z) dy;   dshift[c] = sum dz;   dscale[c] = sum dz h;
+ *   dx = rstd (t - mean(t) - h mean(t h)). */
+typedef struct moce_group_norm_grads {
+    void* dx;             /* layout and type of x */
+    float* dscale;        /* [C] */
+    float* dshift;        /* [C] */
+} moce_group_norm_grads;
+
+/* Bytes of device workspace moce_group_norm_backward needs (0 on an invalid
+ * descriptor). */
+size_t moce_group_norm_backward_workspace_bytes(const moce_group_norm_desc* desc);
+
+/* The gradients for an upstream gradient dy of y (layout and type of y); x,
+ * scale and shift as in the forward, stats as it wrote them (h and z are formed
+ * again).  act' of ReLU is 0 where z <= 0.  dx may be dy or x (in place); no
+ * other output, and not ws, may overlap an input or another output.  Sums are
+ * float32, their order depends on the descriptor alone.  ws as sized above,
+ * 256-byte aligned.  Errors: those of moce_group_norm; MOCE_ERR_NULL for a
+ * missing dy, stats or grads.  Asynchronous on `stream`. */
+moce_status moce_group_norm_backward(const moce_group_norm_desc* desc, const void* x, const float* scale,
+                                     const float* shift, const float* stats, const void* dy,
+                                     const moce_group_norm_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- the losses of a classification head ----------------------------------------
+ *
+ * A head projects P rows of C features to V classes, z[p][v] = sum_c x[p][c]
+ * weight[v][c] + shift[v] (moce_project gives the logits z themselves).  The
+ * calls here take the loss of the logits and its gradients without keeping the
+ * logits: the forward leaves the softmax statistics of a row, the backward
+ * forms the logits again, in pieces of the classes.
+ *
+ * Cross entropy with a label t[p], smoothed by e:
+ *   loss[p] = lse - (1 - e) z[p][t] - e mean_v z[p][v],   lse = log sum_v e^z[p][v].
+ * Distillation from K entries of a teacher's logits, classes i[p][k] and logits
+ * l[p][k], at temperature T: q = softmax(l[p] / T) over the entries, those of
+ * one class added up; with s = z / T,
+ *   loss[p] = T^2 sum_v q_v (log q_v - s[p][v] + log sum_u e^s[p][u]).
+ *
+ * A label outside [0, V) leaves its row out: its loss is 0, it adds nothing to
+ * the gradients and its dx is 0, whatever the row holds.  So does a teacher of
+ * whose entries none has a class in [0, V) and a logit above minus infinity;
+ * an entry whose class is outside counts for nothing. */
+enum { MOCE_LOSS_ROWS = 0, MOCE_LOSS_MEAN = 1 };
+
+typedef struct moce_head_desc {
+    int64_t P, C, V;        /* rows, features, classes */
+    int32_t K;              /* entries of the teacher a row; 1 for labels */
+    int32_t dtype;          /* of x, weight and their gradients: MOCE_F32 or MOCE_BF16 */
+    int32_t teacher_dtype;  /* of the teacher's logits (not read for labels) */
+    int32_t index_bytes;    /* of a label or class, a signed integer: 4 or 8 */
+    int32_t reduction;      /* MOCE_LOSS_ROWS: loss[P]; MOCE_LOSS_MEAN: loss[1], the mean over the
+                             * rows that are not left out (0 where all are) */
+    float smoothing;        /* e in [0, 1] (not read by the distillation) */
+    float temperature;      /* T, finite, > 0 (not read by the cross entropy) */
+    int32_t reserved;       /* set to 0 */
+} moce_head_desc;
+
+/* Elements of the float32 array `saved` that a forward leaves for the backward:
+ * P (K + 1) + 2 (0 on an invalid descriptor). */
+size_t moce_head_saved_floats(const moce_head_desc* desc);
+
+/* Bytes of device workspace the two forward calls need (0 on an invalid
+ * descriptor). */
+size_t moce_head_workspace_bytes(const moce_head_desc* desc);
+
+/* The losses.  x: [P][C], weight: [V][C], of the descriptor's type, 16-byte
+ * aligned; shift: float32 [V] or NULL (minus infinity takes a class out);
+ * labels [P], classes [P][K]: integers of index_bytes; logits: [P][K], of
+ * teacher_dtype; loss: float32, as the reduction has it; saved: float32, sized
+ * as above, or NULL where no backward follows.  All contiguous; no output, and
+ * not ws, may overlap an input or another output.  Sums are float32 (over rows
+ * float64), their order depends on the descriptor alone; a logit that is not
+ * finite makes its row's loss so.  ws: 256-byte aligned, one for each call that can run
+ * at the same time, captured calls that are replayed so too.  Asynchronous on
+ * `stream`.  Errors: MOCE_ERR_NULL (desc, x, weight, the targets, loss),
+ * MOCE_ERR_SHAPE (a size below 1, K not 1 for labels, index_bytes, reduction,
+ * smoothing, temperature, memory that overlaps), MOCE_ERR_DTYPE,
+ * MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED
+ * when P exceeds 2^24, C or V 2^20, K 1024, V C 2^35, P V 2^35 or P C 2^33. */
+moce_status moce_head_cross_entropy(const moce_head_desc* desc, const void* x, const void* weight, const float* shift,
+                                    const void* labels, float* loss, float* saved, void* ws, size_t ws_bytes,
+                                    hipStream_t stream);
+moce_status moce_head_distill(const moce_head_desc* desc, const void* x, const void* weight, const float* shift,
+                              const void* classes, const void* logits, float* loss, float* saved, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of the losses, each optional (NULL: not computed) and fully
+ * overwritten.  With g[p] the upstream dloss[p] (MOCE_LOSS_MEAN: dloss[0] over
+ * the number of rows that count), 0 for a row that is left out:
+ *   cross entropy: dz[p][v] = g (softmax(z)[v] - (1 - e) [v = t] - e / V);
+ *   distillation:  dz[p][v] = g T (softmax(z / T)[v] - q_v);
+ *   dx[p][c] = sum_v dz[p][v] weight[v][c];   dweight[v][c] = sum_p dz[p][v] x[p][c];
+ *   dshift[v] = sum_p dz[p][v]. */
+typedef struct moce_head_grads {
+    void* dx;             /* [P][C], type of x */
+    void* dweight;        /* [V][C], type of weight */
+    float* dshift;        /* [V] */
+} moce_head_grads;
+
+/* Bytes of device workspace the two backward calls need (0 on an invalid
+ * descriptor). */
+size_t moce_head_backward_workspace_bytes(const moce_head_desc* desc);
+
+/* The gradients.  The inputs as in the forward, saved as it wrote them; dloss:
+ * float32 [P], or [1] for MOCE_LOSS_MEAN.  For bfloat16, dz enters the products
+ * rounded to its type; sums are float32, and dshift takes dz as it is.  Rows
+ * that are left out may hold anything, NaN too.  ws and errors as for the
+ * forward; MOCE_ERR_NULL for a missing saved, dloss or grads.  Asynchronous on
+ * `stream`. */
+moce_status moce_head_cross_entropy_backward(const moce_head_desc* desc, const void* x, const void* weight,
+                                             const float* shift, const void* labels, const float* saved,
+                                             const float* dloss, const moce_head_grads* grads, void* ws,
+                                             size_t ws_bytes, hipStream_t stream);
+moce_status moce_head_distill_backward(const moce_head_desc* desc, const void* x, const void* weight,
+                                       const float* shift, const void* classes, const void* logits,
+                                       const float* saved, const float* dloss, const moce_head_grads* grads, void* ws,
+                                       size_t ws_bytes, hipStream_t stream);
+
 /* ---- the global norm of a list of gradients, and clipping ------------------ */
 
 /* One gradient: n elements of `dtype` at src (aligned to its element; n == 0

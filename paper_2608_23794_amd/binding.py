@@ -21,6 +21,7 @@ MOCE_F32, MOCE_BF16 = 0, 1
 MOCE_NCHW, MOCE_NHWC = 0, 1
 MOCE_GATE_SOFTPLUS_LINEAR, MOCE_GATE_MLP_SIGMOID = 0, 1
 MOCE_ACT_NONE, MOCE_ACT_RELU, MOCE_ACT_GELU, MOCE_ACT_SILU = 0, 1, 2, 3
+MOCE_LOSS_ROWS, MOCE_LOSS_MEAN = 0, 1
 MOCE_PRODUCT_FORWARD, MOCE_PRODUCT_DX, MOCE_PRODUCT_DWEIGHT = 0, 1, 2
 
 STATUS = {
@@ -36,7 +37,10 @@ ENTRY_POINTS = (
     "moce_forward_dynamic_workspace_bytes", "moce_forward_dynamic", "moce_backward_workspace_bytes",
     "moce_backward", "moce_logit_backward_workspace_bytes", "moce_logit_backward", "moce_project_workspace_bytes",
     "moce_project", "moce_project_backward_workspace_bytes", "moce_project_backward", "moce_project_path",
-    "moce_gradient_workspace_bytes", "moce_gradient_norm", "moce_gradient_clip", "moce_status_str", "moce_abi_version",
+    "moce_group_norm_workspace_bytes", "moce_group_norm", "moce_group_norm_backward_workspace_bytes",
+    "moce_group_norm_backward", "moce_head_saved_floats", "moce_head_workspace_bytes", "moce_head_cross_entropy",
+    "moce_head_distill", "moce_head_backward_workspace_bytes", "moce_head_cross_entropy_backward",
+    "moce_head_distill_backward", "moce_gradient_workspace_bytes", "moce_gradient_norm", "moce_gradient_clip", "moce_status_str", "moce_abi_version",
 )
 
 MOCE_STATIC_SCRATCH_BYTES = 16 << 20
@@ -93,6 +97,27 @@ class moce_project_cut(ctypes.Structure):
                                               "reserved")]
 
 
+class moce_group_norm_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("C", ctypes.c_int64), ("H", ctypes.c_int64), ("W", ctypes.c_int64),
+                ("G", ctypes.c_int64), ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class moce_group_norm_grads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dscale", ctypes.c_void_p), ("dshift", ctypes.c_void_p)]
+
+
+class moce_head_desc(ctypes.Structure):
+    _fields_ = [("P", ctypes.c_int64), ("C", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32), ("index_bytes", ctypes.c_int32),
+                ("reduction", ctypes.c_int32), ("smoothing", ctypes.c_float), ("temperature", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class moce_head_grads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p), ("dshift", ctypes.c_void_p)]
+
+
 class moce_gradient(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
@@ -145,6 +170,21 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_project_backward_workspace_bytes.restype = SZ
     lib.moce_project_backward.argtypes = [J, P, P, P, P, P, ctypes.POINTER(moce_project_grads), P, SZ, P]
     lib.moce_project_path.argtypes = [J, I32, ctypes.POINTER(moce_project_cut)]
+    N = ctypes.POINTER(moce_group_norm_desc)
+    lib.moce_group_norm_workspace_bytes.argtypes = [N]
+    lib.moce_group_norm_workspace_bytes.restype = SZ
+    lib.moce_group_norm.argtypes = [N, P, P, P, P, P, P, SZ, P]
+    lib.moce_group_norm_backward_workspace_bytes.argtypes = [N]
+    lib.moce_group_norm_backward_workspace_bytes.restype = SZ
+    lib.moce_group_norm_backward.argtypes = [N, P, P, P, P, P, ctypes.POINTER(moce_group_norm_grads), P, SZ, P]
+    H, HG = ctypes.POINTER(moce_head_desc), ctypes.POINTER(moce_head_grads)
+    for name in ("moce_head_saved_floats", "moce_head_workspace_bytes", "moce_head_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = [H]
+        getattr(lib, name).restype = SZ
+    lib.moce_head_cross_entropy.argtypes = [H, P, P, P, P, P, P, P, SZ, P]
+    lib.moce_head_distill.argtypes = [H, P, P, P, P, P, P, P, P, SZ, P]
+    lib.moce_head_cross_entropy_backward.argtypes = [H, P, P, P, P, P, P, HG, P, SZ, P]
+    lib.moce_head_distill_backward.argtypes = [H, P, P, P, P, P, P, P, HG, P, SZ, P]
     # the list as an address, or bytes laid out as an array of moce_gradient
     lib.moce_gradient_workspace_bytes.argtypes = [P, I32]
     lib.moce_gradient_workspace_bytes.restype = SZ
@@ -155,7 +195,9 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moce_abi_version.restype = ctypes.c_int
     for name in ("moce_support_prepare", "moce_support_prepare16", "moce_pool", "moce_gate", "moce_gate_mix", "moce_mix", "moce_forward", "moce_forward_ex",
                  "moce_forward_static", "moce_forward_dynamic", "moce_backward", "moce_logit_backward",
-                 "moce_project", "moce_project_backward", "moce_project_path", "moce_gradient_norm",
+                 "moce_project", "moce_project_backward", "moce_project_path", "moce_group_norm",
+                 "moce_group_norm_backward", "moce_head_cross_entropy", "moce_head_distill",
+                 "moce_head_cross_entropy_backward", "moce_head_distill_backward", "moce_gradient_norm",
                  "moce_gradient_clip"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
@@ -366,6 +408,89 @@ def moce_project_path(desc: moce_project_desc, product: int) -> moce_project_cut
     cut = moce_project_cut()
     _check("moce_project_path", load().moce_project_path(ctypes.byref(desc), product, ctypes.byref(cut)))
     return cut
+
+
+def make_group_norm_desc(B: int, C: int, H: int, W: int, G: int, dtype: int, layout: int,
+                         act: int = MOCE_ACT_NONE, eps: float = 1e-5) -> moce_group_norm_desc:
+    return moce_group_norm_desc(B, C, H, W, G, dtype, layout, act, eps)
+
+
+def moce_group_norm_workspace_bytes(desc: moce_group_norm_desc) -> int:
+    return load().moce_group_norm_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_group_norm(desc: moce_group_norm_desc, x, scale, shift, y, stats, ws, ws_bytes: int, stream=None) -> None:
+    _check("moce_group_norm", load().moce_group_norm(ctypes.byref(desc), _ptr(x), _ptr(scale), _ptr(shift), _ptr(y),
+                                                     _ptr(stats), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_group_norm_grads(dx=None, dscale=None, dshift=None) -> moce_group_norm_grads:
+    """The gradients to compute, device arrays that outlive its use (None: not computed)."""
+    return moce_group_norm_grads(_ptr(dx), _ptr(dscale), _ptr(dshift))
+
+
+def moce_group_norm_backward_workspace_bytes(desc: moce_group_norm_desc) -> int:
+    return load().moce_group_norm_backward_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_group_norm_backward(desc: moce_group_norm_desc, x, scale, shift, stats, dy, grads: moce_group_norm_grads, ws,
+                             ws_bytes: int, stream=None) -> None:
+    _check("moce_group_norm_backward",
+           load().moce_group_norm_backward(ctypes.byref(desc), _ptr(x), _ptr(scale), _ptr(shift), _ptr(stats),
+                                           _ptr(dy), ctypes.byref(grads), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_head_desc(P: int, C: int, V: int, dtype: int, K: int = 1, teacher_dtype: int = MOCE_F32,
+                   index_bytes: int = 8, reduction: int = MOCE_LOSS_MEAN, smoothing: float = 0.0,
+                   temperature: float = 1.0) -> moce_head_desc:
+    return moce_head_desc(P, C, V, K, dtype, teacher_dtype, index_bytes, reduction, smoothing, temperature, 0)
+
+
+def moce_head_saved_floats(desc: moce_head_desc) -> int:
+    return load().moce_head_saved_floats(ctypes.byref(desc))
+
+
+def moce_head_workspace_bytes(desc: moce_head_desc) -> int:
+    return load().moce_head_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_head_backward_workspace_bytes(desc: moce_head_desc) -> int:
+    return load().moce_head_backward_workspace_bytes(ctypes.byref(desc))
+
+
+def moce_head_cross_entropy(desc: moce_head_desc, x, weight, shift, labels, loss, saved, ws, ws_bytes: int,
+                            stream=None) -> None:
+    _check("moce_head_cross_entropy",
+           load().moce_head_cross_entropy(ctypes.byref(desc), _ptr(x), _ptr(weight), _ptr(shift), _ptr(labels),
+                                          _ptr(loss), _ptr(saved), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moce_head_distill(desc: moce_head_desc, x, weight, shift, classes, logits, loss, saved, ws, ws_bytes: int,
+                      stream=None) -> None:
+    _check("moce_head_distill",
+           load().moce_head_distill(ctypes.byref(desc), _ptr(x), _ptr(weight), _ptr(shift), _ptr(classes),
+                                    _ptr(logits), _ptr(loss), _ptr(saved), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def make_head_grads(dx=None, dweight=None, dshift=None) -> moce_head_grads:
+    """The gradients to compute, device arrays that outlive its use (None: not computed)."""
+    return moce_head_grads(_ptr(dx), _ptr(dweight), _ptr(dshift))
+
+
+def moce_head_cross_entropy_backward(desc: moce_head_desc, x, weight, shift, labels, saved, dloss,
+                                     grads: moce_head_grads, ws, ws_bytes: int, stream=None) -> None:
+    _check("moce_head_cross_entropy_backward",
+           load().moce_head_cross_entropy_backward(ctypes.byref(desc), _ptr(x), _ptr(weight), _ptr(shift),
+                                                   _ptr(labels), _ptr(saved), _ptr(dloss), ctypes.byref(grads),
+                                                   _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moce_head_distill_backward(desc: moce_head_desc, x, weight, shift, classes, logits, saved, dloss,
+                               grads: moce_head_grads, ws, ws_bytes: int, stream=None) -> None:
+    _check("moce_head_distill_backward",
+           load().moce_head_distill_backward(ctypes.byref(desc), _ptr(x), _ptr(weight), _ptr(shift), _ptr(classes),
+                                             _ptr(logits), _ptr(saved), _ptr(dloss), ctypes.byref(grads), _ptr(ws),
+                                             ws_bytes, _stream(stream)))
 
 
 def make_gradients(src, dst, sizes, dtypes) -> bytes:

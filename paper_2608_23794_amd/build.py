@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.hip", "prepare.hip", "pool.hip", "gate.hip", "mix.hip", "tilemix.hip", "mfmamix.hip",
            "gmix.hip", "dynamic.hip", "backward.hip", "bwdmfma.hip", "gather.hip", "dyntop.hip", "project.hip",
-           "gradclip.hip"]
+           "gradclip.hip", "headloss.hip", "groupnorm.hip"]
 LIB = os.path.join(HERE, "libmoce.so")
 OBJDIR = os.path.join(HERE, "_build")
 

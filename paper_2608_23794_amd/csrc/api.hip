@@ -702,6 +702,232 @@ moce_status moce_project_path(const moce_project_desc* desc, int32_t product, mo
   return MOCE_OK;
 }
 
+// ---- group norm --------------------------------------------------------------------
+
+namespace {
+
+moce_status check_group(const moce_group_norm_desc* d, moce::GroupShape* s) {
+  if (!d) return MOCE_ERR_NULL;
+  if (d->B < 1 || d->C < 1 || d->H < 1 || d->W < 1 || d->G < 1 || d->G > d->C || d->C % d->G != 0)
+    return MOCE_ERR_SHAPE;
+  if (d->act < MOCE_ACT_NONE || d->act > MOCE_ACT_SILU || !std::isfinite(d->eps) || d->eps < 0.f)
+    return MOCE_ERR_SHAPE;
+  if (d->dtype != MOCE_F32 && d->dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
+  if (d->layout != MOCE_NCHW && d->layout != MOCE_NHWC) return MOCE_ERR_LAYOUT;
+  if (d->H > INT_MAX / d->W) return MOCE_ERR_UNSUPPORTED;
+  s->B = d->B;
+  s->C = d->C;
+  s->HW = d->H * d->W;
+  s->G = d->G;
+  s->elem = d->dtype;
+  s->layout = s->C == 1 ? MOCE_NCHW : d->layout;   // the same memory
+  s->act = d->act;
+  s->eps = d->eps;
+  return moce::group_limits(*s) ? MOCE_OK : MOCE_ERR_UNSUPPORTED;
+}
+struct GroupBytes {
+  size_t x, channels, stats;
+  explicit GroupBytes(const moce::GroupShape& s)
+      : x((size_t)s.B * s.C * s.HW * (s.elem == MOCE_F32 ? 4 : 2)), channels((size_t)s.C * 4),
+        stats((size_t)2 * s.B * s.G * 4) {}
+};
+
+}  // namespace
+
+size_t moce_group_norm_workspace_bytes(const moce_group_norm_desc* desc) {
+  moce::GroupShape s;
+  if (check_group(desc, &s) != MOCE_OK) return 0;
+  return round_up(std::max<size_t>(moce::group_ws_bytes(s), 1));
+}
+
+moce_status moce_group_norm(const moce_group_norm_desc* desc, const void* x, const float* scale, const float* shift,
+                            void* y, float* stats, void* ws, size_t ws_bytes, hipStream_t stream) {
+  moce::GroupShape s;
+  const moce_status st = check_group(desc, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !y) return MOCE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(scale, 4) || !aligned(shift, 4) || !aligned(stats, 4))
+    return MOCE_ERR_ALIGN;
+  const size_t need = moce::group_ws_bytes(s);
+  if (!ws || ws_bytes < need) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const GroupBytes n(s);
+  if (!outputs_apart({{x == y ? nullptr : x, n.x}, {scale, n.channels}, {shift, n.channels}},
+                     {{y, n.x}, {stats, n.stats}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
+  return device_status(moce::launch_group_norm(s, x, scale, shift, y, stats, ws, stream));
+}
+
+size_t moce_group_norm_backward_workspace_bytes(const moce_group_norm_desc* desc) {
+  moce::GroupShape s;
+  if (check_group(desc, &s) != MOCE_OK) return 0;
+  return round_up(std::max<size_t>(moce::group_backward_ws_bytes(s), 1));
+}
+
+moce_status moce_group_norm_backward(const moce_group_norm_desc* desc, const void* x, const float* scale,
+                                     const float* shift, const float* stats, const void* dy,
+                                     const moce_group_norm_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream) {
+  moce::GroupShape s;
+  const moce_status st = check_group(desc, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !stats || !dy || !grads) return MOCE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(grads->dx, 16) || !aligned(scale, 4) || !aligned(shift, 4) ||
+      !aligned(stats, 4) || !aligned(grads->dscale, 4) || !aligned(grads->dshift, 4))
+    return MOCE_ERR_ALIGN;
+  const size_t need = moce::group_backward_ws_bytes(s);
+  if (!ws || ws_bytes < need) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const GroupBytes n(s);
+  // dx may take the place of dy or of x, each of which is then not an input to be kept
+  if (!outputs_apart({{x == grads->dx ? nullptr : x, n.x}, {dy == grads->dx ? nullptr : dy, n.x}, {scale, n.channels},
+                      {shift, n.channels}, {stats, n.stats}},
+                     {{grads->dx, n.x}, {grads->dscale, n.channels}, {grads->dshift, n.channels}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
+  // an output or the workspace over the input that dx replaces is one over dx
+  return device_status(moce::launch_group_norm_backward(s, x, scale, shift, stats, dy, *grads, ws, stream));
+}
+
+// ---- the losses of a head ------------------------------------------------------------
+
+namespace {
+
+moce_status check_head(const moce_head_desc* d, bool teacher, moce::HeadShape* s) {
+  if (!d) return MOCE_ERR_NULL;
+  if (d->P < 1 || d->C < 1 || d->V < 1 || d->K < 1 || (!teacher && d->K != 1)) return MOCE_ERR_SHAPE;
+  if (d->index_bytes != 4 && d->index_bytes != 8) return MOCE_ERR_SHAPE;
+  if (d->reduction != MOCE_LOSS_ROWS && d->reduction != MOCE_LOSS_MEAN) return MOCE_ERR_SHAPE;
+  if (d->dtype != MOCE_F32 && d->dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
+  if (teacher) {
+    if (!std::isfinite(d->temperature) || !(d->temperature > 0.f)) return MOCE_ERR_SHAPE;
+    if (d->teacher_dtype != MOCE_F32 && d->teacher_dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
+  } else if (!(d->smoothing >= 0.f && d->smoothing <= 1.f)) {
+    return MOCE_ERR_SHAPE;
+  }
+  s->P = d->P;
+  s->C = d->C;
+  s->V = d->V;
+  s->K = d->K;
+  s->elem = d->dtype;
+  s->telem = teacher ? d->teacher_dtype : MOCE_F32;
+  s->wide = d->index_bytes == 8;
+  s->mean = d->reduction == MOCE_LOSS_MEAN;
+  s->teacher = teacher;
+  s->smoothing = teacher ? 0.f : d->smoothing;
+  s->temperature = teacher ? d->temperature : 1.f;
+  return moce::head_limits(*s) ? MOCE_OK : MOCE_ERR_UNSUPPORTED;
+}
+struct HeadBytes {
+  size_t x, weight, shift, classes, logits, loss, saved, rows;
+  explicit HeadBytes(const moce::HeadShape& s) {
+    const size_t el = s.elem == MOCE_F32 ? 4 : 2, P = (size_t)s.P, entries = P * s.K;
+    x = P * s.C * el, weight = (size_t)s.V * s.C * el, shift = (size_t)s.V * 4, classes = entries * (s.wide ? 8 : 4);
+    logits = entries * (s.telem == MOCE_F32 ? 4 : 2), rows = s.mean ? 4 : P * 4, loss = rows;
+    saved = moce::head_saved_floats(s) * 4;
+  }
+};
+bool targets_aligned(const moce::HeadShape& s, const void* classes, const void* logits) {
+  return aligned(classes, s.wide ? 8 : 4) && aligned(logits, s.telem == MOCE_F32 ? 4 : 2);
+}
+
+moce_status head_forward(const moce_head_desc* desc, bool teacher, const void* x, const void* weight,
+                         const float* shift, const void* classes, const void* logits, float* loss, float* saved,
+                         void* ws, size_t ws_bytes, hipStream_t stream) {
+  moce::HeadShape s;
+  const moce_status st = check_head(desc, teacher, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !weight || !classes || (teacher && !logits) || !loss) return MOCE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(shift, 4) || !targets_aligned(s, classes, logits) ||
+      !aligned(loss, 4) || !aligned(saved, 4))
+    return MOCE_ERR_ALIGN;
+  const size_t need = moce::head_ws_bytes(s);
+  if (!ws || ws_bytes < need) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const HeadBytes n(s);
+  if (!outputs_apart({{x, n.x}, {weight, n.weight}, {shift, n.shift}, {classes, n.classes}, {logits, n.logits}},
+                     {{loss, n.loss}, {saved, n.saved}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
+  return device_status(moce::launch_head(s, x, weight, shift, {classes, logits}, loss, saved, ws, stream));
+}
+
+moce_status head_backward(const moce_head_desc* desc, bool teacher, const void* x, const void* weight,
+                          const float* shift, const void* classes, const void* logits, const float* saved,
+                          const float* dloss, const moce_head_grads* grads, void* ws, size_t ws_bytes,
+                          hipStream_t stream) {
+  moce::HeadShape s;
+  const moce_status st = check_head(desc, teacher, &s);
+  if (st != MOCE_OK) return st;
+  if (!x || !weight || !classes || (teacher && !logits) || !saved || !dloss || !grads) return MOCE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(shift, 4) || !targets_aligned(s, classes, logits) ||
+      !aligned(saved, 4) || !aligned(dloss, 4) || !aligned(grads->dx, 16) || !aligned(grads->dweight, 16) ||
+      !aligned(grads->dshift, 4))
+    return MOCE_ERR_ALIGN;
+  const size_t need = moce::head_backward_ws_bytes(s);
+  if (!ws || ws_bytes < need) return MOCE_ERR_WORKSPACE;
+  if (!aligned(ws, kAlign)) return MOCE_ERR_ALIGN;
+  const HeadBytes n(s);
+  if (!outputs_apart({{x, n.x}, {weight, n.weight}, {shift, n.shift}, {classes, n.classes}, {logits, n.logits},
+                      {saved, n.saved}, {dloss, n.rows}},
+                     {{grads->dx, n.x}, {grads->dweight, n.weight}, {grads->dshift, n.shift}, {ws, need}}))
+    return MOCE_ERR_SHAPE;
+  return device_status(
+      moce::launch_head_backward(s, x, weight, shift, {classes, logits}, saved, dloss, *grads, ws, stream));
+}
+
+// Sizes are those of the distillation, which asks no less: what the labels'
+// smoothing takes is counted for any K = 1.
+bool head_shape(const moce_head_desc* desc, moce::HeadShape* s) {
+  if (!desc) return false;
+  moce_head_desc d = *desc;
+  if (d.K == 1) {   // either; the labels' smoothing asks for more
+    d.smoothing = 1.f;
+    return check_head(&d, false, s) == MOCE_OK;
+  }
+  return check_head(&d, true, s) == MOCE_OK;
+}
+
+}  // namespace
+
+size_t moce_head_saved_floats(const moce_head_desc* desc) {
+  moce::HeadShape s;
+  return head_shape(desc, &s) ? moce::head_saved_floats(s) : 0;
+}
+
+size_t moce_head_workspace_bytes(const moce_head_desc* desc) {
+  moce::HeadShape s;
+  return head_shape(desc, &s) ? round_up(moce::head_ws_bytes(s)) : 0;
+}
+
+size_t moce_head_backward_workspace_bytes(const moce_head_desc* desc) {
+  moce::HeadShape s;
+  return head_shape(desc, &s) ? round_up(moce::head_backward_ws_bytes(s)) : 0;
+}
+
+moce_status moce_head_cross_entropy(const moce_head_desc* desc, const void* x, const void* weight, const float* shift,
+                                    const void* labels, float* loss, float* saved, void* ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  return head_forward(desc, false, x, weight, shift, labels, nullptr, loss, saved, ws, ws_bytes, stream);
+}
+
+moce_status moce_head_distill(const moce_head_desc* desc, const void* x, const void* weight, const float* shift,
+                              const void* classes, const void* logits, float* loss, float* saved, void* ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  return head_forward(desc, true, x, weight, shift, classes, logits, loss, saved, ws, ws_bytes, stream);
+}
+
+moce_status moce_head_cross_entropy_backward(const moce_head_desc* desc, const void* x, const void* weight,
+                                             const float* shift, const void* labels, const float* saved,
+                                             const float* dloss, const moce_head_grads* grads, void* ws,
+                                             size_t ws_bytes, hipStream_t stream) {
+  return head_backward(desc, false, x, weight, shift, labels, nullptr, saved, dloss, grads, ws, ws_bytes, stream);
+}
+
+moce_status moce_head_distill_backward(const moce_head_desc* desc, const void* x, const void* weight,
+                                       const float* shift, const void* classes, const void* logits,
+                                       const float* saved, const float* dloss, const moce_head_grads* grads, void* ws,
+                                       size_t ws_bytes, hipStream_t stream) {
+  return head_backward(desc, true, x, weight, shift, classes, logits, saved, dloss, grads, ws, ws_bytes, stream);
+}
+
 // ---- gradient norm and clipping --------------------------------------------------
 
 namespace {

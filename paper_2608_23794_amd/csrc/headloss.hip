@@ -1,0 +1,773 @@
+// The losses of a classification head, over labels or a teacher's largest
+// logits, and their gradients, without the logits kept.
+//
+// With z = x W^T + shift and a row's scale T, both losses are lse(z / T) less
+// the logits under a sparse target distribution q, and both gradients are
+// g (softmax(z / T) - q).  So one set of kernels has both; a label is one entry
+// of weight 1 - e (and e / V everywhere).
+//
+// The forward is the product x W^T (product.h) whose epilogue leaves a row's
+// running maximum and sum over the tile's classes instead of the tile;
+// k_head_rows joins a row's tiles and takes the logits of its targets by dot
+// products of their own.  The backward forms the product again, in pieces of
+// the classes; its epilogue writes g softmax, rounded, and sums it over the
+// rows for dshift.  k_head_targets puts the targets' elements right (from
+// float32 values, so that p - q loses no digits), and a piece then goes through
+// the products of dx (whose partial sums are kept in float32 from piece to
+// piece) and dweight.  8 P V C operations in all, bound by the matrix cores
+// where C and P are large.
+//
+// Logits are taken in base 2: u = (z + shift) log2(e) / T.
+#include "product.h"
+
+namespace moce {
+namespace {
+
+struct HeadArgs : GemmArgs {
+  float c1;              // log2(e) / T
+  // forward
+  float2* stat;          // [R][tc] maximum and sum of 2^(u - maximum)
+  float* sums;           // [R][tc] sums of z (nullptr: none)
+  // backward
+  const float* lse;      // a row's, at lse_ld row
+  int64_t lse_ld;
+  const float* grow;     // [R] g; 0: the row is left out, or weighs nothing
+  float even;            // e / V
+  float* colsum;         // [rows of waves][cols_ld] sums of dz (nullptr: none)
+  int64_t cols_ld;
+};
+
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// Maximum and sum of 2^(u - maximum); the maximum of nothing is -inf, its sum 0.
+struct Soft {
+  float m, s;
+};
+__device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ Soft join(Soft a, Soft b) {
+  const float m = fmaxf(a.m, b.m), r = finite_or_0(m);
+  return Soft{m, a.s * exp2_of(a.m - r) + b.s * exp2_of(b.m - r)};
+}
+
+// ---- forward epilogue ------------------------------------------------------------
+// A lane holds 4 FC classes of each of its FR rows; four lanes share a row's
+// classes of the wave, WC waves the tile's.  (NaN is not a maximum, but makes
+// the sum NaN.)
+template <typename T, int BYTES, int FR, int FC, int WR, int WC>
+struct HeadStats {
+  const HeadArgs& g;
+  int r0, c0, lane;
+  __device__ __forceinline__ HeadStats(const HeadArgs& g, int r0, int c0, int lane) : g(g), r0(r0), c0(c0), lane(lane) {}
+
+  template <typename L>
+  __device__ __forceinline__ void run(f32x4 (&acc)[FR][FC], L&& lds, int wave, int, int) {
+    static_assert(BYTES >= FR * 16 * 12, "a wave's rows");
+    float sh[FC][4];
+    bool in[FC][4];
+#pragma unroll
+    for (int j = 0; j < FC; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = c0 + 32 * (j / 2) + 8 * (lane >> 4) + 4 * (j % 2) + e;
+        in[j][e] = c < g.N;
+        sh[j][e] = g.shift ? g.shift[min(c, g.N - 1)] : 0.f;
+      }
+    float* mine = reinterpret_cast<float*>(lds(wave));
+#pragma unroll
+    for (int i = 0; i < FR; ++i) {
+      float u[FC][4], m = -INFINITY, total = 0.f;
+#pragma unroll
+      for (int j = 0; j < FC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = acc[i][j][e] + sh[j][e];
+          total += in[j][e] ? z : 0.f;
+          u[j][e] = in[j][e] ? z * g.c1 : -INFINITY;
+          m = fmaxf(m, u[j][e]);
+        }
+      m = fmaxf(m, __shfl_xor(m, 16, kWave));
+      m = fmaxf(m, __shfl_xor(m, 32, kWave));
+      const float r = finite_or_0(m);
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < FC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += exp2_of(u[j][e] - r);
+      s += __shfl_xor(s, 16, kWave);
+      s += __shfl_xor(s, 32, kWave);
+      total += __shfl_xor(total, 16, kWave);
+      total += __shfl_xor(total, 32, kWave);
+      if (lane < 16) {
+        float* to = mine + 3 * (16 * i + lane);
+        to[0] = m, to[1] = s, to[2] = total;
+      }
+    }
+    __syncthreads();
+    if (wave >= WR) return;
+    const int tile = c0 / (16 * WC * FC);
+    for (int r = lane; r < 16 * FR; r += kWave) {
+      if (r0 + r >= g.R) break;
+      Soft a{mine[3 * r], mine[3 * r + 1]};
+      float total = mine[3 * r + 2];
+#pragma unroll
+      for (int w = 1; w < WC; ++w) {
+        const float* o = reinterpret_cast<const float*>(lds(wave + w * WR)) + 3 * r;
+        a = join(a, Soft{o[0], o[1]});
+        total += o[2];
+      }
+      const int64_t at = (int64_t)(r0 + r) * g.tc + tile;
+      g.stat[at] = make_float2(a.m, a.s);
+      if (g.sums) g.sums[at] = total;
+    }
+  }
+};
+
+// ---- backward epilogue -----------------------------------------------------------
+// Eight classes a lane, in rows, as Finish has them: g (2^(u - lse) - e / V),
+// zeros behind the classes to the end of the line.
+template <typename T, int BYTES, int FR, int FC, int WR, int WC>
+struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
+  using F = Finish<T, BYTES, FR, FC, WR, WC>;
+  const HeadArgs& h;
+  __device__ __forceinline__ HeadGradient(const HeadArgs& g, int r0, int c0, int lane) : F(g, r0, c0, lane), h(g) {}
+
+  template <typename L>
+  __device__ __forceinline__ void run(f32x4 (&acc)[FR][FC], L&& lds, int wave, int lane, int) {
+    unsigned char* l = lds(wave);
+    const int c = this->c, left = h.N - c;   // classes from the lane's first on
+    float sh[8], sum[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sh[i] = h.shift ? h.shift[min(c + i, h.N - 1)] : 0.f;
+    T* y = static_cast<T*>(h.y);
+#pragma unroll
+    for (int f = 0; f < FR; f += F::kFrags) {
+      constexpr int kPer = 16 / F::kDown, kBatch = F::kBatch;
+#pragma unroll
+      for (int i = 0; i < F::kFrags; ++i)
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+          const int r = 16 * i + (lane & 15), ch = 8 * (j / 2) + 2 * (lane >> 4) + (j & 1);
+          *reinterpret_cast<f32x4*>(l + r * F::kPitch + ((ch ^ (r & 7)) << 4)) = acc[f + i][j];
+        }
+      for (int it = 0; it < F::kIters; it += kBatch) {
+        float v[kBatch][8], lse[kBatch], g[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int row = this->row(f * kPer + it + b), r = min(row, h.R - 1);
+          lse[b] = h.lse[r * h.lse_ld];
+          g[b] = row < h.R ? h.grow[r] : 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) this->value(l, it + b, v[b]);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float p = exp2_of((v[b][i] + sh[i]) * h.c1 - lse[b]);
+            v[b][i] = g[b] == 0.f || i >= left ? 0.f : g[b] * (p - h.even);
+            sum[i] += v[b][i];
+          }
+        if (left > 0) {
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const int row = this->row(f * kPer + it + b);
+            if (row >= h.R) continue;
+            T* to = y + row * h.ld + c;
+            if (c + 8 <= h.ld)
+              store8(to, v[b]);
+            else   // float32: a line may end after four
+              store4(to, v[b]);
+          }
+        }
+      }
+    }
+    if (!h.colsum) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int o = F::kAcross; o < kWave; o <<= 1) sum[i] += __shfl_xor(sum[i], o, kWave);
+    if (lane < F::kAcross) {
+      float* to = h.colsum + (int64_t)(this->r0 / (16 * FR)) * h.cols_ld + c;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) to[i] = sum[i];
+    }
+  }
+};
+
+// ---- targets ---------------------------------------------------------------------
+
+constexpr int kMaxEntries = 1024;   // of a teacher, a row
+constexpr int kWaves = kThreads / kWave;
+
+struct Targets {
+  const void *classes, *logits;
+  int K, V, wide, low;       // wide: classes of 64 bits; low: logits of 16
+  bool teacher;
+  float c1, label;           // log2(e) / T; the weight of a label
+
+  __device__ __forceinline__ int index(int64_t p, int k) const {   // -1: outside the classes
+    const int64_t at = p * K + k;
+    const int64_t v = wide ? static_cast<const int64_t*>(classes)[at] : static_cast<const int32_t*>(classes)[at];
+    return v >= 0 && v < V ? (int)v : -1;
+  }
+  __device__ __forceinline__ float logit(int64_t p, int k) const {
+    const int64_t at = p * K + k;
+    return low ? bf16_to_f32(static_cast<const uint16_t*>(logits)[at]) : static_cast<const float*>(logits)[at];
+  }
+};
+
+// A row's targets by one wave, kept in LDS: the classes (-1 for an entry that
+// counts for nothing or whose class came before) and their probabilities.
+// False where the row is left out.
+struct RowTargets {
+  int cls[kMaxEntries];
+  float q[kMaxEntries];
+};
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+__device__ __forceinline__ bool take_targets(const Targets& t, int64_t p, RowTargets& s, int lane) {
+  if (!t.teacher) {
+    const int i = t.index(p, 0);
+    if (lane == 0) s.cls[0] = i, s.q[0] = t.label;
+    wave_fence();
+    return i >= 0;
+  }
+  float m = -INFINITY;
+  for (int k = lane; k < t.K; k += kWave) {
+    const int i = t.index(p, k);
+    const float v = i >= 0 ? t.logit(p, k) * t.c1 : -INFINITY;
+    s.cls[k] = i, s.q[k] = v;
+    m = fmaxf(m, v);
+  }
+  m = finite_or_0(wave_max(m));
+  float sum = 0.f;
+  for (int k = lane; k < t.K; k += kWave) sum += s.q[k] = exp2_of(s.q[k] - m);
+  sum = wave_sum(sum);
+  wave_fence();
+  if (sum == 0.f) return false;
+  const float r = 1.f / sum;
+  // the first entry of a class has the sum over all of it
+  constexpr int kEach = kMaxEntries / kWave;
+  float q[kEach];
+  bool again[kEach];
+#pragma unroll
+  for (int n = 0; n < kEach; ++n) {
+    q[n] = 0.f, again[n] = false;
+    if (n * kWave >= t.K) continue;
+    const int k = min(n * kWave + lane, t.K - 1), i = s.cls[k];
+    for (int o = 0; o < t.K; ++o) {
+      const bool same = s.cls[o] == i;
+      again[n] = again[n] || (same && o < k);
+      q[n] += same ? s.q[o] : 0.f;
+    }
+  }
+  wave_fence();
+#pragma unroll
+  for (int n = 0; n < kEach; ++n) {
+    const int k = n * kWave + lane;
+    if (k < t.K) {
+      s.q[k] = q[n] * r;
+      if (again[n]) s.cls[k] = -1;
+    }
+  }
+  wave_fence();
+  return true;
+}
+
+// ---- the forward's rows ----------------------------------------------------------
+
+struct RowsArgs {
+  Targets t;
+  const void *x, *w;
+  const float* shift;
+  const float2* stat;
+  const float* sums;
+  float *rows, *code, *saved;   // code: 0 left out, 1 counts, 2 left out and not finite
+  int64_t P;
+  int C, tc;
+  float smoothing, factor;      // factor: T^2 ln 2
+};
+
+template <typename T>
+__device__ __forceinline__ float dot_row(const T* a, const T* b, int n, int lane) {
+  float s = 0.f;
+  int i = lane * 8;
+  for (; i + 8 <= n; i += 8 * kWave) {
+    float u[8], v[8];
+    load8(a + i, u);
+    load8(b + i, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(u[e], v[e], s);
+  }
+  for (int e = i; e < min(i + 8, n); ++e) s = fmaf(Elem<T>::to_f(a[e]), Elem<T>::to_f(b[e]), s);
+  return wave_sum(s);
+}
+
+// A workgroup takes a row: its statistics over the tiles, its targets' logits
+// (a wave each), its loss.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_head_rows(RowsArgs a) {
+  __shared__ RowTargets s;
+  __shared__ float u[kMaxEntries];
+  __shared__ Soft part[kWaves];
+  __shared__ float total[kWaves];
+  __shared__ int there, wild;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t p = blockIdx.x; p < a.P; p += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + p * a.C;
+    if (threadIdx.x == 0) wild = 0;
+    if (wave == 0) {
+      const bool ok = take_targets(a.t, p, s, lane);
+      if (lane == 0) there = ok;
+    }
+    __syncthreads();
+    if (!there) {   // uniform
+      if (a.saved) {
+        for (int c = threadIdx.x; c < a.C; c += kThreads)
+          if (!__builtin_isfinite(Elem<T>::to_f(x[c]))) wild = 1;
+        __syncthreads();
+      }
+      if (threadIdx.x == 0) {
+        a.rows[p] = 0.f;
+        a.code[p] = wild ? 2.f : 0.f;
+        if (a.saved) a.saved[p * (a.t.K + 1)] = INFINITY;
+      }
+      __syncthreads();
+      continue;
+    }
+    Soft m{-INFINITY, 0.f};
+    float sum = 0.f;
+    for (int i = threadIdx.x; i < a.tc; i += kThreads) {
+      const float2 o = a.stat[p * a.tc + i];
+      m = join(m, Soft{o.x, o.y});
+      if (a.sums) sum += a.sums[p * a.tc + i];
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+      m = join(m, Soft{__shfl_xor(m.m, o, kWave), __shfl_xor(m.s, o, kWave)});
+      sum += __shfl_xor(sum, o, kWave);
+    }
+    if (lane == 0) part[wave] = m, total[wave] = sum;
+    for (int k = wave; k < a.t.K; k += kWaves) {
+      const int i = s.cls[k];
+      if (i < 0) continue;
+      const float d = dot_row(x, static_cast<const T*>(a.w) + (int64_t)i * a.C, a.C, lane);
+      if (lane == 0) u[k] = (d + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      m = part[0], sum = total[0];
+      for (int w = 1; w < kWaves; ++w) m = join(m, part[w]), sum += total[w];
+      const float lse = m.m + log2f(m.s);
+      float l = 0.f;
+      for (int k = lane; k < a.t.K; k += kWave) {
+        const int i = s.cls[k];
+        if (i < 0) continue;
+        const float q = s.q[k];
+        if (a.t.teacher)
+          l += q == 0.f ? 0.f : q * (log2f(q) - u[k] + lse);
+        else
+          l = (lse - u[k]) * q;
+        if (a.saved) a.saved[p * (a.t.K + 1) + 1 + k] = u[k];
+      }
+      l = wave_sum(l);
+      if (lane == 0) {
+        if (a.sums && a.smoothing > 0.f) l += a.smoothing * (lse - sum / (float)a.t.V * a.t.c1);
+        a.rows[p] = l * a.factor;
+        a.code[p] = 1.f;
+        if (a.saved) a.saved[p * (a.t.K + 1)] = lse;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The mean over the rows that count, and what the backward wants to know of all
+// rows: their number, and whether a row that is left out is not finite.
+constexpr int kMeanThreads = 1024;
+__global__ void __launch_bounds__(kMeanThreads)
+k_head_mean(const float* __restrict__ rows, const float* __restrict__ code, int64_t P, float* __restrict__ loss,
+            float* __restrict__ tail) {
+  __shared__ double sums[kMeanThreads / kWave], counts[kMeanThreads / kWave];
+  __shared__ int wild;
+  if (threadIdx.x == 0) wild = 0;
+  __syncthreads();
+  double sum = 0., count = 0.;
+#pragma unroll 4
+  for (int64_t p = threadIdx.x; p < P; p += kMeanThreads) {
+    const float c = code[p];
+    sum += rows[p];
+    count += c == 1.f;
+    if (c == 2.f) wild = 1;
+  }
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) {
+    sum += __shfl_xor(sum, o, kWave);
+    count += __shfl_xor(count, o, kWave);
+  }
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum, counts[threadIdx.x >> 6] = count;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kMeanThreads / kWave; ++w) sum += sums[w], count += counts[w];
+  if (loss) *loss = count > 0. ? (float)(sum / count) : 0.f;
+  if (tail) tail[0] = (float)count, tail[1] = (float)wild;
+}
+
+// ---- the backward's rows ---------------------------------------------------------
+
+constexpr int kPrepBlocks = 1024;
+struct PrepArgs {
+  const void* x;
+  void* lines;                // x in lines of ld, rows that are left out as zeros
+  int ragged;                 // written always, else only where such a row is not finite
+  int64_t P;
+  int C, ld, K, mean;
+  float T;
+  const float *saved, *dloss;
+  float *grow, *gmax;         // gmax: [kPrepBlocks] largest |g|, finite ones
+  unsigned long long* fixed;  // [V] cleared (nullptr: none)
+  int V;
+};
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_head_prep(PrepArgs a) {
+  __shared__ float tops[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (a.fixed)
+    for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < a.V; i += (int64_t)gridDim.x * kThreads)
+      a.fixed[i] = 0;
+  const float* tail = a.saved + a.P * (a.K + 1);
+  const bool copy = a.lines && (a.ragged || tail[1] != 0.f);
+  float top = 0.f;
+  for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
+    const bool there = a.saved[p * (a.K + 1)] != INFINITY;
+    float g = 0.f;
+    if (there) g = a.T * (a.mean ? a.dloss[0] / tail[0] : a.dloss[p]);
+    if (lane == 0) a.grow[p] = g;
+    if (__builtin_isfinite(g)) top = fmaxf(top, fabsf(g));
+    if (!copy) continue;
+    const T* x = static_cast<const T*>(a.x) + p * a.C;
+    T* to = static_cast<T*>(a.lines) + p * a.ld;
+    for (int c = lane * Elem<T>::kVec; c < a.ld; c += kWave * Elem<T>::kVec) {
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (there) {
+        if (c + Elem<T>::kVec <= a.C) {
+          __builtin_memcpy(&v, x + c, 16);
+        } else {
+          T e[Elem<T>::kVec] = {};
+#pragma unroll
+          for (int i = 0; i < Elem<T>::kVec; ++i)
+            if (c + i < a.C) e[i] = x[c + i];
+          __builtin_memcpy(&v, e, 16);
+        }
+      }
+      *reinterpret_cast<u32x4*>(to + c) = v;
+    }
+  }
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+    a.gmax[blockIdx.x] = top;
+  }
+}
+
+// A unit for the sums of g q over the rows of a class: |sum| <= P max |g|, so
+// they fit 62 bits in units of 2^-62 of that bound, and whole numbers add up to
+// the same in any order.
+__device__ __forceinline__ int fixed_exponent(const float* gmax, int n, int64_t P, int lane) {
+  float top = 0.f;
+  for (int i = lane; i < n; i += kWave) top = fmaxf(top, gmax[i]);
+  top = wave_max(top);
+  return 61 - (64 - __clzll(P)) - (top > 0.f ? ilogbf(top) + 1 : 0);
+}
+
+struct TargetArgs {
+  Targets t;
+  const float *saved, *grow, *gmax;
+  int blocks;                 // of gmax
+  int64_t P, ld;
+  int v0, n;                  // the piece's classes
+  float even;
+  void* dz;
+  unsigned long long* fixed;  // nullptr: none
+};
+// The targets' elements of a piece of dz, a wave a row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_head_targets(TargetArgs a) {
+  __shared__ RowTargets rows[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  RowTargets& s = rows[wave];
+  const int unit = a.fixed ? fixed_exponent(a.gmax, a.blocks, a.P, lane) : 0;
+  for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
+    const float g = a.grow[p];
+    if (g == 0.f || !take_targets(a.t, p, s, lane)) continue;
+    const float* saved = a.saved + p * (a.t.K + 1);
+    const float lse = saved[0];
+    for (int k = lane; k < a.t.K; k += kWave) {
+      const int i = s.cls[k] - a.v0;
+      if (s.cls[k] < 0 || i < 0 || i >= a.n) continue;
+      const float q = s.q[k], d = g * (exp2_of(saved[1 + k] - lse) - a.even - q);
+      static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
+      const double w = (double)g * (double)q;
+      if (a.fixed && __builtin_isfinite(w))
+        atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, unit)));
+    }
+    wave_fence();
+  }
+}
+
+// dshift[v]: the sums over the rows' groups less the targets'.  16 classes a workgroup.
+__global__ void __launch_bounds__(kThreads)
+k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned long long* __restrict__ fixed,
+              const float* __restrict__ gmax, int blocks, int64_t P, float* __restrict__ out) {
+  __shared__ double s[kThreads];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, v = blockIdx.x * 16 + x;
+  const int unit = fixed_exponent(gmax, blocks, P, threadIdx.x & 63);
+  double t = 0.;
+  if (v < V)
+#pragma unroll 8
+    for (int i = y; i < groups; i += kThreads / 16) t += part[(int64_t)i * V + v];
+  s[threadIdx.x] = t;
+  __syncthreads();
+  if (y != 0 || v >= V) return;
+#pragma unroll
+  for (int i = 1; i < kThreads / 16; ++i) t += s[16 * i + x];
+  out[v] = (float)(t - ldexp((double)(long long)fixed[v], -unit));
+}
+
+// ---- launches --------------------------------------------------------------------
+
+// The gradient of the logits goes through the GPU in pieces of so many bytes,
+// which the infinity cache holds from the product that writes them to the two
+// that read them.
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;
+constexpr int kPieceClasses = 256;   // a multiple of every tile and of whole lines
+constexpr int64_t kMaxBlocks = 1 << 20;
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+struct Sizes {
+  const HeadShape& s;
+  int vec;
+  explicit Sizes(const HeadShape& s) : s(s), vec(s.elem == MOCE_F32 ? 4 : 8) {}
+  size_t el() const { return 16 / vec; }
+  int64_t up(int64_t n) const { return (n + vec - 1) / vec * vec; }
+  bool ragged() const { return s.C % vec != 0; }
+  size_t x_bytes() const { return up256((size_t)s.P * up(s.C) * el()); }
+  size_t w_bytes() const { return ragged() ? up256((size_t)s.V * up(s.C) * el()) : 0; }
+};
+
+struct FwdLayout {
+  Plan p;
+  int tc;
+  size_t x, w, stat, sums, rows, code, total;
+};
+FwdLayout fwd_layout(const HeadShape& s) {
+  const Sizes z(s);
+  FwdLayout l{};
+  l.p = plan(s.P, s.V, s.C, s.elem, false, false, 1);
+  l.tc = (int)ceil_div(s.V, kTile[l.p.tile].tc);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t here = at;
+    at += up256(n);
+    return here;
+  };
+  l.x = take(z.ragged() ? z.x_bytes() : 0);
+  l.w = take(z.w_bytes());
+  l.stat = take((size_t)s.P * l.tc * sizeof(float2));
+  l.sums = take(!s.teacher && s.smoothing > 0.f ? (size_t)s.P * l.tc * sizeof(float) : 0);
+  l.rows = take((size_t)s.P * sizeof(float));
+  l.code = take((size_t)s.P * sizeof(float));
+  l.total = at;
+  return l;
+}
+
+struct BwdLayout {
+  Plan pz, px, pw;
+  int n, pieces, groups;   // classes of a piece, pieces; groups of rows of dshift's sums
+  int64_t ld;              // of a piece of dz
+  size_t x, w, grow, gmax, fixed, cols, dz, part, dx, total;
+};
+BwdLayout bwd_layout(const HeadShape& s) {
+  const Sizes z(s);
+  BwdLayout l{};
+  const int64_t most = std::max<int64_t>(kPieceBytes / (int64_t)(s.P * z.el()) / kPieceClasses, 1) * kPieceClasses;
+  const int64_t each = ceil_div(ceil_div(s.V, ceil_div(s.V, most)), kPieceClasses) * kPieceClasses;
+  l.n = (int)std::min(each, s.V), l.pieces = (int)ceil_div(s.V, l.n), l.ld = z.up(l.n);
+  l.pz = plan(s.P, l.n, s.C, s.elem, false, false, 1);
+  l.px = plan(s.P, s.C, l.n, s.elem, z.ragged(), false);
+  l.pw = plan(l.n, s.C, s.P, s.elem, z.ragged(), true);
+  const int wave_rows = kTile[l.pz.tile].tr / 2;   // every tile has two waves down
+  l.groups = (int)ceil_div(s.P, kTile[l.pz.tile].tr) * (kTile[l.pz.tile].tr / wave_rows);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t here = at;
+    at += up256(n);
+    return here;
+  };
+  l.x = take(z.x_bytes());
+  l.w = take(z.w_bytes());
+  l.grow = take((size_t)s.P * sizeof(float));
+  l.gmax = take(kPrepBlocks * sizeof(float));
+  l.fixed = take((size_t)s.V * 8);
+  l.cols = take((size_t)l.groups * s.V * sizeof(float));
+  l.dz = take((size_t)s.P * l.ld * z.el());
+  l.dx = take(l.px.splits > 1 || l.pieces > 1 ? part_bytes(s.P, s.C, l.px) : 0);
+  l.part = take(l.pw.splits > 1 ? part_bytes(l.n, s.C, l.pw) : 0);
+  l.total = at;
+  return l;
+}
+
+float scale_of(const HeadShape& s) { return s.teacher ? s.temperature : 1.f; }
+
+Targets targets_of(const HeadShape& s, const HeadTargets& t) {
+  Targets r{};
+  r.classes = t.classes, r.logits = t.logits, r.K = s.K, r.V = (int)s.V, r.wide = s.wide;
+  r.low = s.telem == MOCE_BF16, r.teacher = s.teacher, r.c1 = (float)((double)kLog2e / scale_of(s));
+  r.label = 1.f - s.smoothing;
+  return r;
+}
+
+// The arguments of the logits of classes v0.. v0 + n, x and w in whole lines.
+HeadArgs logits(const HeadShape& s, const void* x, const void* w, const float* shift, int64_t v0, int64_t n) {
+  const Sizes z(s);
+  HeadArgs g{};
+  g.R = (int)s.P, g.N = (int)n, g.K = (int)s.C, g.klen = (int)ceil_div(s.C, 64) * 64;
+  g.a = Operand{x, z.up(s.C), 0, 0};
+  g.b = Operand{static_cast<const char*>(w) + v0 * z.up(s.C) * z.el(), z.up(s.C), 0, 0};
+  g.shift = shift ? shift + v0 : nullptr;
+  g.c1 = (float)((double)kLog2e / scale_of(s));
+  return g;
+}
+
+template <typename T>
+hipError_t forward(const HeadShape& s, const void* x, const void* w, const float* shift, const HeadTargets& t,
+                   float* loss, float* saved, char* ws, hipStream_t st) {
+  const Sizes z(s);
+  const FwdLayout l = fwd_layout(s);
+  const void *xl = x, *wl = w;
+  hipError_t e = hipSuccess;
+  if (z.ragged()) {
+    xl = ws + l.x, wl = ws + l.w;
+    e = launch_weight_lines(s.elem, x, s.P, s.C, ws + l.x, st);
+    if (e == hipSuccess) e = launch_weight_lines(s.elem, w, s.V, s.C, ws + l.w, st);
+    if (e != hipSuccess) return e;
+  }
+  HeadArgs g = logits(s, xl, wl, shift, 0, s.V);
+  g.stat = reinterpret_cast<float2*>(ws + l.stat);
+  g.sums = !s.teacher && s.smoothing > 0.f ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+  e = launch_product<T, true, true, HeadStats>(g, l.p, st);
+  if (e != hipSuccess) return e;
+  RowsArgs a{};
+  a.t = targets_of(s, t);
+  a.x = x, a.w = w, a.shift = shift, a.stat = g.stat, a.sums = g.sums, a.saved = saved;
+  a.rows = s.mean ? reinterpret_cast<float*>(ws + l.rows) : loss;
+  a.code = reinterpret_cast<float*>(ws + l.code);
+  a.P = s.P, a.C = (int)s.C, a.tc = l.tc, a.smoothing = s.smoothing;
+  a.factor = (float)(0.69314718055994531 * scale_of(s) * scale_of(s));
+  hipLaunchKernelGGL(k_head_rows<T>, dim3((unsigned)std::min(s.P, kMaxBlocks)), dim3(kThreads), 0, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || (!s.mean && !saved)) return e;
+  hipLaunchKernelGGL(k_head_mean, dim3(1), dim3(kMeanThreads), 0, st, a.rows, a.code, s.P, s.mean ? loss : nullptr,
+                     saved ? saved + s.P * (s.K + 1) : nullptr);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(const HeadShape& s, const void* x, const void* w, const float* shift, const HeadTargets& t,
+                    const float* saved, const float* dloss, const moce_head_grads& gr, char* ws, hipStream_t st) {
+  const Sizes z(s);
+  const BwdLayout l = bwd_layout(s);
+  const int blocks = (int)std::min<int64_t>(kPrepBlocks, ceil_div(s.P, kWaves));
+  float *grow = reinterpret_cast<float*>(ws + l.grow), *gmax = reinterpret_cast<float*>(ws + l.gmax);
+  unsigned long long* fixed = gr.dshift ? reinterpret_cast<unsigned long long*>(ws + l.fixed) : nullptr;
+  float* cols = gr.dshift ? reinterpret_cast<float*>(ws + l.cols) : nullptr;
+  {
+    PrepArgs a{};
+    a.x = x, a.lines = z.ragged() || gr.dweight ? ws + l.x : nullptr, a.ragged = z.ragged(), a.P = s.P;
+    a.C = (int)s.C, a.ld = (int)z.up(s.C), a.K = s.K, a.mean = s.mean, a.T = scale_of(s);
+    a.saved = saved, a.dloss = dloss, a.grow = grow, a.gmax = gmax, a.fixed = fixed, a.V = (int)s.V;
+    hipLaunchKernelGGL(k_head_prep<T>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
+  }
+  hipError_t e = hipGetLastError();
+  const void *xl = x, *wl = w;
+  if (z.ragged()) {
+    xl = ws + l.x, wl = ws + l.w;
+    if (e == hipSuccess) e = launch_weight_lines(s.elem, w, s.V, s.C, ws + l.w, st);
+  }
+  if (e != hipSuccess) return e;
+  const float even = s.teacher ? 0.f : s.smoothing / (float)s.V;
+  for (int i = 0; i < l.pieces; ++i) {
+    const int64_t v0 = (int64_t)i * l.n, n = std::min<int64_t>(l.n, s.V - v0);
+    HeadArgs g = logits(s, xl, wl, shift, v0, n);
+    g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.even = even;
+    g.y = ws + l.dz, g.ld = l.ld, g.colsum = cols ? cols + v0 : nullptr, g.cols_ld = s.V;
+    e = launch_product<T, true, true, HeadGradient>(g, l.pz, st);
+    if (e != hipSuccess) return e;
+    TargetArgs a{};
+    a.t = targets_of(s, t);
+    a.saved = saved, a.grow = grow, a.gmax = gmax, a.blocks = blocks, a.P = s.P, a.ld = l.ld;
+    a.v0 = (int)v0, a.n = (int)n, a.even = even, a.dz = ws + l.dz, a.fixed = fixed;
+    hipLaunchKernelGGL(k_head_targets<T>, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
+                       0, st, a);
+    e = hipGetLastError();
+    if (e == hipSuccess && gr.dx) {
+      LineProduct p{};
+      p.a = ws + l.dz, p.lda = l.ld, p.a_along = true;
+      p.b = static_cast<const char*>(wl) + v0 * z.up(s.C) * z.el(), p.ldb = z.up(s.C);
+      p.R = (int)s.P, p.N = (int)s.C, p.K = (int)n, p.tile = l.px.tile, p.splits = l.px.splits, p.klen = l.px.klen;
+      p.y = gr.dx;
+      if (l.px.splits > 1 || l.pieces > 1)
+        p.part = reinterpret_cast<float*>(ws + l.dx), p.add = i > 0, p.join = i + 1 == l.pieces;
+      e = launch_line_product(s.elem, p, st);
+    }
+    if (e == hipSuccess && gr.dweight) {
+      LineProduct p{};
+      p.a = ws + l.dz, p.lda = l.ld, p.b = xl, p.ldb = z.up(s.C);
+      if (!z.ragged()) p.pick = saved + s.P * (s.K + 1) + 1, p.other = ws + l.x;
+      p.R = (int)n, p.N = (int)s.C, p.K = (int)s.P, p.tile = l.pw.tile, p.splits = l.pw.splits, p.klen = l.pw.klen;
+      p.y = static_cast<char*>(gr.dweight) + v0 * s.C * z.el();
+      if (l.pw.splits > 1) p.part = reinterpret_cast<float*>(ws + l.part), p.join = true;
+      e = launch_line_product(s.elem, p, st);
+    }
+    if (e != hipSuccess) return e;
+  }
+  if (cols)
+    hipLaunchKernelGGL(k_head_dshift, dim3((unsigned)ceil_div(s.V, 16)), dim3(kThreads), 0, st, cols, l.groups,
+                       (int)s.V, fixed, gmax, blocks, s.P, gr.dshift);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool head_limits(const HeadShape& s) {
+  constexpr int64_t kCh = 1 << 20;
+  return s.P <= (int64_t)1 << 24 && s.C <= kCh && s.V <= kCh && s.K <= kMaxEntries &&
+         s.V <= ((int64_t)1 << 35) / s.C && s.P <= ((int64_t)1 << 35) / s.V && s.P <= ((int64_t)1 << 33) / s.C;
+}
+
+size_t head_saved_floats(const HeadShape& s) { return (size_t)s.P * (s.K + 1) + 2; }
+size_t head_ws_bytes(const HeadShape& s) { return fwd_layout(s).total; }
+size_t head_backward_ws_bytes(const HeadShape& s) { return bwd_layout(s).total; }
+
+hipError_t launch_head(const HeadShape& s, const void* x, const void* w, const float* shift, const HeadTargets& t,
+                       float* loss, float* saved, void* ws, hipStream_t st) {
+  char* base = static_cast<char*>(ws);
+  return s.elem == MOCE_F32 ? forward<float>(s, x, w, shift, t, loss, saved, base, st)
+                            : forward<uint16_t>(s, x, w, shift, t, loss, saved, base, st);
+}
+
+hipError_t launch_head_backward(const HeadShape& s, const void* x, const void* w, const float* shift,
+                                const HeadTargets& t, const float* saved, const float* dloss, const moce_head_grads& gr,
+                                void* ws, hipStream_t st) {
+  char* base = static_cast<char*>(ws);
+  return s.elem == MOCE_F32 ? backward<float>(s, x, w, shift, t, saved, dloss, gr, base, st)
+                            : backward<uint16_t>(s, x, w, shift, t, saved, dloss, gr, base, st);
+}
+
+}  // namespace moce

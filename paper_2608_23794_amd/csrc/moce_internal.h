@@ -315,6 +315,60 @@ hipError_t launch_project_backward(const ProjectShape& s, const void* x, const v
                                    const void* z, const void* dy, const moce_project_grads& gr, void* ws,
                                    hipStream_t st);
 
+// out[r][c] = sum_k A[r][k] B[k][c], B by rows of ldb elements, A by rows of lda
+// (a_along) or [k][r]; rows of whole 16 bytes, cut as product.h's plan() has it
+// (tile, splits, klen).  part: [splits][R][N] float32, written or (add) added to,
+// and joined into y; without join y is not written.  Without part y is written directly.
+struct LineProduct {
+  const void *a, *b;
+  int64_t lda, ldb;
+  const float* pick;     // where *pick is not 0, b lies at `other` (nullptr: no choice)
+  const void* other;
+  int R, N, K, tile, splits, klen;
+  void* y;               // [R][N]
+  float* part;
+  bool a_along, add, join;
+};
+hipError_t launch_line_product(int elem, const LineProduct& p, hipStream_t st);
+// The weight [O][C] in rows of whole 16 bytes.
+hipError_t launch_weight_lines(int elem, const void* w, int64_t O, int64_t C, void* out, hipStream_t st);
+
+// The losses of a classification head and their gradients (headloss.hip).
+struct HeadShape {
+  int64_t P, C, V;
+  int K, elem, telem, wide;   // wide: labels and classes of 64 bits
+  bool mean, teacher;
+  float smoothing, temperature;
+};
+struct HeadTargets {
+  const void* classes;   // labels [P], or the teacher's classes [P][K]
+  const void* logits;    // the teacher's [P][K]
+};
+bool head_limits(const HeadShape& s);
+size_t head_saved_floats(const HeadShape& s);
+size_t head_ws_bytes(const HeadShape& s);
+size_t head_backward_ws_bytes(const HeadShape& s);
+hipError_t launch_head(const HeadShape& s, const void* x, const void* w, const float* shift, const HeadTargets& t,
+                       float* loss, float* saved, void* ws, hipStream_t st);
+hipError_t launch_head_backward(const HeadShape& s, const void* x, const void* w, const float* shift,
+                                const HeadTargets& t, const float* saved, const float* dloss, const moce_head_grads& gr,
+                                void* ws, hipStream_t st);
+
+// Group norm with an activation and its gradients (groupnorm.hip).
+struct GroupShape {
+  int64_t B, C, HW, G;
+  int elem, layout, act;
+  float eps;
+};
+bool group_limits(const GroupShape& s);
+size_t group_ws_bytes(const GroupShape& s);
+hipError_t launch_group_norm(const GroupShape& s, const void* x, const float* scale, const float* shift, void* y,
+                             float* stats, void* ws, hipStream_t st);
+size_t group_backward_ws_bytes(const GroupShape& s);
+hipError_t launch_group_norm_backward(const GroupShape& s, const void* x, const float* scale, const float* shift,
+                                      const float* stats, const void* dy, const moce_group_norm_grads& gr, void* ws,
+                                      hipStream_t st);
+
 // The norm of a list of gradients and their clipping (gradclip.hip), over a validated list.
 size_t gradient_ws_bytes(const moce_gradient* g, int count);
 hipError_t launch_gradient_norm(const moce_gradient* g, int count, float* norm, void* ws, hipStream_t st);

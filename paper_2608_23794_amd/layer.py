@@ -5,10 +5,12 @@ selected logits, gate parameters), prepares the supports once with
 ``moce_support_prepare`` and then forwards batches with ``moce_forward`` or
 the individual ``moce_pool`` / ``moce_gate`` / ``moce_mix`` calls.
 ``ProjectLayer`` is a dense projection beside it (``moce_project`` and its
-backward), and ``gradient_norm`` / ``clip_gradients`` take the global norm of
-the gradients of both (``moce_gradient_norm`` / ``moce_gradient_clip``).  Torch
-provides device memory and the current stream; every step of the layer runs in
-libmoce's HIP kernels.
+backward), ``GroupNormLayer`` a normalisation with an activation
+(``moce_group_norm``), ``HeadLoss`` the losses of a classification head against
+labels or a teacher (``moce_head_*``), and ``gradient_norm`` /
+``clip_gradients`` take the global norm of the gradients of all of them
+(``moce_gradient_norm`` / ``moce_gradient_clip``).  Torch provides device memory
+and the current stream; every step of the layers runs in libmoce's HIP kernels.
 """
 from __future__ import annotations
 
@@ -414,6 +416,268 @@ class ProjectLayer:
                                          mb.make_project_grads(dweight=out["dweight"], dscale=out["dscale"]), ws, n,
                                          stream)
         return out
+
+
+class GroupNormLayer:
+    """Group norm with an activation: y = act(scale (x - mean) rstd + shift), mean and rstd over an image's positions
+    and the channels of a group.
+
+    scale and shift: float32 [C] on the GPU, or None; act: "none", "relu", "gelu" or "silu".  x: float32 or bfloat16,
+    [B, C, H, W] for layout "nchw"; [B, ..., C] for "nhwc" (images, tokens, or rows [B, C]).  The layer keeps the
+    tensors it is given: updating them in place updates the layer."""
+
+    def __init__(self, groups: int, scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                 eps: float = 1e-5, act: str = "none", layout: str = "nhwc"):
+        if act not in _ACT or layout not in _LAYOUT:
+            raise ValueError(f"act {act!r}, layout {layout!r}")
+        if groups < 1 or not math.isfinite(eps) or eps < 0.0:
+            raise ValueError(f"groups {groups}, eps {eps}")
+        self.C = self.device = None        # where there are no parameters, every x says them
+        for name, t in (("scale", scale), ("shift", shift)):
+            if t is None:
+                continue
+            if t.dim() != 1 or not t.is_cuda:
+                raise ValueError(f"{name} has to be a float32 [C] tensor on the GPU, got {t.dtype} {tuple(t.shape)} "
+                                 f"on {t.device}")
+            if self.C is None:
+                self.C, self.device = t.shape[0], t.device
+            _need(name, t, (self.C,), torch.float32, self.device)
+        if self.C is not None and (self.C == 0 or self.C % groups):
+            raise ValueError(f"{self.C} channels in {groups} groups")
+        self.groups, self.scale, self.shift, self.eps, self.act, self.layout = groups, scale, shift, eps, act, layout
+
+    def desc(self, x_shape, dtype) -> mb.moce_group_norm_desc:
+        """The call's descriptor for an x of this shape and type."""
+        s = tuple(x_shape)
+        if dtype not in _DTYPE_OF:
+            raise ValueError(f"x has to be float32 or bfloat16, got {dtype}")
+        if self.layout == "nchw":
+            if len(s) != 4:
+                raise ValueError(f"x has to be [B, C, H, W], got {s}")
+            B, C, H, W = s
+        else:
+            if len(s) < 2:
+                raise ValueError(f"x has to be [B, ..., C], got {s}")
+            B, C, H, W = s[0], s[-1], math.prod(s[1:-1]), 1
+        if C != self.C if self.C is not None else C == 0 or C % self.groups:
+            raise ValueError(f"x of {C} channels in {self.groups} groups, {self.C} parameters")
+        return mb.moce_group_norm_desc(B, C, H, W, self.groups, _DTYPE_OF[dtype], _LAYOUT[self.layout],
+                                       _ACT[self.act], self.eps)
+
+    def workspace_bytes(self, x_shape, dtype) -> int:
+        return mb.moce_group_norm_workspace_bytes(self.desc(x_shape, dtype))
+
+    def backward_workspace_bytes(self, x_shape, dtype) -> int:
+        return mb.moce_group_norm_backward_workspace_bytes(self.desc(x_shape, dtype))
+
+    def new_stats(self, x_shape, device: Optional[torch.device] = None) -> torch.Tensor:
+        """What a forward leaves for the backward of an x of this shape: means and rstd, [2, B, G]."""
+        return torch.empty((2, x_shape[0], self.groups), dtype=torch.float32, device=self.device or device or "cuda")
+
+    def _check(self, x: torch.Tensor) -> mb.moce_group_norm_desc:
+        desc = self.desc(x.shape, x.dtype)
+        if not x.is_cuda:
+            raise ValueError(f"x has to be on the GPU, got one on {x.device}")
+        _need("x", x, x.shape, x.dtype, self.device or x.device)
+        return desc
+
+    def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """moce_group_norm.  stats, where given, receives what the backward needs; y may be x."""
+        desc, dev = self._check(x), x.device
+        if y is None:
+            y = torch.empty_like(x)
+        _need("y", y, x.shape, x.dtype, dev)
+        if stats is not None:
+            _need("stats", stats, (2, x.shape[0], self.groups), torch.float32, dev)
+        if x.numel() == 0:
+            if stats is not None:
+                stats.fill_(math.nan)      # of no elements
+            return y
+        with _on(dev):
+            n = mb.moce_group_norm_workspace_bytes(desc)
+            ws, n = _given_workspace(ws, dev) if ws is not None else (
+                torch.empty(n, dtype=torch.uint8, device=dev), n)
+            mb.moce_group_norm(desc, x, self.scale, self.shift, y, stats, ws, n, _raw_stream(dev.index))
+        return y
+
+    def backward(self, x: torch.Tensor, dy: torch.Tensor, stats: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                 ws: Optional[torch.Tensor] = None) -> dict:
+        """moce_group_norm_backward: dx, and dscale and dshift where the layer has them; dx may be dy or x."""
+        desc, dev = self._check(x), x.device
+        _need("dy", dy, x.shape, x.dtype, dev)
+        _need("stats", stats, (2, x.shape[0], self.groups), torch.float32, dev)
+        if dx is None:
+            dx = torch.empty_like(x)
+        _need("dx", dx, x.shape, x.dtype, dev)
+        out = {"dx": dx}
+        if self.scale is not None:
+            out["dscale"] = torch.empty(self.C, dtype=torch.float32, device=dev)
+        if self.shift is not None:
+            out["dshift"] = torch.empty(self.C, dtype=torch.float32, device=dev)
+        if x.numel() == 0:
+            for t in out.values():
+                t.zero_()
+            return out
+        with _on(dev):
+            n = mb.moce_group_norm_backward_workspace_bytes(desc)
+            ws, n = _given_workspace(ws, dev) if ws is not None else (
+                torch.empty(n, dtype=torch.uint8, device=dev), n)
+            mb.moce_group_norm_backward(desc, x, self.scale, self.shift, stats, dy, mb.make_group_norm_grads(**out),
+                                        ws, n, _raw_stream(dev.index))
+        return out
+
+
+_REDUCTION = {"mean": mb.MOCE_LOSS_MEAN, "rows": mb.MOCE_LOSS_ROWS}
+_INDEX_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+class HeadLoss:
+    """The losses of a classification head with logits x W^T + shift, and their gradients, without the logits kept.
+
+    weight: [V, C], float32 or bfloat16, on the GPU; shift: float32 [V] or None; reduction "mean" (a loss [1], the
+    mean over the rows that count) or "rows" (a loss of every row).  x: [..., C].  A label outside [0, V) leaves its
+    row out, and so does a teacher of whose entries none has a class in [0, V) and a logit above minus infinity.  The
+    head keeps the tensors it is given: updating them in place updates the head.  ProjectLayer(weight, None, shift)
+    gives the logits."""
+
+    def __init__(self, weight: torch.Tensor, shift: Optional[torch.Tensor] = None, reduction: str = "mean"):
+        if reduction not in _REDUCTION:
+            raise ValueError(f"reduction {reduction!r}")
+        if weight.dim() != 2 or weight.dtype not in _DTYPE_OF or not weight.is_cuda or weight.numel() == 0:
+            raise ValueError(f"weight has to be a float32 or bfloat16 [V, C] tensor on the GPU, got {weight.dtype} "
+                             f"{tuple(weight.shape)} on {weight.device}")
+        self.V, self.C = weight.shape
+        self.dtype, self.device = weight.dtype, weight.device
+        _need("weight", weight, weight.shape, self.dtype, self.device)
+        if shift is not None:
+            _need("shift", shift, (self.V,), torch.float32, self.device)
+        self.weight, self.shift, self.reduction = weight, shift, reduction
+
+    def desc(self, x_shape, entries: int = 1, index=torch.int64, teacher=torch.float32, smoothing: float = 0.0,
+             temperature: float = 1.0) -> mb.moce_head_desc:
+        """The call's descriptor for an x of this shape, of so many entries of a teacher a row (1 for labels)."""
+        if len(x_shape) < 1 or x_shape[-1] != self.C:
+            raise ValueError(f"x has to be [..., {self.C}], got {tuple(x_shape)}")
+        return mb.moce_head_desc(math.prod(x_shape[:-1]), self.C, self.V, entries, _DTYPE_OF[self.dtype],
+                                 _DTYPE_OF[teacher], _INDEX_BYTES[index], _REDUCTION[self.reduction], smoothing,
+                                 temperature, 0)
+
+    def new_saved(self, x_shape, entries: int = 1) -> torch.Tensor:
+        """What a forward leaves for the backward: float32 [rows (entries + 1) + 2]."""
+        return torch.empty(math.prod(x_shape[:-1]) * (entries + 1) + 2, dtype=torch.float32, device=self.device)
+
+    def workspace_bytes(self, x_shape, entries: int = 1) -> int:
+        return mb.moce_head_workspace_bytes(self.desc(x_shape, entries))
+
+    def backward_workspace_bytes(self, x_shape, entries: int = 1) -> int:
+        return mb.moce_head_backward_workspace_bytes(self.desc(x_shape, entries))
+
+    def _targets(self, x, classes, logits, smoothing, temperature):
+        """The call's descriptor, from checked tensors."""
+        rows = tuple(x.shape[:-1])
+        if not isinstance(classes, torch.Tensor) or classes.dtype not in _INDEX_BYTES:
+            raise ValueError(f"{'labels' if logits is None else 'classes'} have to be an int32 or int64 tensor")
+        if logits is None:
+            if not 0.0 <= smoothing <= 1.0:
+                raise ValueError(f"smoothing {smoothing}")
+            desc = self.desc(x.shape, 1, classes.dtype, smoothing=smoothing)
+            _need("labels", classes, rows, classes.dtype, self.device)
+        else:
+            if not (math.isfinite(temperature) and temperature > 0.0):
+                raise ValueError(f"temperature {temperature}")
+            if classes.dim() != len(rows) + 1 or classes.shape[-1] < 1 or logits.dtype not in _DTYPE_OF:
+                raise ValueError(f"classes and logits have to be [..., K], logits of float32 or bfloat16, got "
+                                 f"{tuple(classes.shape)}, {logits.dtype} {tuple(logits.shape)}")
+            K = classes.shape[-1]
+            desc = self.desc(x.shape, K, classes.dtype, logits.dtype, temperature=temperature)
+            _need("classes", classes, rows + (K,), classes.dtype, self.device)
+            _need("logits", logits, rows + (K,), logits.dtype, self.device)
+        _need("x", x, x.shape, self.dtype, self.device)
+        return desc
+
+    def _loss_shape(self, x):
+        return (1,) if self.reduction == "mean" else tuple(x.shape[:-1])
+
+    def _forward(self, x, classes, logits, smoothing, temperature, saved, ws):
+        desc = self._targets(x, classes, logits, smoothing, temperature)
+        if saved is not None:
+            _need("saved", saved, (desc.P * (desc.K + 1) + 2,), torch.float32, self.device)
+        loss = torch.empty(self._loss_shape(x), dtype=torch.float32, device=self.device)
+        if x.numel() == 0:
+            if saved is not None:
+                saved.zero_()
+            return loss.zero_()
+        with _on(self.device):
+            n = mb.moce_head_workspace_bytes(desc)
+            ws, n = _given_workspace(ws, self.device) if ws is not None else (
+                torch.empty(n, dtype=torch.uint8, device=self.device), n)
+            stream = _raw_stream(self.device.index)
+            if logits is None:
+                mb.moce_head_cross_entropy(desc, x, self.weight, self.shift, classes, loss, saved, ws, n, stream)
+            else:
+                mb.moce_head_distill(desc, x, self.weight, self.shift, classes, logits, loss, saved, ws, n, stream)
+        return loss
+
+    def _backward(self, x, classes, logits, smoothing, temperature, saved, dloss, dx, dweight, ws):
+        desc = self._targets(x, classes, logits, smoothing, temperature)
+        _need("saved", saved, (desc.P * (desc.K + 1) + 2,), torch.float32, self.device)
+        shape = self._loss_shape(x)
+        if dloss is None:
+            dloss = torch.ones(shape, dtype=torch.float32, device=self.device)
+        _need("dloss", dloss, shape, torch.float32, self.device)
+        if dx is None:
+            dx = torch.empty_like(x)
+        _need("dx", dx, x.shape, self.dtype, self.device)
+        if dweight is None:
+            dweight = torch.empty_like(self.weight)
+        _need("dweight", dweight, self.weight.shape, self.dtype, self.device)
+        out = {"dx": dx, "dweight": dweight}
+        if self.shift is not None:
+            out["dshift"] = torch.empty_like(self.shift)
+        if x.numel() == 0:
+            for t in out.values():
+                t.zero_()
+            return out
+        with _on(self.device):
+            n = mb.moce_head_backward_workspace_bytes(desc)
+            ws, n = _given_workspace(ws, self.device) if ws is not None else (
+                torch.empty(n, dtype=torch.uint8, device=self.device), n)
+            stream, grads = _raw_stream(self.device.index), mb.make_head_grads(**out)
+            if logits is None:
+                mb.moce_head_cross_entropy_backward(desc, x, self.weight, self.shift, classes, saved, dloss, grads,
+                                                    ws, n, stream)
+            else:
+                mb.moce_head_distill_backward(desc, x, self.weight, self.shift, classes, logits, saved, dloss, grads,
+                                              ws, n, stream)
+        return out
+
+    def cross_entropy(self, x: torch.Tensor, labels: torch.Tensor, smoothing: float = 0.0,
+                      saved: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """moce_head_cross_entropy: the loss against labels [...] (int32 or int64), smoothed.  saved (new_saved),
+        where given, receives what the backward needs."""
+        return self._forward(x, labels, None, smoothing, 1.0, saved, ws)
+
+    def cross_entropy_backward(self, x: torch.Tensor, labels: torch.Tensor, saved: torch.Tensor,
+                               dloss: Optional[torch.Tensor] = None, smoothing: float = 0.0,
+                               dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                               ws: Optional[torch.Tensor] = None) -> dict:
+        """moce_head_cross_entropy_backward: dx, dweight, and dshift where the head has it, for an upstream dloss of
+        the loss's shape (None: ones)."""
+        return self._backward(x, labels, None, smoothing, 1.0, saved, dloss, dx, dweight, ws)
+
+    def distill(self, x: torch.Tensor, classes: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0,
+                saved: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """moce_head_distill: the loss against a teacher's K logits a row, [..., K] (float32 or bfloat16), and their
+        classes (int32 or int64).  saved (new_saved), where given, receives what the backward needs."""
+        return self._forward(x, classes, logits, 0.0, temperature, saved, ws)
+
+    def distill_backward(self, x: torch.Tensor, classes: torch.Tensor, logits: torch.Tensor, saved: torch.Tensor,
+                         dloss: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                         dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None) -> dict:
+        """moce_head_distill_backward: as cross_entropy_backward, for the teacher's entries."""
+        return self._backward(x, classes, logits, 0.0, temperature, saved, dloss, dx, dweight, ws)
 
 
 _dtype = operator.attrgetter("dtype")

@@ -1,0 +1,432 @@
+"""The losses of a classification head and their gradients on the GPU, against float64."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_23794_amd import binding as mb
+from paper_2608_23794_amd.layer import HeadLoss
+
+pytestmark = pytest.mark.gpu
+
+F, H = torch.float32, torch.bfloat16
+HALF = {F: 2.0 ** -24, H: 2.0 ** -8}
+
+
+def make(P, C, V, dtype, shift=True, seed=0, spread=2.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(P, C, generator=g, device="cuda").to(dtype)
+    w = (torch.randn(V, C, generator=g, device="cuda") * spread * C ** -0.5).to(dtype)
+    b = torch.randn(V, generator=g, device="cuda") * 0.5 if shift else None
+    return x, w, b, g
+
+
+def entries(P, K, V, g, dtype=F):
+    """K classes a row, repeated ones among them, and their logits."""
+    cls = torch.randint(0, V, (P, K), generator=g, device="cuda")
+    return cls, (torch.randn(P, K, generator=g, device="cuda") * 2).to(dtype)
+
+
+def reference(x, w, b, target, there, T, dloss, mean, teacher):
+    """In float64: target [P, V] the distribution to be met, there [P] the rows that count."""
+    ok = there.unsqueeze(1)
+    xd = torch.where(ok, x.double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+    wd = w.double()
+    s = torch.matmul(xd, wd.t().contiguous())
+    size = torch.matmul(xd.abs(), wd.abs().t().contiguous())
+    if b is not None:
+        s += b.double()
+    s /= T
+    logp = torch.log_softmax(s, 1)
+    cross = torch.where(target == 0, torch.zeros_like(s), target * logp)
+    rows = -cross.sum(1)
+    if teacher:
+        rows = T * T * (rows + torch.xlogy(target, target).sum(1))
+    rows = torch.where(there, rows, torch.zeros_like(rows))
+    count = max(1, int(there.sum()))
+    loss = (rows.sum() / count).reshape(1) if mean else rows
+    g = dloss.double() / count if mean else dloss.double()
+    g = torch.where(there, g.expand(len(there)) * T, torch.zeros((), dtype=torch.float64, device="cuda")).unsqueeze(1)
+    p = torch.exp(logp)
+    dz = g * (p - target)
+    # the logits' sums of C products are off by C steps of their sizes' sum at most, and a few steps more of
+    # themselves in base 2; so the exponents
+    C = x.shape[1]
+    size = torch.where(s == -math.inf, torch.zeros_like(s), s.abs() * 8 + size * (C + 4) / T)
+    off = size.max(1, keepdim=True)[0] * 2.0 ** -24 + 2.0 ** -21
+    lse = torch.logsumexp(s, 1)
+    lse = torch.where(lse.abs() < math.inf, lse.abs(), torch.zeros_like(lse))
+    terms = 2 * off.squeeze(1) + 2.0 ** -21 * (1 + lse)
+    if teacher:     # the sizes of log q beside
+        terms = terms + 2.0 ** -21 * torch.xlogy(target, target).abs().sum(1)
+    tol_rows = torch.where(there, (T * T if teacher else 1.0) * terms + 2.0 ** -22 * rows.abs(), torch.zeros_like(rows))
+    tol_loss = tol_rows.sum().reshape(1) / count + 2.0 ** -23 * loss.abs() if mean else tol_rows
+    # dz before its rounding, then rounded to the operands' type (up to 2^-100 it may be lost)
+    e = g.abs() * (p * 4 * off + 2.0 ** -21 * (p + target))
+    r = e + (dz.abs() + e) * (HALF[x.dtype] if x.dtype == H else 2.0 ** -23)
+    out = {"loss": loss, "dx": torch.matmul(dz, wd), "dweight": torch.matmul(dz.t().contiguous(), xd), "dshift": dz.sum(0)}
+    tol = {"loss": tol_loss}
+    acc_x, acc_w = (w.shape[0] + 8) * 2.0 ** -24, (x.shape[0] + 8) * 2.0 ** -24
+    tol["dx"] = torch.matmul(r + dz.abs() * acc_x, wd.abs())
+    tol["dweight"] = torch.matmul((r + dz.abs() * acc_w).t().contiguous(), xd.abs())
+    for n in ("dx", "dweight"):
+        tol[n] = tol[n] * 1.01 + HALF[x.dtype] * (out[n].abs() + tol[n]) + 2.0 ** -100
+    # p and the targets are added up apart
+    tol["dshift"] = (e + g.abs() * (p + target) * (64 * 2.0 ** -24 + 2.0 ** -23)).sum(0) + 2.0 ** -23 * out["dshift"].abs()
+    return out, tol
+
+
+def check(got, want, tol):
+    for n, t in got.items():
+        d = (t.double() - want[n]).abs()
+        assert (d <= tol[n]).all(), (n, float((d / tol[n].clamp(min=1e-300)).max()))
+
+
+def label_target(labels, V, smoothing):
+    there = (labels >= 0) & (labels < V)
+    t = torch.full((len(labels), V), smoothing / V, dtype=torch.float64, device="cuda")
+    t.scatter_add_(1, torch.where(there, labels, 0).long().unsqueeze(1),
+                   torch.full((len(labels), 1), 1.0 - smoothing, dtype=torch.float64, device="cuda"))
+    return t, there
+
+
+def teacher_target(cls, logits, V, T):
+    inside = (cls >= 0) & (cls < V)
+    l = torch.where(inside, logits.double(), torch.tensor(-math.inf, dtype=torch.float64, device="cuda")) / T
+    there = (l > -math.inf).any(1)
+    q = torch.softmax(torch.where(there.unsqueeze(1), l, torch.zeros_like(l)), 1)
+    q = torch.where(inside, q, torch.zeros_like(q))
+    t = torch.zeros((len(cls), V), dtype=torch.float64, device="cuda")
+    return t.scatter_add_(1, torch.where(inside, cls, 0).long(), q), there
+
+
+def both(head, x, labels, dloss, smoothing=0.0):
+    saved = head.new_saved(x.shape)
+    loss = head.cross_entropy(x, labels, smoothing, saved=saved)
+    return dict(head.cross_entropy_backward(x, labels, saved, dloss, smoothing), loss=loss)
+
+
+def both_teacher(head, x, cls, logits, dloss, T):
+    saved = head.new_saved(x.shape, cls.shape[-1])
+    loss = head.distill(x, cls, logits, T, saved=saved)
+    return dict(head.distill_backward(x, cls, logits, saved, dloss, T), loss=loss)
+
+
+def upstream(head, P, g):
+    return torch.full((1,), 0.7, device="cuda") if head.reduction == "mean" else torch.randn(
+        P, generator=g, device="cuda") / P
+
+
+SIZES = [
+    # rows, features, classes
+    (1, 1, 1), (1, 8, 2), (1, 768, 1000), (2, 5, 3), (7, 64, 11), (31, 33, 65), (33, 64, 100), (64, 128, 1000),
+    (65, 40, 257), (130, 72, 515), (257, 264, 2050), (1024, 32, 300), (300, 541, 703), (50, 2048, 1000),
+    (1000, 96, 10), (3, 1030, 5003),
+]
+
+
+@pytest.mark.parametrize("dtype", [F, H], ids=["f32", "bf16"])
+@pytest.mark.parametrize("P,C,V", SIZES)
+def test_labels(P, C, V, dtype):
+    i = SIZES.index((P, C, V)) + (dtype == H)
+    x, w, b, g = make(P, C, V, dtype, shift=i % 3 != 0, seed=i)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    if P > 2:
+        labels[P // 2] = -100
+    smoothing = 0.1 * (i % 2)
+    head = HeadLoss(w, b, reduction="rows" if i % 2 else "mean")
+    dloss = upstream(head, P, g)
+    got = both(head, x, labels, dloss, smoothing)
+    target, there = label_target(labels, V, smoothing)
+    check(got, *reference(x, w, b, target, there, 1.0, dloss, head.reduction == "mean", False))
+    again = both(head, x, labels.int(), dloss, smoothing)      # 32-bit labels: the same bits
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert torch.equal(head.cross_entropy(x, labels, smoothing), got["loss"])
+
+
+@pytest.mark.parametrize("dtype", [F, H], ids=["f32", "bf16"])
+@pytest.mark.parametrize("P,C,V", SIZES)
+def test_teacher(P, C, V, dtype):
+    i = SIZES.index((P, C, V)) + (dtype == H)
+    x, w, b, g = make(P, C, V, dtype, shift=i % 3 != 1, seed=100 + i)
+    K = [1, 3, 10, 64, 65, 130][i % 6]
+    cls, logits = entries(P, K, V, g, H if i % 2 else F)
+    T = [1.0, 2.0, 0.5][i % 3]
+    head = HeadLoss(w, b, reduction="mean" if i % 2 else "rows")
+    dloss = upstream(head, P, g)
+    got = both_teacher(head, x, cls, logits, dloss, T)
+    target, there = teacher_target(cls, logits, V, T)
+    assert there.all()
+    check(got, *reference(x, w, b, target, there, T, dloss, head.reduction == "mean", True))
+    again = both_teacher(head, x, cls.int(), logits, dloss, T)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert torch.equal(head.distill(x, cls, logits, T), got["loss"])
+
+
+@pytest.mark.parametrize("P,C,V,dtype,K", [
+    (8192, 64, 20000, H, 0), (4100, 41, 40000, H, 5), (9000, 24, 8000, F, 0), (16500, 8, 9001, H, 3),
+])
+def test_classes_in_pieces(P, C, V, dtype, K):
+    """More classes than the gradient of the logits holds at once."""
+    x, w, b, g = make(P, C, V, dtype, seed=5)
+    head = HeadLoss(w, b)
+    dloss = torch.ones(1, device="cuda")
+    if K:
+        cls, logits = entries(P, K, V, g)
+        got = both_teacher(head, x, cls, logits, dloss, 2.0)
+        target, there = teacher_target(cls, logits, V, 2.0)
+        check(got, *reference(x, w, b, target, there, 2.0, dloss, True, True))
+    else:
+        labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+        got = both(head, x, labels, dloss, 0.1)
+        target, there = label_target(labels, V, 0.1)
+        check(got, *reference(x, w, b, target, there, 1.0, dloss, True, False))
+
+
+@pytest.mark.parametrize("dtype", [F, H], ids=["f32", "bf16"])
+@pytest.mark.parametrize("P,C,V", [(40, 64, 130), (40, 61, 130), (3, 16, 5), (300, 128, 1000)])
+def test_rows_left_out_hold_anything(P, C, V, dtype):
+    x, w, b, g = make(P, C, V, dtype, seed=9)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    out = torch.arange(P, device="cuda") % 3 == 1
+    labels[out] = torch.tensor([-100, -1, V, 1 << 40, -(1 << 40)], device="cuda")[torch.arange(int(out.sum())) % 5]
+    zeros = torch.where(out.unsqueeze(1), torch.zeros_like(x), x)
+    for fill in (math.nan, math.inf, -math.inf, 1e30):
+        dirty = torch.where(out.unsqueeze(1), torch.full_like(x, fill), x)
+        for reduction in ("mean", "rows"):
+            head = HeadLoss(w, b, reduction=reduction)
+            dloss = upstream(head, P, g)
+            if reduction == "rows":
+                dloss = torch.where(out, torch.full_like(dloss, math.nan), dloss)
+            a, c = both(head, dirty, labels, dloss, 0.1), both(head, zeros, labels, dloss, 0.1)
+            assert all(torch.equal(a[n], c[n]) for n in a)
+            assert all(t.isfinite().all() for t in a.values())
+            assert float(a["dx"][out].abs().max()) == 0.0
+            target, there = label_target(labels, V, 0.1)
+            safe = torch.where(there, dloss, torch.zeros_like(dloss)) if reduction == "rows" else dloss
+            check(c, *reference(zeros, w, b, target, there, 1.0, safe, reduction == "mean", False))
+    # all of them
+    head = HeadLoss(w, b)
+    got = both(head, torch.full_like(x, math.nan), torch.full_like(labels, -1), torch.ones(1, device="cuda"))
+    assert all(float(t.abs().max()) == 0.0 for t in got.values())
+
+
+def test_teachers_entries():
+    """Classes outside, logits of minus infinity, one class in every entry, rows with nothing left."""
+    P, C, V, K, T = 64, 72, 90, 9, 2.0
+    x, w, b, g = make(P, C, V, F, seed=21)
+    cls, logits = entries(P, K, V, g)
+    cls[0], cls[1] = 5, -1
+    cls[2, 3:], cls[3, ::2] = V, -7
+    logits[4, 2:5], logits[5] = -math.inf, -math.inf
+    logits[6, 0], logits[6, 1:] = 300.0, -300.0
+    cls[7, 0] = -1
+    logits[7, 1:] = -math.inf
+    logits[8, 2], cls[8, 2] = math.nan, -1           # a NaN of an entry that counts for nothing
+    cls[9] = torch.arange(K, device="cuda") // 3
+    x[1] = math.nan
+    for dtype in (F, H):
+        xs, ws = x.to(dtype), w.to(dtype)
+        target, there = teacher_target(cls, torch.where(cls < 0, torch.zeros_like(logits), logits), V, T)
+        assert there.sum() == P - 3 and not there[[1, 5, 7]].any()
+        for reduction in ("mean", "rows"):
+            head = HeadLoss(ws, b, reduction=reduction)
+            dloss = upstream(head, P, g)
+            got = both_teacher(head, xs, cls, logits, dloss, T)
+            check(got, *reference(xs, ws, b, target, there, T, dloss, reduction == "mean", True))
+            assert float(got["dx"][[1, 5, 7]].abs().max()) == 0.0
+    # a NaN that counts, and a logit of the head that is not finite, stay in their rows
+    logits[10, 1] = math.nan
+    x[11, 3] = math.inf
+    head = HeadLoss(w, b, reduction="rows")
+    loss = head.distill(x, cls, logits, T)
+    assert loss[10:12].isnan().all() and loss[:10].isfinite().all() and loss[12:].isfinite().all()
+
+
+def test_classes_taken_out():
+    """A shift of minus infinity: no probability, no gradient; as a label an infinite loss."""
+    P, C, V = 20, 48, 33
+    x, w, b, g = make(P, C, V, F, seed=31)
+    out = torch.tensor([0, 7, 32], device="cuda")
+    b[out] = -math.inf
+    labels = torch.randint(1, 7, (P,), generator=g, device="cuda")
+    head = HeadLoss(w, b, reduction="rows")
+    dloss = torch.rand(P, generator=g, device="cuda")
+    got = both(head, x, labels, dloss)
+    target, there = label_target(labels, V, 0.0)
+    check(got, *reference(x, w, b, target, there, 1.0, dloss, False, False))
+    assert float(got["dshift"][out].abs().max()) == 0.0 and float(got["dweight"][out].abs().max()) == 0.0
+    labels[4] = 7
+    got = both(head, x, labels, dloss)
+    assert float(got["loss"][4]) == math.inf and got["loss"].isfinite().sum() == P - 1
+    assert all(got[n].isfinite().all() for n in ("dx", "dweight", "dshift"))
+    assert abs(float(got["dshift"][7]) + float(dloss[4])) <= 2.0 ** -22
+    # logits far apart: one class has all of the probability, the others' gradients are zero
+    sharp = HeadLoss(w * 4096, None, reduction="rows")
+    top = torch.matmul(x, w.t()).argmax(1)
+    got = both(sharp, x, top, dloss)
+    # (the losses vanish: what is left is the logits' own error, C steps of sizes of tens of thousands)
+    target, there = label_target(top, V, 0.0)
+    check(got, *reference(x, w * 4096, None, target, there, 1.0, dloss, False, False))
+
+
+def test_differences():
+    """The gradients against differences of the loss along a direction, float32."""
+    P, C, V, K = 24, 16, 30, 4
+    x, w, b, g = make(P, C, V, F, seed=41)
+    cls, logits = entries(P, K, V, g)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    e = 2.0 ** -5
+    one = torch.ones(1, device="cuda")
+    for name in ("labels", "teacher"):
+        def run(x, w, b):
+            head = HeadLoss(w, b)
+            return float(head.cross_entropy(x, labels, 0.2) if name == "labels" else head.distill(x, cls, logits, 2.0))
+
+        head = HeadLoss(w, b)
+        got = both(head, x, labels, one, 0.2) if name == "labels" else both_teacher(head, x, cls, logits, one, 2.0)
+        for n, t in (("dx", x), ("dweight", w), ("dshift", b)):
+            d = torch.randn(t.shape, generator=g, device="cuda")
+            d = d / float(d.abs().max())
+            args = {"dx": x, "dweight": w, "dshift": b}
+            diff = (run(*dict(args, **{n: t + e * d}).values()) - run(*dict(args, **{n: t - e * d}).values())) / (2 * e)
+            # The loss's third derivative is below the logits' change cubed; a logit changes by s at most here.
+            # The loss is right to 2^-18 (its value is below 16, the logits' sums have 16 terms).
+            s = {"dx": float(w.abs().sum(1).max()), "dweight": float(x.abs().sum(1).max()), "dshift": 1.0}[n]
+            assert abs(diff - float((got[n].double() * d).sum())) <= e * e * min(s, 30.0) ** 3 / 6 + 2.0 ** -18 / e, n
+
+
+@pytest.mark.parametrize("P,C,V,dtype", [(70, 48, 130, H), (33, 17, 65, H), (33, 18, 66, F), (5, 64, 1000, F)])
+def test_memory_around_stays(P, C, V, dtype):
+    x, w, b, g = make(P, C, V, dtype, seed=51)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    head = HeadLoss(w, b)
+    bufs = []
+
+    def new(dt, *shape):
+        n, pad = math.prod(shape), 256 // torch.empty(0, dtype=dt).element_size()
+        buf = torch.full((n + 2 * pad,), 77, dtype=dt, device="cuda")
+        bufs.append((buf, pad, n))
+        return buf[pad:pad + n].reshape(shape)
+
+    saved, ws = new(F, P * 2 + 2), new(torch.uint8, head.workspace_bytes(x.shape))
+    head.cross_entropy(x, labels, 0.1, saved=saved, ws=ws)
+    dx, dw, wb = new(dtype, P, C), new(dtype, V, C), new(torch.uint8, head.backward_workspace_bytes(x.shape))
+    head.cross_entropy_backward(x, labels, saved, smoothing=0.1, dx=dx, dweight=dw, ws=wb)
+    torch.cuda.synchronize()
+    want = both(head, x, labels, None, 0.1)
+    assert torch.equal(dx, want["dx"]) and torch.equal(dw, want["dweight"])
+    for buf, pad, n in bufs:
+        assert (buf[:pad] == 77).all() and (buf[pad + n:] == 77).all()
+
+
+def test_each_gradient_by_itself():
+    P, C, V = 40, 64, 130
+    x, w, b, g = make(P, C, V, H, seed=61)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    head = HeadLoss(w, b)
+    want = both(head, x, labels, None)
+    saved = head.new_saved(x.shape)
+    head.cross_entropy(x, labels, saved=saved)
+    desc = head.desc(x.shape)
+    n = mb.moce_head_backward_workspace_bytes(desc)
+    ws, one = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.ones(1, device="cuda")
+    for name in ("dx", "dweight", "dshift"):
+        out = torch.full_like(want[name], math.nan)
+        mb.moce_head_cross_entropy_backward(desc, x, w, b, labels, saved, one, mb.make_head_grads(**{name: out}), ws, n,
+                                            torch.cuda.current_stream())
+        assert torch.equal(out, want[name])
+    mb.moce_head_cross_entropy_backward(desc, x, w, b, labels, saved, one, mb.make_head_grads(), ws, n,
+                                        torch.cuda.current_stream())
+    torch.cuda.synchronize()
+
+
+def test_on_another_stream_and_captured():
+    P, C, V, K = 200, 96, 1000, 6
+    x, w, b, g = make(P, C, V, H, seed=71)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    cls, logits = entries(P, K, V, g)
+    head = HeadLoss(w, b)
+    one = torch.ones(1, device="cuda")
+
+    def step():
+        a = both(head, x, labels, one, 0.1)
+        t = both_teacher(head, x, cls, logits, one, 2.0)
+        return list(a.values()) + list(t.values())
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(4):
+        x.copy_(torch.randn(P, C, generator=g, device="cuda"))
+        labels.copy_(torch.randint(-5, V, (P,), generator=g, device="cuda"))
+        if i == 2:
+            x[labels < 0] = math.nan
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        want = step()
+        torch.cuda.synchronize()
+        for a, c in zip(got, want):
+            assert torch.equal(a.nan_to_num(9.0), c.nan_to_num(9.0))
+
+
+def test_leading_dimensions_and_empty():
+    x, w, b, g = make(24, 16, 30, F, seed=81)
+    labels = torch.randint(0, 30, (24,), generator=g, device="cuda")
+    head = HeadLoss(w, b, reduction="rows")
+    want = both(head, x, labels, None)
+    got = both(head, x.reshape(2, 3, 4, 16), labels.reshape(2, 3, 4), None)
+    assert got["loss"].shape == (2, 3, 4) and got["dx"].shape == (2, 3, 4, 16)
+    assert all(torch.equal(got[n].flatten(), want[n].flatten()) for n in got)
+    one = head.cross_entropy(x[0], labels[0])
+    assert one.shape == () and abs(float(one) - float(want["loss"][0])) <= 2.0 ** -18
+    for reduction, shape in (("rows", (0,)), ("mean", (1,))):
+        head = HeadLoss(w, b, reduction=reduction)
+        got = both(head, x[:0], labels[:0], None)
+        assert got["loss"].shape == shape and got["dx"].shape == (0, 16)
+        assert float(got["dweight"].abs().max()) == 0.0 and float(got["dshift"].abs().max()) == 0.0
+
+
+def test_refusals():
+    x, w, b, g = make(4, 16, 30, F)
+    labels = torch.zeros(4, dtype=torch.int64, device="cuda")
+    cls, logits = entries(4, 3, 30, g)
+    head = HeadLoss(w, b)
+    for args in ((x.bfloat16(), labels), (x[:, :8], labels), (x.t().contiguous().t(), labels), (x, labels[:3]),
+                 (x, labels.float()), (x, labels.short()), (x, labels.cpu()), (x, None), (x.cpu(), labels),
+                 (torch.randn(4, 17, device="cuda"), labels)):
+        with pytest.raises(ValueError):
+            head.cross_entropy(*args)
+    for s in (-0.1, 1.1, math.nan):
+        with pytest.raises(ValueError):
+            head.cross_entropy(x, labels, s)
+    for t in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(ValueError):
+            head.distill(x, cls, logits, t)
+    for args in ((x, cls, logits.double()), (x, cls[:, :2], logits), (x, cls[:, :0], logits[:, :0]), (x, labels, logits),
+                 (x, cls.t().contiguous().t(), logits), (x, cls, logits[:, :2])):
+        with pytest.raises(ValueError):
+            head.distill(*args)
+    saved = head.new_saved(x.shape)
+    with pytest.raises(ValueError):
+        head.cross_entropy(x, labels, saved=saved[:-1])
+    with pytest.raises(ValueError):
+        head.cross_entropy_backward(x, labels, saved, torch.ones(4, device="cuda"))
+    with pytest.raises(ValueError):
+        head.distill_backward(x, cls, logits, saved)
+    with pytest.raises(mb.MoceError):
+        head.cross_entropy(x, labels, ws=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        HeadLoss(w, b, reduction="sum")
+    with pytest.raises(ValueError):
+        HeadLoss(w, b[:3])
+    with pytest.raises(ValueError):
+        HeadLoss(w.cpu(), None)
+    with pytest.raises(ValueError):
+        HeadLoss(w[:0])
