@@ -47,6 +47,9 @@ struct NormArgs {
   float *dscale, *dshift;
   int64_t B;
   int C, G, cg, hw, len, chunks, act;
+  int fold;                  // groups of a workgroup whose parts are joined by those who read them (0: by k_norm_stats)
+  Parts group_parts;         // [B][chunks][G], as `parts`, where they are
+  int params;                // workgroups of k_norm_dx_rows ahead of the others, for dscale and dshift
   int tx;                    // threads across a row (channels-last) or a plane
   int span, spans, each;     // groups in registers: channels of a workgroup, workgroups of an image; vectors of a plane
   float eps;
@@ -71,8 +74,8 @@ __device__ __forceinline__ Moments moments(float n, float off, float s1, float s
 struct Group {
   float mean, rstd;
 };
-__device__ __forceinline__ Group group_of(double m, float s1, float s2, double n, float eps) {
-  const double d = (double)s1 / n, var = fmax(((double)s2 - (double)s1 * d) / n, 0.) + ((double)s2 - (double)s2);
+__device__ __forceinline__ Group group_of(double m, double s1, double s2, double n, float eps) {
+  const double d = s1 / n, var = fmax((s2 - s1 * d) / n, 0.) + (s2 - s2);
   return Group{(float)(m + d), (float)(1. / sqrt(var + (double)eps))};
 }
 
@@ -80,6 +83,9 @@ __device__ __forceinline__ Group group_of(double m, float s1, float s2, double n
 struct Channel {
   float mean, rstd, scale, shift;
 };
+__device__ __forceinline__ Channel channel(const NormArgs& a, const Group& g, int c) {
+  return Channel{g.mean, g.rstd, a.scale ? a.scale[c] : 1.f, a.shift ? a.shift[c] : 0.f};
+}
 __device__ __forceinline__ Channel channel(const NormArgs& a, int64_t b, int c) {
   const int64_t at = b * a.G + c / a.cg;
   return Channel{a.stats[at], a.stats[a.B * a.G + at], a.scale ? a.scale[c] : 1.f, a.shift ? a.shift[c] : 0.f};
@@ -156,6 +162,28 @@ __device__ __forceinline__ void store_n(T* p, int n, const float (&v)[8]) {
     if (i < n) p[i] = Elem<T>::from_f(v[i]);
 }
 
+// dscale and dshift of 16 channels: their sums over the images, or (fold) over
+// the images' parts.
+__device__ __forceinline__ void sum_params(const NormArgs& a, int block, float2* s) {
+  const float2* sums = a.fold ? static_cast<const float2*>(a.parts.p) : a.sums;
+  const int64_t n = a.fold ? a.B * a.chunks : a.B;
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = block * 16 + x;
+  float2 t = make_float2(0.f, 0.f);
+  if (c < a.C)
+#pragma unroll 8
+    for (int64_t i = y; i < n; i += kThreads / 16) {
+      const float2 o = sums[i * a.C + c];
+      t.x += o.x, t.y += o.y;
+    }
+  s[threadIdx.x] = t;
+  __syncthreads();
+  if (y != 0 || c >= a.C) return;
+#pragma unroll
+  for (int i = 1; i < kThreads / 16; ++i) t.x += s[16 * i + x].x, t.y += s[16 * i + x].y;
+  if (a.dshift) a.dshift[c] = t.x;
+  if (a.dscale) a.dscale[c] = t.y;
+}
+
 // ---- channels-last: a thread holds 16 bytes of channels of every `down`-th row of a part ----
 
 constexpr int kAhead = 4;   // rows whose loads are in flight together
@@ -188,7 +216,7 @@ __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kVE<T>])
 template <typename T, typename F>
 __device__ __forceinline__ void each_rows(const NormArgs& a, F&& f) {
   const int x = threadIdx.x % a.tx, c = (blockIdx.y * a.tx + x) * kVE<T>;
-  for (int64_t u = blockIdx.x; u < a.B * a.chunks; u += gridDim.x) {
+  for (int64_t u = blockIdx.x - a.params; u < a.B * a.chunks; u += gridDim.x - a.params) {
     const int64_t b = u / a.chunks;
     const int k = (int)(u - b * a.chunks), r0 = k * a.len, r1 = min(a.hw, r0 + a.len);
     f(b, k, r0 + (int)threadIdx.x / a.tx, r1, c, min(kVE<T>, a.C - c));
@@ -221,6 +249,7 @@ k_norm_sums_rows(NormArgs a) {
   constexpr int VE = kVE<T>;
   __shared__ Moments s[kThreads][VE + 1];
   __shared__ float origin[32 * VE];   // tx is 32 at most
+  __shared__ Part channels[32 * VE];
   const int down = kThreads / a.tx;
   each_rows<T>(a, [&](int64_t b, int k, int r, int r1, int c, int n) __attribute__((always_inline)) {
     const T* const x[1] = {static_cast<const T*>(a.x)};
@@ -253,22 +282,75 @@ k_norm_sums_rows(NormArgs a) {
       if (cc >= a.C) continue;
       Moments t = s[q / VE][q % VE];
       for (int d = 1; d < down; ++d) t = join(t, s[d * a.tx + q / VE][q % VE]);
-      a.parts.at<Part>(b, cc, k) = Part{(double)origin[q] + (double)t.mean, t.m2};
+      const Part o{(double)origin[q] + (double)t.mean, t.m2};
+      if (a.fold)
+        channels[q] = o;
+      else
+        a.parts.at<Part>(b, cc, k) = o;
+    }
+    if (!a.fold) return;
+    __syncthreads();
+    const int g = blockIdx.y * a.fold + threadIdx.x, rows = min(a.hw, (k + 1) * a.len) - k * a.len;
+    if ((int)threadIdx.x < a.fold && g < a.G) {   // equal counts: the mean of the means
+      const Part* o = channels + threadIdx.x * a.cg;
+      double mean = 0., m2 = 0.;
+      for (int i = 0; i < a.cg; ++i) mean += o[i].mean;
+      mean /= a.cg;
+      for (int i = 0; i < a.cg; ++i) m2 += (double)o[i].m2 + (o[i].mean - mean) * (o[i].mean - mean) * rows;
+      a.group_parts.at<Part>(b, g, k) = Part{mean, (float)m2};
     }
   });
 }
 
-template <typename T, bool WHOLE>
+// Sums over an image's parts of the workgroup's groups, by all of its threads:
+// sum(group, part, its sums so far), then done(group, sums) by one thread each.
+template <typename V, typename S, typename D>
+__device__ __forceinline__ void fold_groups(const NormArgs& a, V* s, S&& sum, D&& done) {
+  const int per = kThreads / a.fold, x = threadIdx.x % a.fold, y = threadIdx.x / a.fold;
+  const int g = blockIdx.y * a.fold + x;
+  V v{};
+  if (y < per && g < a.G)
+    for (int k = y; k < a.chunks; k += per) sum(g, k, v);
+  __syncthreads();
+  s[threadIdx.x] = v;
+  __syncthreads();
+  if (y == 0 && g < a.G) {
+    for (int i = 1; i < per; ++i) v.x += s[i * a.fold + x].x, v.y += s[i * a.fold + x].y;
+    done(g, x, v);
+  }
+  __syncthreads();
+}
+
+template <typename T, bool WHOLE, bool FOLD>
 __global__ void __launch_bounds__(kThreads)
 k_norm_apply_rows(NormArgs a) {
   constexpr int VE = kVE<T>;
+  __shared__ double2 s[kThreads];
+  __shared__ Group groups[kThreads];
   const int down = kThreads / a.tx;
-  each_rows<T>(a, [&](int64_t b, int, int r, int r1, int c, int n) __attribute__((always_inline)) {
+  each_rows<T>(a, [&](int64_t b, int chunk, int r, int r1, int c, int n) __attribute__((always_inline)) {
+    if constexpr (FOLD) {
+      const int last = a.hw - (a.chunks - 1) * a.len;
+      fold_groups(a, s, [&](int g, int k, double2& v) __attribute__((always_inline)) {
+        const Part t = a.group_parts.at<Part>(b, g, k);
+        const double m = (double)(k + 1 < a.chunks ? a.len : last) * a.cg, d = t.mean - a.group_parts.at<Part>(b, g, 0).mean;
+        v.x += d * m;
+        v.y += (double)t.m2 + d * d * m;
+      }, [&](int g, int x, const double2& v) __attribute__((always_inline)) {
+        groups[x] = group_of(a.group_parts.at<Part>(b, g, 0).mean, v.x, v.y, (double)a.cg * a.hw, a.eps);
+        if (chunk == 0) a.stats[b * a.G + g] = groups[x].mean, a.stats[(a.B + b) * a.G + g] = groups[x].rstd;
+      });
+    }
     if (n <= 0) return;
     float m[VE], f[VE], h[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
-      const Channel q = channel(a, b, min(c + i, a.C - 1));
+      const int cc = min(c + i, a.C - 1);
+      Channel q;
+      if constexpr (FOLD)
+        q = channel(a, groups[cc / a.cg - blockIdx.y * a.fold], cc);
+      else
+        q = channel(a, b, cc);
       m[i] = q.mean, f[i] = q.rstd * q.scale, h[i] = q.shift;
     }
     const T* const x[1] = {static_cast<const T*>(a.x)};
@@ -290,7 +372,7 @@ template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
 k_norm_dsums_rows(NormArgs a) {
   constexpr int VE = kVE<T>;
-  __shared__ float2 s[kThreads][VE + 1];
+  __shared__ float2 s[kThreads][VE + 1], channels[32 * VE];   // tx is 32 at most
   const int down = kThreads / a.tx;
   each_rows<T>(a, [&](int64_t b, int k, int r, int r1, int c, int n) __attribute__((always_inline)) {
     float s0[VE] = {}, s1[VE] = {};
@@ -327,16 +409,40 @@ k_norm_dsums_rows(NormArgs a) {
         t.x += o.x, t.y += o.y;
       }
       a.parts.at<float2>(b, cc, k) = t;
+      if (!a.fold) continue;
+      const float f = a.scale ? a.scale[cc] : 1.f;
+      channels[q] = make_float2(f * t.x, f * t.y);
+    }
+    if (!a.fold) return;
+    __syncthreads();
+    const int g = blockIdx.y * a.fold + threadIdx.x;
+    if ((int)threadIdx.x < a.fold && g < a.G) {
+      float2 t = make_float2(0.f, 0.f);
+      for (int i = 0; i < a.cg; ++i) t.x += channels[threadIdx.x * a.cg + i].x, t.y += channels[threadIdx.x * a.cg + i].y;
+      a.group_parts.at<float2>(b, g, k) = t;
     }
   });
 }
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool FOLD>
 __global__ void __launch_bounds__(kThreads)
 k_norm_dx_rows(NormArgs a) {
   constexpr int VE = kVE<T>;
+  __shared__ float2 s[kThreads], groups[kThreads];
+  if ((int)blockIdx.x < a.params) {   // uniform
+    if (blockIdx.y == 0) sum_params(a, blockIdx.x, s);
+    return;
+  }
   const int down = kThreads / a.tx;
   each_rows<T>(a, [&](int64_t b, int, int r, int r1, int c, int n) __attribute__((always_inline)) {
+    if constexpr (FOLD)
+      fold_groups(a, s, [&](int g, int k, float2& v) __attribute__((always_inline)) {
+        const float2 t = a.group_parts.at<float2>(b, g, k);
+        v.x += t.x, v.y += t.y;
+      }, [&](int, int x, const float2& v) __attribute__((always_inline)) {
+        const float count = (float)a.cg * (float)a.hw;
+        groups[x] = make_float2(v.x / count, v.y / count);
+      });
     if (n <= 0) return;
     Channel q[VE];
     float2 m[VE];
@@ -344,7 +450,10 @@ k_norm_dx_rows(NormArgs a) {
     for (int i = 0; i < VE; ++i) {
       const int cc = min(c + i, a.C - 1);
       q[i] = channel(a, b, cc);
-      m[i] = a.means[b * a.G + cc / a.cg];
+      if constexpr (FOLD)
+        m[i] = groups[cc / a.cg - blockIdx.y * a.fold];
+      else
+        m[i] = a.means[b * a.G + cc / a.cg];
     }
     const T* const p[2] = {static_cast<const T*>(a.x), static_cast<const T*>(a.dy)};
     T* dx = static_cast<T*>(a.dx);
@@ -960,9 +1069,8 @@ k_norm_stats(NormArgs a, int down) {
       }
     s1 = group_sum_f64(s1, s), s2 = group_sum_f64(s2, s);
     if (threadIdx.x == 0) {
-      const double d = s1 / n;
-      a.stats[u] = (float)(p + d);
-      a.stats[groups + u] = (float)(1. / sqrt(fmax(s2 - s1 * d, 0.) / n + (s2 - s2) + (double)a.eps));
+      const Group g = group_of(p, s1, s2, n, a.eps);
+      a.stats[u] = g.mean, a.stats[groups + u] = g.rstd;
     }
   }
 }
@@ -1006,25 +1114,10 @@ k_norm_dstats(NormArgs a, int down) {
   }
 }
 
-// dscale and dshift: the sums over the images, 16 channels a workgroup.
 __global__ void __launch_bounds__(kThreads)
 k_norm_dparams(NormArgs a) {
   __shared__ float2 s[kThreads];
-  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
-  float2 t = make_float2(0.f, 0.f);
-  if (c < a.C)
-#pragma unroll 4
-    for (int64_t b = y; b < a.B; b += kThreads / 16) {
-      const float2 o = a.sums[b * a.C + c];
-      t.x += o.x, t.y += o.y;
-    }
-  s[threadIdx.x] = t;
-  __syncthreads();
-  if (y != 0 || c >= a.C) return;
-#pragma unroll
-  for (int i = 1; i < kThreads / 16; ++i) t.x += s[16 * i + x].x, t.y += s[16 * i + x].y;
-  if (a.dshift) a.dshift[c] = t.x;
-  if (a.dscale) a.dscale[c] = t.y;
+  sum_params(a, blockIdx.x, s);
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -1037,7 +1130,8 @@ struct Layout {
   int threads, n;           // of a workgroup that holds groups in registers, and their vectors; 0: none does
   int span, spans, each;
   int tx, len, chunks, across;   // across: workgroups over the channels
-  size_t parts, stats, sums, means, total;
+  int fold;
+  size_t parts, group_parts, stats, sums, means, total;
 };
 
 // Vectors a thread, of the kernels there are: twice the registers a vector in
@@ -1120,7 +1214,19 @@ Layout layout_of(const GroupShape& s, bool back) {
     at += up256(n);
     return here;
   };
-  l.parts = take((size_t)s.B * s.C * l.chunks * (back ? sizeof(float2) : sizeof(Part)));
+  // Few groups of few channels, whole ones in a workgroup, and few parts: joined
+  // by the kernels that read them, which saves a launch (8 images of 64 channels
+  // at 56 x 56: backward 21 to 17 us).  Each of their workgroups does so: of
+  // many, the launch is cheaper (64 images of 256 channels: 96 us either way).
+  if (l.rows && l.threads == 0) {
+    const int64_t cg = s.C / s.G, width = l.tx * (s.elem == MOCE_F32 ? 4 : 8), groups = width / cg;
+    if (cg <= 32 && width % cg == 0 && groups * ceil_div(s.HW, l.len) <= 2048 &&
+        s.B * ceil_div(s.HW, l.len) * l.across <= 1024)
+      l.fold = (int)groups;
+  }
+  l.group_parts = take(l.fold ? (size_t)s.B * s.G * l.chunks * (back ? sizeof(float2) : sizeof(Part)) : 0);
+  const size_t part = back ? sizeof(float2) : sizeof(Part);
+  l.parts = take(!back && l.fold ? 0 : (size_t)s.B * s.C * l.chunks * part);
   l.stats = take(back ? 0 : (size_t)2 * s.B * s.G * sizeof(float));
   l.sums = take(back ? (size_t)s.B * s.C * sizeof(float2) : 0);
   l.means = take(back ? (size_t)s.B * s.G * sizeof(float2) : 0);
@@ -1133,6 +1239,7 @@ NormArgs args_of(const GroupShape& s, const Layout& l, const void* x, const floa
   a.x = x, a.scale = scale, a.shift = shift, a.B = s.B, a.C = (int)s.C, a.G = (int)s.G, a.cg = (int)(s.C / s.G);
   a.hw = (int)s.HW, a.len = l.len, a.chunks = l.chunks, a.act = s.act, a.tx = l.tx, a.eps = s.eps;
   a.span = l.span, a.spans = l.spans, a.each = l.each;
+  a.fold = l.fold, a.group_parts = Parts{ws + l.group_parts, s.G * l.chunks, 1, s.G};
   a.parts.p = ws + l.parts;
   a.parts.sb = s.C * l.chunks;
   a.parts.sc = l.rows ? 1 : l.chunks, a.parts.sk = l.rows ? s.C : 1;
@@ -1198,9 +1305,13 @@ hipError_t forward(const GroupShape& s, const void* x, const float* scale, const
   hipLaunchKernelGGL(sums, grid, block, 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_norm_stats, group_grid(s), block, 0, st, a, share(a));
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  const auto apply = !l.rows ? k_norm_apply_planes<T> : whole ? k_norm_apply_rows<T, true> : k_norm_apply_rows<T, false>;
+  if (!l.fold) {
+    hipLaunchKernelGGL(k_norm_stats, group_grid(s), block, 0, st, a, share(a));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const auto apply = !l.rows  ? k_norm_apply_planes<T>
+                     : l.fold ? (whole ? k_norm_apply_rows<T, true, true> : k_norm_apply_rows<T, false, true>)
+                              : (whole ? k_norm_apply_rows<T, true, false> : k_norm_apply_rows<T, false, false>);
   hipLaunchKernelGGL(apply, grid, block, 0, st, a);
   return hipGetLastError();
 }
@@ -1234,17 +1345,27 @@ hipError_t backward(const GroupShape& s, const void* x, const float* scale, cons
         !l.rows ? k_norm_dsums_planes<T> : whole ? k_norm_dsums_rows<T, true> : k_norm_dsums_rows<T, false>;
     hipLaunchKernelGGL(sums, part_grid(s, l), block, 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_norm_dstats, group_grid(s), block, 0, st, a, share(a));
-    e = hipGetLastError();
+    if (!l.fold) {
+      hipLaunchKernelGGL(k_norm_dstats, group_grid(s), block, 0, st, a, share(a));
+      e = hipGetLastError();
+    }
   }
   if (e != hipSuccess) return e;
+  dim3 grid = l.threads ? dim3(1) : part_grid(s, l);   // of dx, where it has a launch of its own
   if (gr.dscale || gr.dshift) {
-    hipLaunchKernelGGL(k_norm_dparams, dim3((unsigned)ceil_div(s.C, 16)), block, 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const unsigned params = (unsigned)ceil_div(s.C, 16);
+    if (l.rows && l.threads == 0 && gr.dx) {   // beside dx
+      a.params = (int)params, grid.x += params;
+    } else {
+      hipLaunchKernelGGL(k_norm_dparams, dim3(params), block, 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
   }
   if (!gr.dx || l.threads) return hipSuccess;
-  const auto dx = !l.rows ? k_norm_dx_planes<T> : whole ? k_norm_dx_rows<T, true> : k_norm_dx_rows<T, false>;
-  hipLaunchKernelGGL(dx, part_grid(s, l), block, 0, st, a);
+  const auto dx = !l.rows  ? k_norm_dx_planes<T>
+                  : l.fold ? (whole ? k_norm_dx_rows<T, true, true> : k_norm_dx_rows<T, false, true>)
+                           : (whole ? k_norm_dx_rows<T, true, false> : k_norm_dx_rows<T, false, false>);
+  hipLaunchKernelGGL(dx, grid, block, 0, st, a);
   return hipGetLastError();
 }
 

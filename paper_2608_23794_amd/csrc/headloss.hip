@@ -217,17 +217,21 @@ struct Targets {
   }
 };
 
-// A row's targets by one wave, kept in LDS: the classes (-1 for an entry that
-// counts for nothing or whose class came before) and their probabilities.
-// False where the row is left out.
+// A row's targets by one wave, kept in LDS (K of each): the classes (-1 for an
+// entry that counts for nothing or whose class came before) and their
+// probabilities; u is room for as many values.  False where the row is left out.
 struct RowTargets {
-  int cls[kMaxEntries];
-  float q[kMaxEntries];
+  int* cls;
+  float *q, *u;
 };
+__device__ __forceinline__ RowTargets targets_at(int* p, int K) {
+  return RowTargets{p, reinterpret_cast<float*>(p + K), reinterpret_cast<float*>(p + 2 * K)};
+}
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-__device__ __forceinline__ bool take_targets(const Targets& t, int64_t p, RowTargets& s, int lane) {
-  if (!t.teacher) {
+template <bool TEACHER>
+__device__ __forceinline__ bool take_targets(const Targets& t, int64_t p, const RowTargets& s, int lane) {
+  if constexpr (!TEACHER) {
     const int i = t.index(p, 0);
     if (lane == 0) s.cls[0] = i, s.q[0] = t.label;
     wave_fence();
@@ -247,29 +251,23 @@ __device__ __forceinline__ bool take_targets(const Targets& t, int64_t p, RowTar
   wave_fence();
   if (sum == 0.f) return false;
   const float r = 1.f / sum;
-  // the first entry of a class has the sum over all of it
-  constexpr int kEach = kMaxEntries / kWave;
-  float q[kEach];
-  bool again[kEach];
-#pragma unroll
-  for (int n = 0; n < kEach; ++n) {
-    q[n] = 0.f, again[n] = false;
-    if (n * kWave >= t.K) continue;
-    const int k = min(n * kWave + lane, t.K - 1), i = s.cls[k];
+  // the first entry of a class has the sum over all of it, the others -1
+  for (int k = lane; k < t.K; k += kWave) {
+    const int i = s.cls[k];
+    float all = 0.f;
+    bool before = false;
+#pragma unroll 4
     for (int o = 0; o < t.K; ++o) {
       const bool same = s.cls[o] == i;
-      again[n] = again[n] || (same && o < k);
-      q[n] += same ? s.q[o] : 0.f;
+      before = before || (same && o < k);
+      all += same ? s.q[o] : 0.f;
     }
+    s.u[k] = before ? -1.f : all * r;
   }
   wave_fence();
-#pragma unroll
-  for (int n = 0; n < kEach; ++n) {
-    const int k = n * kWave + lane;
-    if (k < t.K) {
-      s.q[k] = q[n] * r;
-      if (again[n]) s.cls[k] = -1;
-    }
+  for (int k = lane; k < t.K; k += kWave) {
+    if (s.u[k] < 0.f) s.cls[k] = -1;
+    s.q[k] = s.u[k];
   }
   wave_fence();
   return true;
@@ -284,119 +282,77 @@ struct RowsArgs {
   const float2* stat;
   const float* sums;
   float *rows, *code, *saved;   // code: 0 left out, 1 counts, 2 left out and not finite
+  float *loss, *tail;           // of the mean, as k_head_mean has them
+  bool alone;                   // one workgroup has all rows, and the mean
   int64_t P;
   int C, tc;
   float smoothing, factor;      // factor: T^2 ln 2
 };
 
-template <typename T>
+// The dot product of two rows by LANES neighbouring lanes, each of them has it.
+template <typename T, int LANES>
 __device__ __forceinline__ float dot_row(const T* a, const T* b, int n, int lane) {
-  float s = 0.f;
+  constexpr int kStep = 8 * LANES;
+  float s[2] = {0.f, 0.f};
   int i = lane * 8;
-  for (; i + 8 <= n; i += 8 * kWave) {
+  for (; i + kStep + 8 <= n; i += 2 * kStep) {   // two steps' loads together
+    float u[2][8], v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load8(a + i + h * kStep, u[h]), load8(b + i + h * kStep, v[h]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[h] = fmaf(u[h][e], v[h][e], s[h]);
+  }
+  for (; i + 8 <= n; i += kStep) {
     float u[8], v[8];
     load8(a + i, u);
     load8(b + i, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(u[e], v[e], s);
+    for (int e = 0; e < 8; ++e) s[0] = fmaf(u[e], v[e], s[0]);
   }
-  for (int e = i; e < min(i + 8, n); ++e) s = fmaf(Elem<T>::to_f(a[e]), Elem<T>::to_f(b[e]), s);
-  return wave_sum(s);
+  for (int e = i; e < min(i + 8, n); ++e) s[1] = fmaf(Elem<T>::to_f(a[e]), Elem<T>::to_f(b[e]), s[1]);
+  return wave_sum<LANES>(s[0] + s[1]);
 }
 
-// A workgroup takes a row: its statistics over the tiles, its targets' logits
-// (a wave each), its loss.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-k_head_rows(RowsArgs a) {
-  __shared__ RowTargets s;
-  __shared__ float u[kMaxEntries];
-  __shared__ Soft part[kWaves];
-  __shared__ float total[kWaves];
-  __shared__ int there, wild;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t p = blockIdx.x; p < a.P; p += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + p * a.C;
-    if (threadIdx.x == 0) wild = 0;
-    if (wave == 0) {
-      const bool ok = take_targets(a.t, p, s, lane);
-      if (lane == 0) there = ok;
-    }
-    __syncthreads();
-    if (!there) {   // uniform
-      if (a.saved) {
-        for (int c = threadIdx.x; c < a.C; c += kThreads)
-          if (!__builtin_isfinite(Elem<T>::to_f(x[c]))) wild = 1;
-        __syncthreads();
-      }
-      if (threadIdx.x == 0) {
-        a.rows[p] = 0.f;
-        a.code[p] = wild ? 2.f : 0.f;
-        if (a.saved) a.saved[p * (a.t.K + 1)] = INFINITY;
-      }
-      __syncthreads();
-      continue;
-    }
-    Soft m{-INFINITY, 0.f};
-    float sum = 0.f;
-    for (int i = threadIdx.x; i < a.tc; i += kThreads) {
-      const float2 o = a.stat[p * a.tc + i];
-      m = join(m, Soft{o.x, o.y});
-      if (a.sums) sum += a.sums[p * a.tc + i];
-    }
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      m = join(m, Soft{__shfl_xor(m.m, o, kWave), __shfl_xor(m.s, o, kWave)});
-      sum += __shfl_xor(sum, o, kWave);
-    }
-    if (lane == 0) part[wave] = m, total[wave] = sum;
-    for (int k = wave; k < a.t.K; k += kWaves) {
-      const int i = s.cls[k];
-      if (i < 0) continue;
-      const float d = dot_row(x, static_cast<const T*>(a.w) + (int64_t)i * a.C, a.C, lane);
-      if (lane == 0) u[k] = (d + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
-    }
-    __syncthreads();
-    if (wave == 0) {
-      m = part[0], sum = total[0];
-      for (int w = 1; w < kWaves; ++w) m = join(m, part[w]), sum += total[w];
-      const float lse = m.m + log2f(m.s);
-      float l = 0.f;
-      for (int k = lane; k < a.t.K; k += kWave) {
-        const int i = s.cls[k];
-        if (i < 0) continue;
-        const float q = s.q[k];
-        if (a.t.teacher)
-          l += q == 0.f ? 0.f : q * (log2f(q) - u[k] + lse);
-        else
-          l = (lse - u[k]) * q;
-        if (a.saved) a.saved[p * (a.t.K + 1) + 1 + k] = u[k];
-      }
-      l = wave_sum(l);
-      if (lane == 0) {
-        if (a.sums && a.smoothing > 0.f) l += a.smoothing * (lse - sum / (float)a.t.V * a.t.c1);
-        a.rows[p] = l * a.factor;
-        a.code[p] = 1.f;
-        if (a.saved) a.saved[p * (a.t.K + 1)] = lse;
-      }
-    }
-    __syncthreads();
+// A row's statistics over its tiles, by one wave; every lane has them.
+__device__ __forceinline__ Soft row_stats(const RowsArgs& a, int64_t p, int lane, float* sum) {
+  Soft m{-INFINITY, 0.f};
+  float t = 0.f;
+#pragma unroll 2
+  for (int i = lane; i < a.tc; i += kWave) {
+    const float2 o = a.stat[p * a.tc + i];
+    m = join(m, Soft{o.x, o.y});
+    if (a.sums) t += a.sums[p * a.tc + i];
   }
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) {
+    m = join(m, Soft{__shfl_xor(m.m, o, kWave), __shfl_xor(m.s, o, kWave)});
+    t += __shfl_xor(t, o, kWave);
+  }
+  *sum = t;
+  return m;
+}
+
+// Whether a row holds a value that is not finite, to every lane.
+template <typename T>
+__device__ __forceinline__ bool wild_row(const T* x, int C, int lane) {
+  bool w = false;
+  for (int c = lane; c < C; c += kWave) w = w || !__builtin_isfinite(Elem<T>::to_f(x[c]));
+  return __any(w);
 }
 
 // The mean over the rows that count, and what the backward wants to know of all
 // rows: their number, and whether a row that is left out is not finite.
-constexpr int kMeanThreads = 1024;
-__global__ void __launch_bounds__(kMeanThreads)
-k_head_mean(const float* __restrict__ rows, const float* __restrict__ code, int64_t P, float* __restrict__ loss,
-            float* __restrict__ tail) {
-  __shared__ double sums[kMeanThreads / kWave], counts[kMeanThreads / kWave];
+template <int NT>
+__device__ __forceinline__ void mean_of_rows(const float* rows, const float* code, int64_t P, float* loss, float* tail) {
+  __shared__ double sums[NT / kWave], counts[NT / kWave];
   __shared__ int wild;
   if (threadIdx.x == 0) wild = 0;
   __syncthreads();
   double sum = 0., count = 0.;
 #pragma unroll 4
-  for (int64_t p = threadIdx.x; p < P; p += kMeanThreads) {
+  for (int64_t p = threadIdx.x; p < P; p += NT) {
     const float c = code[p];
     sum += rows[p];
     count += c == 1.f;
@@ -410,9 +366,99 @@ k_head_mean(const float* __restrict__ rows, const float* __restrict__ code, int6
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum, counts[threadIdx.x >> 6] = count;
   __syncthreads();
   if (threadIdx.x != 0) return;
-  for (int w = 1; w < kMeanThreads / kWave; ++w) sum += sums[w], count += counts[w];
+  for (int w = 1; w < NT / kWave; ++w) sum += sums[w], count += counts[w];
   if (loss) *loss = count > 0. ? (float)(sum / count) : 0.f;
   if (tail) tail[0] = (float)count, tail[1] = (float)wild;
+}
+// By a launch of its own, where k_head_rows is more than one workgroup.  (Its
+// last workgroup to end, found by a counter, needs a fence in all of them: 256
+// rows 10.5 us, not 5.2 and 2.6.)
+constexpr int kMeanThreads = 1024;
+__global__ void __launch_bounds__(kMeanThreads)
+k_head_mean(const float* rows, const float* code, int64_t P, float* loss, float* tail) {
+  mean_of_rows<kMeanThreads>(rows, code, P, loss, tail);
+}
+
+// The rows' losses, and what the backward reads.  Labels: a wave a row.  A
+// teacher: a workgroup a row, whose 16 groups of 16 lanes take the targets'
+// dot products (a wave for each: 3152 rows of 768 with 32 entries 77 us).
+template <typename T, bool TEACHER>
+__global__ void __launch_bounds__(kThreads)
+k_head_rows(RowsArgs a) {
+  extern __shared__ int entries[];   // a teacher's: classes, probabilities, logits
+  __shared__ int there, one_cls[kWaves];
+  __shared__ float one_q[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.t.K;
+  const RowTargets s = TEACHER ? targets_at(entries, K) : RowTargets{one_cls + wave, one_q + wave, nullptr};
+  float* u = s.u;
+  constexpr int kRows = TEACHER ? 1 : kWaves;   // of a workgroup
+  for (int64_t p0 = blockIdx.x * (int64_t)kRows; p0 < a.P; p0 += (int64_t)gridDim.x * kRows) {
+    const int64_t p = TEACHER ? p0 : p0 + wave;
+    if (p >= a.P) break;   // a wave of labels
+    const T* x = static_cast<const T*>(a.x) + p * a.C;
+    bool ok;
+    if constexpr (TEACHER) {
+      __syncthreads();   // the last row's entries are read
+      if (wave == 0) {
+        const bool t = take_targets<TEACHER>(a.t, p, s, lane);
+        if (lane == 0) there = t;
+      }
+      __syncthreads();
+      ok = there;
+    } else {
+      ok = take_targets<TEACHER>(a.t, p, s, lane);
+    }
+    if (!ok) {
+      const bool wild = a.saved && (!TEACHER || wave == 0) && wild_row(x, a.C, lane);
+      if (lane == 0 && (!TEACHER || wave == 0)) {
+        a.rows[p] = 0.f;
+        a.code[p] = wild ? 2.f : 0.f;
+        if (a.saved) a.saved[p * (K + 1)] = INFINITY;
+      }
+      continue;
+    }
+    float* saved = a.saved ? a.saved + p * (K + 1) : nullptr;
+    if constexpr (TEACHER) {
+      constexpr int kLanes = 16;
+      for (int k = threadIdx.x / kLanes; k < K; k += kThreads / kLanes) {
+        const int i = s.cls[k];
+        if (i < 0) continue;
+        const float d = dot_row<T, kLanes>(x, static_cast<const T*>(a.w) + (int64_t)i * a.C, a.C, threadIdx.x % kLanes);
+        if (threadIdx.x % kLanes == 0) u[k] = (d + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
+      }
+      __syncthreads();
+      if (wave != 0) continue;
+    }
+    float sum;
+    const Soft m = row_stats(a, p, lane, &sum);
+    const float lse = m.m + log2f(m.s);
+    float l = 0.f;
+    if constexpr (TEACHER) {
+      for (int k = lane; k < K; k += kWave) {
+        if (s.cls[k] < 0) continue;
+        const float q = s.q[k];
+        l += q == 0.f ? 0.f : q * (log2f(q) - u[k] + lse);
+        if (saved) saved[1 + k] = u[k];
+      }
+      l = wave_sum(l);
+    } else {
+      const int i = s.cls[0];
+      const float d = dot_row<T, kWave>(x, static_cast<const T*>(a.w) + (int64_t)i * a.C, a.C, lane);
+      const float z = (d + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
+      l = (lse - z) * s.q[0];
+      if (saved && lane == 0) saved[1] = z;
+      if (a.sums && a.smoothing > 0.f) l += a.smoothing * (lse - sum / (float)a.t.V * a.t.c1);
+    }
+    if (lane == 0) {
+      a.rows[p] = l * a.factor;
+      a.code[p] = 1.f;
+      if (saved) saved[0] = lse;
+    }
+  }
+  if (!a.alone) return;
+  __threadfence_block();
+  __syncthreads();
+  mean_of_rows<kThreads>(a.rows, a.code, a.P, a.loss, a.tail);
 }
 
 // ---- the backward's rows ---------------------------------------------------------
@@ -495,16 +541,16 @@ struct TargetArgs {
   unsigned long long* fixed;  // nullptr: none
 };
 // The targets' elements of a piece of dz, a wave a row.
-template <typename T>
+template <typename T, bool TEACHER>
 __global__ void __launch_bounds__(kThreads)
 k_head_targets(TargetArgs a) {
-  __shared__ RowTargets rows[kWaves];
+  extern __shared__ int entries[];   // a wave's targets
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  RowTargets& s = rows[wave];
+  const RowTargets s = targets_at(entries + wave * 3 * a.t.K, a.t.K);
   const int unit = a.fixed ? fixed_exponent(a.gmax, a.blocks, a.P, lane) : 0;
   for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
     const float g = a.grow[p];
-    if (g == 0.f || !take_targets(a.t, p, s, lane)) continue;
+    if (g == 0.f || !take_targets<TEACHER>(a.t, p, s, lane)) continue;
     const float* saved = a.saved + p * (a.t.K + 1);
     const float lse = saved[0];
     for (int k = lane; k < a.t.K; k += kWave) {
@@ -587,23 +633,51 @@ FwdLayout fwd_layout(const HeadShape& s) {
   return l;
 }
 
+// The products of a piece of n classes.
+struct Products {
+  Plan z, x, w;
+  double time() const { return z.time + x.time + w.time; }
+};
+Products products_of(const HeadShape& s, int64_t n, int most_splits = INT_MAX) {
+  const bool ragged = Sizes(s).ragged();
+  return Products{plan(s.P, n, s.C, s.elem, false, false, 1), plan(s.P, s.C, n, s.elem, ragged, false, most_splits),
+                  plan(n, s.C, s.P, s.elem, ragged, true)};
+}
+
 struct BwdLayout {
-  Plan pz, px, pw;
+  Products all, last;      // of a piece, of the last one
   int n, pieces, groups;   // classes of a piece, pieces; groups of rows of dshift's sums
   int64_t ld;              // of a piece of dz
   size_t x, w, grow, gmax, fixed, cols, dz, part, dx, total;
 };
+// How the classes are cut: evenly, or in pieces whose 256 x 256 tiles fill the
+// CUs in whole rounds, by the time of their products (4095 rows of 2048 by
+// 100003 classes: 7 rounds and not 6.1, 6.7 ms to 5.9).
+int64_t piece_of(const HeadShape& s) {
+  const Sizes z(s);
+  const int64_t most = std::max<int64_t>(kPieceBytes / (int64_t)(s.P * z.el()) / kPieceClasses, 1) * kPieceClasses;
+  const int64_t least = ceil_div(s.V, most);   // pieces
+  if (least == 1) return s.V;
+  int64_t round = kPieceClasses;
+  for (int64_t tiles = ceil_div(s.P, 256); tiles % 256 != 0 && round * 2 <= most; tiles *= 2) round *= 2;
+  int64_t best = 0;
+  double time = 1e300;
+  for (const int64_t n : {ceil_div(ceil_div(s.V, least), kPieceClasses) * kPieceClasses,
+                          ceil_div(ceil_div(s.V, least + 1), kPieceClasses) * kPieceClasses, most / round * round}) {
+    const int64_t full = s.V / n, rest = s.V - full * n;
+    const double t = full * products_of(s, n).time() + (rest ? products_of(s, rest).time() : 0.);
+    if (t < time) time = t, best = n;
+  }
+  return best;
+}
 BwdLayout bwd_layout(const HeadShape& s) {
   const Sizes z(s);
   BwdLayout l{};
-  const int64_t most = std::max<int64_t>(kPieceBytes / (int64_t)(s.P * z.el()) / kPieceClasses, 1) * kPieceClasses;
-  const int64_t each = ceil_div(ceil_div(s.V, ceil_div(s.V, most)), kPieceClasses) * kPieceClasses;
-  l.n = (int)std::min(each, s.V), l.pieces = (int)ceil_div(s.V, l.n), l.ld = z.up(l.n);
-  l.pz = plan(s.P, l.n, s.C, s.elem, false, false, 1);
-  l.px = plan(s.P, s.C, l.n, s.elem, z.ragged(), false);
-  l.pw = plan(l.n, s.C, s.P, s.elem, z.ragged(), true);
-  const int wave_rows = kTile[l.pz.tile].tr / 2;   // every tile has two waves down
-  l.groups = (int)ceil_div(s.P, kTile[l.pz.tile].tr) * (kTile[l.pz.tile].tr / wave_rows);
+  l.n = (int)piece_of(s), l.pieces = (int)ceil_div(s.V, l.n), l.ld = z.up(l.n);
+  l.all = l.last = products_of(s, l.n);
+  const int64_t rest = s.V - (int64_t)(l.pieces - 1) * l.n;
+  if (rest < l.n) l.last = products_of(s, rest, l.all.x.splits), l.last.z = l.all.z;
+  l.groups = (int)ceil_div(s.P, kTile[l.all.z.tile].tr) * 2;   // every tile has two waves down
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -617,8 +691,9 @@ BwdLayout bwd_layout(const HeadShape& s) {
   l.fixed = take((size_t)s.V * 8);
   l.cols = take((size_t)l.groups * s.V * sizeof(float));
   l.dz = take((size_t)s.P * l.ld * z.el());
-  l.dx = take(l.px.splits > 1 || l.pieces > 1 ? part_bytes(s.P, s.C, l.px) : 0);
-  l.part = take(l.pw.splits > 1 ? part_bytes(l.n, s.C, l.pw) : 0);
+  l.dx = take(l.all.x.splits > 1 || l.pieces > 1 ? part_bytes(s.P, s.C, l.all.x) : 0);
+  auto parts = [&](int64_t n, const Plan& p) { return p.splits > 1 ? part_bytes(n, s.C, p) : 0; };
+  l.part = take(std::max(parts(l.n, l.all.w), parts(rest, l.last.w)));
   l.total = at;
   return l;
 }
@@ -669,12 +744,19 @@ hipError_t forward(const HeadShape& s, const void* x, const void* w, const float
   a.rows = s.mean ? reinterpret_cast<float*>(ws + l.rows) : loss;
   a.code = reinterpret_cast<float*>(ws + l.code);
   a.P = s.P, a.C = (int)s.C, a.tc = l.tc, a.smoothing = s.smoothing;
+  const bool mean = s.mean || saved;
+  a.loss = s.mean ? loss : nullptr, a.tail = saved ? saved + s.P * (s.K + 1) : nullptr;
+  a.alone = mean && s.P <= (s.teacher ? 1 : kWaves);
   a.factor = (float)(0.69314718055994531 * scale_of(s) * scale_of(s));
-  hipLaunchKernelGGL(k_head_rows<T>, dim3((unsigned)std::min(s.P, kMaxBlocks)), dim3(kThreads), 0, st, a);
+  if (s.teacher)
+    hipLaunchKernelGGL((k_head_rows<T, true>), dim3((unsigned)std::min(s.P, kMaxBlocks)), dim3(kThreads),
+                       (unsigned)s.K * 12, st, a);
+  else
+    hipLaunchKernelGGL((k_head_rows<T, false>), dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)),
+                       dim3(kThreads), 0, st, a);
   e = hipGetLastError();
-  if (e != hipSuccess || (!s.mean && !saved)) return e;
-  hipLaunchKernelGGL(k_head_mean, dim3(1), dim3(kMeanThreads), 0, st, a.rows, a.code, s.P, s.mean ? loss : nullptr,
-                     saved ? saved + s.P * (s.K + 1) : nullptr);
+  if (e != hipSuccess || !mean || a.alone) return e;
+  hipLaunchKernelGGL(k_head_mean, dim3(1), dim3(kMeanThreads), 0, st, a.rows, a.code, s.P, a.loss, a.tail);
   return hipGetLastError();
 }
 
@@ -707,22 +789,25 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
     HeadArgs g = logits(s, xl, wl, shift, v0, n);
     g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.even = even;
     g.y = ws + l.dz, g.ld = l.ld, g.colsum = cols ? cols + v0 : nullptr, g.cols_ld = s.V;
-    e = launch_product<T, true, true, HeadGradient>(g, l.pz, st);
+    const Products& plans = i + 1 < l.pieces ? l.all : l.last;
+    e = launch_product<T, true, true, HeadGradient>(g, plans.z, st);
     if (e != hipSuccess) return e;
     TargetArgs a{};
     a.t = targets_of(s, t);
     a.saved = saved, a.grow = grow, a.gmax = gmax, a.blocks = blocks, a.P = s.P, a.ld = l.ld;
     a.v0 = (int)v0, a.n = (int)n, a.even = even, a.dz = ws + l.dz, a.fixed = fixed;
-    hipLaunchKernelGGL(k_head_targets<T>, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
-                       0, st, a);
+    const auto targets = s.teacher ? k_head_targets<T, true> : k_head_targets<T, false>;
+    hipLaunchKernelGGL(targets, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
+                       (unsigned)(kWaves * s.K * 12), st, a);
     e = hipGetLastError();
     if (e == hipSuccess && gr.dx) {
       LineProduct p{};
       p.a = ws + l.dz, p.lda = l.ld, p.a_along = true;
       p.b = static_cast<const char*>(wl) + v0 * z.up(s.C) * z.el(), p.ldb = z.up(s.C);
-      p.R = (int)s.P, p.N = (int)s.C, p.K = (int)n, p.tile = l.px.tile, p.splits = l.px.splits, p.klen = l.px.klen;
+      p.R = (int)s.P, p.N = (int)s.C, p.K = (int)n, p.tile = plans.x.tile, p.klen = plans.x.klen;
+      p.splits = l.all.x.splits;   // those that are joined
       p.y = gr.dx;
-      if (l.px.splits > 1 || l.pieces > 1)
+      if (l.all.x.splits > 1 || l.pieces > 1)
         p.part = reinterpret_cast<float*>(ws + l.dx), p.add = i > 0, p.join = i + 1 == l.pieces;
       e = launch_line_product(s.elem, p, st);
     }
@@ -730,9 +815,10 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
       LineProduct p{};
       p.a = ws + l.dz, p.lda = l.ld, p.b = xl, p.ldb = z.up(s.C);
       if (!z.ragged()) p.pick = saved + s.P * (s.K + 1) + 1, p.other = ws + l.x;
-      p.R = (int)n, p.N = (int)s.C, p.K = (int)s.P, p.tile = l.pw.tile, p.splits = l.pw.splits, p.klen = l.pw.klen;
+      p.R = (int)n, p.N = (int)s.C, p.K = (int)s.P, p.tile = plans.w.tile, p.klen = plans.w.klen;
+      p.splits = plans.w.splits;
       p.y = static_cast<char*>(gr.dweight) + v0 * s.C * z.el();
-      if (l.pw.splits > 1) p.part = reinterpret_cast<float*>(ws + l.part), p.join = true;
+      if (plans.w.splits > 1) p.part = reinterpret_cast<float*>(ws + l.part), p.join = true;
       e = launch_line_product(s.elem, p, st);
     }
     if (e != hipSuccess) return e;

@@ -822,6 +822,7 @@ constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 16, 24, 32, 48, 64, 96, 128, 192, 2
 // the contraction in `splits` lengths whose sums are joined by another kernel.
 struct Plan {
   int tile, splits, klen;
+  double time;   // microseconds, by the model
 };
 // ragged: the output's rows are not whole chunks; turned: both operands lie
 // across the contraction (more LDS reads); most: splits.
@@ -856,7 +857,7 @@ inline Plan plan(int64_t R, int64_t N, int64_t K, int elem, bool ragged, bool tu
       }
       if (time < least) {
         least = time;
-        best = Plan{t, (int)splits, (int)(each * depth)};
+        best = Plan{t, (int)splits, (int)(each * depth), time};
       }
     }
   }
