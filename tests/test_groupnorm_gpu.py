@@ -124,6 +124,57 @@ def check_backward(out, ref, dtype, act, layout):
 
 ACTS = ["none", "relu", "gelu", "silu"]
 
+# Larger ones, through parts of an image: parts joined by their readers or by a launch, groups that end inside a
+# workgroup's channels, whole and ragged rows, many and few parts, groups of all channels.
+PARTS = [
+    (2, 64, 8, 120, 130), (1, 256, 8, 100, 90), (3, 36, 9, 150, 60), (1, 512, 2, 90, 90), (20, 128, 32, 80, 80),
+    (1, 1030, 103, 40, 41), (1, 520, 65, 64, 70), (1, 768, 1, 300, 20), (4, 33, 3, 200, 100), (300, 24, 3, 60, 70),
+    (2, 2, 1, 700, 700), (1, 1024, 1024, 80, 80), (70, 256, 32, 56, 56), (64, 512, 32, 28, 28), (16, 100, 5, 64, 64),
+]
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", PARTS)
+def test_larger_ones(shape, dtype, layout):
+    i = PARTS.index(shape)
+    act = ACTS[(i + (dtype == "bf16") + 2 * (layout == "nchw")) % 4]
+    x, dy, scale, shift = make(shape, dtype, layout, seed=100 + i)
+    layer = GroupNormLayer(shape[2], scale, shift, act=act, layout=layout)
+    stats = layer.new_stats(x.shape)
+    y = layer.forward(x, stats=stats)
+    ref = reference(x, dy, scale, shift, shape[2], 1e-5, act, layout)
+    check_forward(y, stats, ref, x.dtype, act, shape[2], layout)
+    out = layer.backward(x, dy, stats)
+    check_backward(out, ref, x.dtype, act, layout)
+    again = layer.backward(x, dy, stats)
+    assert torch.equal(layer.forward(x), y) and all(torch.equal(again[n], out[n]) for n in out)
+    # the parameters' gradients without dx
+    n = mb.moce_group_norm_backward_workspace_bytes(layer.desc(x.shape, x.dtype))
+    ws, some = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.full_like(scale, 7.0)
+    mb.moce_group_norm_backward(layer.desc(x.shape, x.dtype), x, scale, shift, stats, dy,
+                                mb.make_group_norm_grads(dscale=some), ws, n, torch.cuda.current_stream())
+    assert torch.equal(some, out["dscale"])
+
+
+@pytest.mark.parametrize("shape,layout", [((600, 64, 8, 65536, 1), "nhwc"), ((40, 32, 4, 1400, 1300), "nchw")])
+def test_offsets_past_32_bits(shape, layout):
+    """Images behind 2^31 elements as they are by themselves: a copy of the first ones at the end."""
+    B, C, G, H, W = shape
+    assert B * C * H * W > 1 << 31
+    s = (B, C, H, W) if layout == "nchw" else (B, H, W, C)
+    x = torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_()
+    x[-1] = x[0]
+    layer = GroupNormLayer(G, torch.rand(C, device="cuda") + 0.5, torch.rand(C, device="cuda"), act="relu", layout=layout)
+    stats = layer.new_stats(x.shape)
+    y = layer.forward(x, stats=stats)
+    assert torch.equal(y[-1], y[0]) and torch.equal(stats[:, -1], stats[:, 0])
+    ref = reference(x[-1:], x[-1:], layer.scale, layer.shift, G, 1e-5, "relu", layout)
+    check_forward(y[-1:], stats[:, -1:], ref, x.dtype, "relu", G, layout)
+    del ref
+    out = layer.backward(x, x, stats, dx=y)
+    assert torch.equal(out["dx"][-1], out["dx"][0])
+
 
 @pytest.mark.parametrize("layout", ["nchw", "nhwc"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

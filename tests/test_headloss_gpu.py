@@ -430,3 +430,59 @@ def test_refusals():
         HeadLoss(w.cpu(), None)
     with pytest.raises(ValueError):
         HeadLoss(w[:0])
+
+
+def test_many_rows():
+    """More rows than workgroups, few classes; the same rows again behind 2^22."""
+    P, C, V = 4_600_000, 8, 9
+    x, w, b, g = make(P, C, V, F, seed=91)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    labels[5::1000] = -1
+    x[-1000:], labels[-1000:] = x[:1000], labels[:1000]
+    head = HeadLoss(w, b)
+    got = both(head, x, labels, torch.ones(1, device="cuda"), 0.1)
+    target, there = label_target(labels, V, 0.1)
+    check(got, *reference(x, w, b, target, there, 1.0, torch.ones(1, device="cuda"), True, False))
+    assert torch.equal(got["dx"][-1000:], got["dx"][:1000])
+
+
+def test_offsets_past_32_bits():
+    """Rows, and classes, behind 2^31 elements."""
+    P, C, V = 1_050_000, 2056, 16
+    x = torch.empty((P, C), dtype=H, device="cuda").normal_()
+    _, w, b, g = make(1, C, V, H, seed=92)
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    x[-256:], labels[-256:] = x[:256], labels[:256]
+    head = HeadLoss(w, b, reduction="rows")
+    dloss = torch.ones(P, device="cuda")
+    got = both(head, x, labels, dloss)
+    assert torch.equal(got["loss"][-256:], got["loss"][:256]) and torch.equal(got["dx"][-256:], got["dx"][:256])
+    target, there = label_target(labels[-256:], V, 0.0)
+    want, tol = reference(x[-256:], w, b, target, there, 1.0, dloss[:256], False, False)
+    check({n: got[n][-256:] for n in ("loss", "dx")}, want, tol)
+    # sums over the rows: those of two halves (float32, so each is right to its own tolerance)
+    half = P // 2
+    parts = [both(head, x[i:i + half].contiguous(), labels[i:i + half].contiguous(), dloss[:half]) for i in (0, half)]
+    for n in ("dweight", "dshift"):
+        a, c = got[n].double(), sum(p[n].double() for p in parts)
+        # sums of P terms of about 0.3 |x| in float32 by splits of at most 2^15 rows, then bfloat16
+        assert ((a - c).abs() <= 2.0 ** -7 * c.abs() + 2.0 ** -9 * P ** 0.5).all()
+    del x, got, parts
+    P, V = 8, 1_048_576
+    x, w = torch.randn(P, C, device="cuda").to(H), torch.empty((V, C), dtype=H, device="cuda").normal_().mul_(0.02)
+    labels = torch.tensor([0, 1, V - 1, V - 2, V // 2, 3, V, -1], device="cuda")
+    w[-1] = w[0]
+    head = HeadLoss(w, None, reduction="rows")
+    got = both(head, x, labels, torch.ones(P, device="cuda"))
+    assert (got["loss"][6:] == 0).all() and (got["dx"][6:] == 0).all() and got["loss"][:6].isfinite().all()
+    z = torch.empty((P, V), dtype=torch.float64, device="cuda")
+    for v in range(0, V, 1 << 16):
+        z[:, v:v + (1 << 16)] = torch.matmul(x.double(), w[v:v + (1 << 16)].double().t().contiguous())
+    lse = torch.logsumexp(z, 1)
+    want = lse[:6] - z[torch.arange(6, device="cuda"), labels[:6]]
+    # sums of C products of sizes up to 0.02 x 5 each
+    assert ((got["loss"][:6].double() - want).abs() <= 2 * (C + 16) * 2.0 ** -24 * C * 0.1).all()
+    p = torch.exp(z[:6, -1:] - lse[:6, None])
+    p[2] -= 1
+    last = (p * x[:6].double()).sum(0)
+    assert ((got["dweight"][-1].double() - last).abs() <= 2.0 ** -6 * (p.abs() * x[:6].double().abs()).sum(0)).all()
