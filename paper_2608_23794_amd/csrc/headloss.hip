@@ -32,6 +32,7 @@ struct HeadArgs : GemmArgs {
   const float* lse;      // a row's, at lse_ld row
   int64_t lse_ld;
   const float* grow;     // [R] g; 0: the row is left out, or weighs nothing
+  const float* top;      // the largest |g|, and 1 over it
   float even;            // e / V
   float* colsum;         // [rows of waves][cols_ld] sums of dz (nullptr: none)
   int64_t cols_ld;
@@ -123,8 +124,12 @@ struct HeadStats {
 };
 
 // ---- backward epilogue -----------------------------------------------------------
-// Eight classes a lane, in rows, as Finish has them: g (2^(u - lse) - e / V),
-// zeros behind the classes to the end of the line.
+// Eight classes a lane, in rows, as Finish has them: g / G (2^(u - lse) - e / V),
+// zeros behind the classes to the end of the line.  G, the largest |g|, comes
+// in behind the products: with it, equal weights of the rows are 1, and a
+// label's element, near -1, is rounded by its own small rest; within dz, the
+// rounding of g would be one factor of all rows' gradients (dx and dweight of
+// 8192 rows and 65536 classes were 3.3e-3 off in the 2-norm, not 1.7e-3).
 template <typename T, int BYTES, int FR, int FC, int WR, int WC>
 struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
   using F = Finish<T, BYTES, FR, FC, WR, WC>;
@@ -139,6 +144,7 @@ struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sh[i] = h.shift ? h.shift[min(c + i, h.N - 1)] : 0.f;
     T* y = static_cast<T*>(h.y);
+    const float unit = h.top[1];
 #pragma unroll
     for (int f = 0; f < FR; f += F::kFrags) {
       constexpr int kPer = 16 / F::kDown, kBatch = F::kBatch;
@@ -155,7 +161,7 @@ struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
         for (int b = 0; b < kBatch; ++b) {
           const int row = this->row(f * kPer + it + b), r = min(row, h.R - 1);
           lse[b] = h.lse[r * h.lse_ld];
-          g[b] = row < h.R ? h.grow[r] : 0.f;
+          g[b] = row < h.R ? h.grow[r] * unit : 0.f;
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) this->value(l, it + b, v[b]);
@@ -472,10 +478,16 @@ struct PrepArgs {
   int C, ld, K, mean;
   float T;
   const float *saved, *dloss;
-  float *grow, *gmax;         // gmax: [kPrepBlocks] largest |g|, finite ones
+  float *grow, *gmax;         // gmax: [kPrepBlocks] largest |g|, finite ones, of rows' weights
+  float* top;                 // G and 1 / G: here of the mean, else by k_head_top
   unsigned long long* fixed;  // [V] cleared (nullptr: none)
   int V;
 };
+// (Without rows that count, or of a weight that is not finite, any G will do.)
+__device__ __forceinline__ void set_top(float* top, float g) {
+  g = __builtin_isfinite(g) ? fmaxf(g, 0x1p-100f) : 1.f;
+  top[0] = g, top[1] = 1.f / g;
+}
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_head_prep(PrepArgs a) {
@@ -514,26 +526,35 @@ k_head_prep(PrepArgs a) {
   }
   if (lane == 0) tops[wave] = top;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+  if (!a.mean)
     a.gmax[blockIdx.x] = top;
-  }
+  else if (blockIdx.x == 0)
+    set_top(a.top, fabsf(a.T * a.dloss[0] / tail[0]));
+}
+__global__ void __launch_bounds__(kThreads)
+k_head_top(const float* __restrict__ gmax, int n, float* __restrict__ top) {
+  __shared__ float s[kWaves];
+  float t = 0.f;
+  for (int i = threadIdx.x; i < n; i += kThreads) t = fmaxf(t, gmax[i]);
+  t = wave_max(t);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) set_top(top, fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
 }
 
-// A unit for the sums of g q over the rows of a class: |sum| <= P max |g|, so
-// they fit 62 bits in units of 2^-62 of that bound, and whole numbers add up to
-// the same in any order.
-__device__ __forceinline__ int fixed_exponent(const float* gmax, int n, int64_t P, int lane) {
-  float top = 0.f;
-  for (int i = lane; i < n; i += kWave) top = fmaxf(top, gmax[i]);
-  top = wave_max(top);
-  return 61 - (64 - __clzll(P)) - (top > 0.f ? ilogbf(top) + 1 : 0);
+// The sums of (g / G) q over the rows of a class, each at most 1, go in whole
+// numbers of 2^-fixed_bits: the same in any order.
+__host__ __device__ inline int fixed_bits(int64_t P) {
+  int n = 60;
+  for (; P > 0; P >>= 1) --n;
+  return n;
 }
 
 struct TargetArgs {
   Targets t;
-  const float *saved, *grow, *gmax;
-  int blocks;                 // of gmax
+  const float *saved, *grow, *top;
   int64_t P, ld;
   int v0, n;                  // the piece's classes
   float even;
@@ -547,9 +568,10 @@ k_head_targets(TargetArgs a) {
   extern __shared__ int entries[];   // a wave's targets
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const RowTargets s = targets_at(entries + wave * 3 * a.t.K, a.t.K);
-  const int unit = a.fixed ? fixed_exponent(a.gmax, a.blocks, a.P, lane) : 0;
+  const int bits = fixed_bits(a.P);
+  const float unit = a.top[1];
   for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
-    const float g = a.grow[p];
+    const float g = a.grow[p] * unit;
     if (g == 0.f || !take_targets<TEACHER>(a.t, p, s, lane)) continue;
     const float* saved = a.saved + p * (a.t.K + 1);
     const float lse = saved[0];
@@ -560,19 +582,18 @@ k_head_targets(TargetArgs a) {
       static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
       const double w = (double)g * (double)q;
       if (a.fixed && __builtin_isfinite(w))
-        atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, unit)));
+        atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
     }
     wave_fence();
   }
 }
 
-// dshift[v]: the sums over the rows' groups less the targets'.  16 classes a workgroup.
+// dshift[v]: G times the sums over the rows' groups less the targets'.  16 classes a workgroup.
 __global__ void __launch_bounds__(kThreads)
 k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned long long* __restrict__ fixed,
-              const float* __restrict__ gmax, int blocks, int64_t P, float* __restrict__ out) {
+              const float* __restrict__ top, int bits, float* __restrict__ out) {
   __shared__ double s[kThreads];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, v = blockIdx.x * 16 + x;
-  const int unit = fixed_exponent(gmax, blocks, P, threadIdx.x & 63);
   double t = 0.;
   if (v < V)
 #pragma unroll 8
@@ -582,7 +603,7 @@ k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned 
   if (y != 0 || v >= V) return;
 #pragma unroll
   for (int i = 1; i < kThreads / 16; ++i) t += s[16 * i + x];
-  out[v] = (float)(t - ldexp((double)(long long)fixed[v], -unit));
+  out[v] = (float)((double)top[0] * (t - ldexp((double)(long long)fixed[v], -bits)));
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -648,7 +669,7 @@ struct BwdLayout {
   Products all, last;      // of a piece, of the last one
   int n, pieces, groups;   // classes of a piece, pieces; groups of rows of dshift's sums
   int64_t ld;              // of a piece of dz
-  size_t x, w, grow, gmax, fixed, cols, dz, part, dx, total;
+  size_t x, w, grow, gmax, top, fixed, cols, dz, part, dx, total;
 };
 // How the classes are cut: evenly, or in pieces whose 256 x 256 tiles fill the
 // CUs in whole rounds, by the time of their products (4095 rows of 2048 by
@@ -688,6 +709,7 @@ BwdLayout bwd_layout(const HeadShape& s) {
   l.w = take(z.w_bytes());
   l.grow = take((size_t)s.P * sizeof(float));
   l.gmax = take(kPrepBlocks * sizeof(float));
+  l.top = take(2 * sizeof(float));
   l.fixed = take((size_t)s.V * 8);
   l.cols = take((size_t)l.groups * s.V * sizeof(float));
   l.dz = take((size_t)s.P * l.ld * z.el());
@@ -767,16 +789,22 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
   const BwdLayout l = bwd_layout(s);
   const int blocks = (int)std::min<int64_t>(kPrepBlocks, ceil_div(s.P, kWaves));
   float *grow = reinterpret_cast<float*>(ws + l.grow), *gmax = reinterpret_cast<float*>(ws + l.gmax);
+  float* top = reinterpret_cast<float*>(ws + l.top);
   unsigned long long* fixed = gr.dshift ? reinterpret_cast<unsigned long long*>(ws + l.fixed) : nullptr;
   float* cols = gr.dshift ? reinterpret_cast<float*>(ws + l.cols) : nullptr;
   {
     PrepArgs a{};
     a.x = x, a.lines = z.ragged() || gr.dweight ? ws + l.x : nullptr, a.ragged = z.ragged(), a.P = s.P;
     a.C = (int)s.C, a.ld = (int)z.up(s.C), a.K = s.K, a.mean = s.mean, a.T = scale_of(s);
-    a.saved = saved, a.dloss = dloss, a.grow = grow, a.gmax = gmax, a.fixed = fixed, a.V = (int)s.V;
+    a.saved = saved, a.dloss = dloss, a.grow = grow, a.gmax = gmax, a.top = top, a.fixed = fixed;
+    a.V = (int)s.V;
     hipLaunchKernelGGL(k_head_prep<T>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
   }
   hipError_t e = hipGetLastError();
+  if (e == hipSuccess && !s.mean) {
+    hipLaunchKernelGGL(k_head_top, dim3(1), dim3(kThreads), 0, st, gmax, blocks, top);
+    e = hipGetLastError();
+  }
   const void *xl = x, *wl = w;
   if (z.ragged()) {
     xl = ws + l.x, wl = ws + l.w;
@@ -787,14 +815,14 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
   for (int i = 0; i < l.pieces; ++i) {
     const int64_t v0 = (int64_t)i * l.n, n = std::min<int64_t>(l.n, s.V - v0);
     HeadArgs g = logits(s, xl, wl, shift, v0, n);
-    g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.even = even;
+    g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.top = top, g.even = even;
     g.y = ws + l.dz, g.ld = l.ld, g.colsum = cols ? cols + v0 : nullptr, g.cols_ld = s.V;
     const Products& plans = i + 1 < l.pieces ? l.all : l.last;
     e = launch_product<T, true, true, HeadGradient>(g, plans.z, st);
     if (e != hipSuccess) return e;
     TargetArgs a{};
     a.t = targets_of(s, t);
-    a.saved = saved, a.grow = grow, a.gmax = gmax, a.blocks = blocks, a.P = s.P, a.ld = l.ld;
+    a.saved = saved, a.grow = grow, a.top = top, a.P = s.P, a.ld = l.ld;
     a.v0 = (int)v0, a.n = (int)n, a.even = even, a.dz = ws + l.dz, a.fixed = fixed;
     const auto targets = s.teacher ? k_head_targets<T, true> : k_head_targets<T, false>;
     hipLaunchKernelGGL(targets, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
@@ -806,7 +834,7 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
       p.b = static_cast<const char*>(wl) + v0 * z.up(s.C) * z.el(), p.ldb = z.up(s.C);
       p.R = (int)s.P, p.N = (int)s.C, p.K = (int)n, p.tile = plans.x.tile, p.klen = plans.x.klen;
       p.splits = l.all.x.splits;   // those that are joined
-      p.y = gr.dx;
+      p.y = gr.dx, p.alpha = top;
       if (l.all.x.splits > 1 || l.pieces > 1)
         p.part = reinterpret_cast<float*>(ws + l.dx), p.add = i > 0, p.join = i + 1 == l.pieces;
       e = launch_line_product(s.elem, p, st);
@@ -817,7 +845,7 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
       if (!z.ragged()) p.pick = saved + s.P * (s.K + 1) + 1, p.other = ws + l.x;
       p.R = (int)n, p.N = (int)s.C, p.K = (int)s.P, p.tile = plans.w.tile, p.klen = plans.w.klen;
       p.splits = plans.w.splits;
-      p.y = static_cast<char*>(gr.dweight) + v0 * s.C * z.el();
+      p.y = static_cast<char*>(gr.dweight) + v0 * s.C * z.el(), p.alpha = top;
       if (plans.w.splits > 1) p.part = reinterpret_cast<float*>(ws + l.part), p.join = true;
       e = launch_line_product(s.elem, p, st);
     }
@@ -825,7 +853,7 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
   }
   if (cols)
     hipLaunchKernelGGL(k_head_dshift, dim3((unsigned)ceil_div(s.V, 16)), dim3(kThreads), 0, st, cols, l.groups,
-                       (int)s.V, fixed, gmax, blocks, s.P, gr.dshift);
+                       (int)s.V, fixed, top, fixed_bits(s.P), gr.dshift);
   return hipGetLastError();
 }
 

@@ -324,6 +324,7 @@ struct LineProduct {
   int64_t lda, ldb;
   const float* pick;     // where *pick is not 0, b lies at `other` (nullptr: no choice)
   const void* other;
+  const float* alpha;    // a factor of y (nullptr: 1)
   int R, N, K, tile, splits, klen;
   void* y;               // [R][N]
   float* part;

@@ -46,6 +46,7 @@ struct GemmArgs {
   const float *scale, *shift;
   int per_row;            // scale and shift by row (else by column)
   int act;
+  const float* alpha;     // of everything, instead of scale and shift (nullptr: 1)
   // where *pick is not 0, b lies at `other` (nullptr: no choice)
   const float* pick;
   const void* other;
@@ -275,7 +276,7 @@ __device__ __forceinline__ void column_affine(const GemmArgs& g, int c, float (&
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int j = min(c + i, g.N - 1);
-    sc[i] = g.scale && !g.per_row ? g.scale[j] : 1.f;
+    sc[i] = g.alpha ? *g.alpha : g.scale && !g.per_row ? g.scale[j] : 1.f;
     sh[i] = g.shift && !g.per_row ? g.shift[j] : 0.f;
   }
 }

@@ -883,7 +883,7 @@ template <typename T>
 hipError_t line_product(const LineProduct& p, hipStream_t st) {
   GemmArgs g{};
   g.a = Operand{p.a, p.lda, 0, 0}, g.b = Operand{p.b, p.ldb, 0, 0};
-  g.pick = p.pick, g.other = p.other;
+  g.pick = p.pick, g.other = p.other, g.alpha = p.alpha;
   g.R = p.R, g.N = p.N, g.K = p.K, g.klen = p.klen, g.y = p.y, g.ld = p.N, g.part = p.part, g.add = p.add;
   const Plan c{p.tile, (int)ceil_div(p.K, p.klen), p.klen, 0.};
   const hipError_t e = p.a_along ? launch_product<T, true, false>(g, c, st) : launch_product<T, false, false>(g, c, st);
