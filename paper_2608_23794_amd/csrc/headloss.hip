@@ -357,13 +357,21 @@ __device__ __forceinline__ void mean_of_rows(const float* rows, const float* cod
   if (threadIdx.x == 0) wild = 0;
   __syncthreads();
   double sum = 0., count = 0.;
-#pragma unroll 4
-  for (int64_t p = threadIdx.x; p < P; p += NT) {
-    const float c = code[p];
-    sum += rows[p];
+  auto add = [&](float r, float c) __attribute__((always_inline)) {
+    sum += r;
     count += c == 1.f;
     if (c == 2.f) wild = 1;
+  };
+  const int64_t whole = P / 4 * 4;
+#pragma unroll 4
+  for (int64_t p = threadIdx.x * 4; p < whole; p += NT * 4) {
+    float r[4], c[4];
+    load4(rows + p, r);
+    load4(code + p, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) add(r[i], c[i]);
   }
+  if (whole + threadIdx.x < P) add(rows[whole + threadIdx.x], code[whole + threadIdx.x]);
 #pragma unroll
   for (int o = kWave / 2; o > 0; o >>= 1) {
     sum += __shfl_xor(sum, o, kWave);
@@ -467,6 +475,83 @@ k_head_rows(RowsArgs a) {
   mean_of_rows<kThreads>(a.rows, a.code, a.P, a.loss, a.tail);
 }
 
+// ---- few classes -------------------------------------------------------------------
+//
+// Where a row's targets would read more for their dot products than all of its
+// logits take, written and read, the forward keeps the logits of a row until
+// its loss is there: float32, bounded as a piece of the gradient is.  (32
+// entries of 209 classes, 43209 rows of 2057: 73 us, not 964; a label of 16
+// classes, 43810 rows of 864 float32: 27, not 43.  Few rows are faster by their
+// dot products: 250 of 768, 10 entries of 1000 classes, 9 us to 6.)
+constexpr int64_t kLogitClasses = 4096, kDotBytes = (int64_t)64 << 20;
+
+// k_head_rows from the logits z [P][V], a wave a row.
+template <typename T, bool TEACHER>
+__global__ void __launch_bounds__(kThreads)
+k_head_logits(RowsArgs a, const float* __restrict__ logits) {
+  extern __shared__ int entries[];   // a wave's targets
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.t.K, V = a.t.V;
+  const RowTargets s = targets_at(entries + wave * 3 * K, K);
+  for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
+    float* saved = a.saved ? a.saved + p * (K + 1) : nullptr;
+    wave_fence();
+    if (!take_targets<TEACHER>(a.t, p, s, lane)) {
+      const bool wild = saved && wild_row(static_cast<const T*>(a.x) + p * a.C, a.C, lane);
+      if (lane == 0) {
+        a.rows[p] = 0.f;
+        a.code[p] = wild ? 2.f : 0.f;
+        if (saved) saved[0] = INFINITY;
+      }
+      continue;
+    }
+    const float* z = logits + p * V;
+    Soft m{-INFINITY, 0.f};
+    float sum = 0.f;
+    constexpr int kAt = 4;   // of a lane at a time
+    for (int v = lane; v < V; v += kAt * kWave) {
+      float u[kAt], top = -INFINITY, part = 0.f;
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        const int c = v + i * kWave;
+        u[i] = c < V ? z[c] + (a.shift ? a.shift[c] : 0.f) : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        sum += v + i * kWave < V ? u[i] : 0.f;
+        u[i] *= a.t.c1;
+        top = fmaxf(top, u[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) part += exp2_of(u[i] - finite_or_0(top));
+      m = join(m, Soft{top, part});
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+      m = join(m, Soft{__shfl_xor(m.m, o, kWave), __shfl_xor(m.s, o, kWave)});
+      sum += __shfl_xor(sum, o, kWave);
+    }
+    const float lse = m.m + log2f(m.s);
+    float loss = 0.f;
+    for (int k = lane; k < K; k += kWave) {
+      const int i = s.cls[k];
+      if (i < 0) continue;
+      const float q = s.q[k], u = (z[i] + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
+      if constexpr (TEACHER)
+        loss += q == 0.f ? 0.f : q * (log2f(q) - u + lse);
+      else
+        loss = (lse - u) * q;
+      if (saved) saved[1 + k] = u;
+    }
+    loss = wave_sum(loss);
+    if (lane == 0) {
+      if (!TEACHER && a.smoothing > 0.f) loss += a.smoothing * (lse - sum / (float)V * a.t.c1);
+      a.rows[p] = loss * a.factor;
+      a.code[p] = 1.f;
+      if (saved) saved[0] = lse;
+    }
+  }
+}
+
 // ---- the backward's rows ---------------------------------------------------------
 
 constexpr int kPrepBlocks = 1024;
@@ -561,7 +646,7 @@ struct TargetArgs {
   void* dz;
   unsigned long long* fixed;  // nullptr: none
 };
-// The targets' elements of a piece of dz, a wave a row.
+// The targets' elements of a piece of dz, a teacher's by a wave a row.
 template <typename T, bool TEACHER>
 __global__ void __launch_bounds__(kThreads)
 k_head_targets(TargetArgs a) {
@@ -570,6 +655,21 @@ k_head_targets(TargetArgs a) {
   const RowTargets s = targets_at(entries + wave * 3 * a.t.K, a.t.K);
   const int bits = fixed_bits(a.P);
   const float unit = a.top[1];
+  auto put = [&](int64_t p, float g, int i, float u, float lse, float q) __attribute__((always_inline)) {
+    const float d = g * (exp2_of(u - lse) - a.even - q);
+    static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
+    const double w = (double)g * (double)q;
+    if (a.fixed && __builtin_isfinite(w))
+      atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
+  };
+  if constexpr (!TEACHER) {   // a thread a row
+    for (int64_t p = blockIdx.x * (int64_t)kThreads + threadIdx.x; p < a.P; p += (int64_t)gridDim.x * kThreads) {
+      const float g = a.grow[p] * unit;
+      const int i = a.t.index(p, 0) - a.v0;
+      if (g != 0.f && i >= 0 && i < a.n) put(p, g, i, a.saved[2 * p + 1], a.saved[2 * p], a.t.label);
+    }
+    return;
+  }
   for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
     const float g = a.grow[p] * unit;
     if (g == 0.f || !take_targets<TEACHER>(a.t, p, s, lane)) continue;
@@ -578,11 +678,7 @@ k_head_targets(TargetArgs a) {
     for (int k = lane; k < a.t.K; k += kWave) {
       const int i = s.cls[k] - a.v0;
       if (s.cls[k] < 0 || i < 0 || i >= a.n) continue;
-      const float q = s.q[k], d = g * (exp2_of(saved[1 + k] - lse) - a.even - q);
-      static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
-      const double w = (double)g * (double)q;
-      if (a.fixed && __builtin_isfinite(w))
-        atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
+      put(p, g, i, saved[1 + k], lse, s.q[k]);
     }
     wave_fence();
   }
@@ -630,14 +726,17 @@ struct Sizes {
 
 struct FwdLayout {
   Plan p;
+  bool logits;
   int tc;
-  size_t x, w, stat, sums, rows, code, total;
+  size_t x, w, part, stat, sums, rows, code, total;
 };
 FwdLayout fwd_layout(const HeadShape& s) {
   const Sizes z(s);
   FwdLayout l{};
   l.p = plan(s.P, s.V, s.C, s.elem, false, false, 1);
-  l.tc = (int)ceil_div(s.V, kTile[l.p.tile].tc);
+  const int64_t dots = s.K * s.C * (int64_t)z.el();   // bytes a row
+  l.logits = s.V <= kLogitClasses && dots > 8 * s.V && s.P * dots >= kDotBytes && s.P * s.V * 4 <= kPieceBytes;
+  l.tc = l.logits ? 0 : (int)ceil_div(s.V, kTile[l.p.tile].tc);
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -646,6 +745,7 @@ FwdLayout fwd_layout(const HeadShape& s) {
   };
   l.x = take(z.ragged() ? z.x_bytes() : 0);
   l.w = take(z.w_bytes());
+  l.part = take(l.logits ? part_bytes(s.P, s.V, l.p) : 0);
   l.stat = take((size_t)s.P * l.tc * sizeof(float2));
   l.sums = take(!s.teacher && s.smoothing > 0.f ? (size_t)s.P * l.tc * sizeof(float) : 0);
   l.rows = take((size_t)s.P * sizeof(float));
@@ -755,22 +855,34 @@ hipError_t forward(const HeadShape& s, const void* x, const void* w, const float
     if (e == hipSuccess) e = launch_weight_lines(s.elem, w, s.V, s.C, ws + l.w, st);
     if (e != hipSuccess) return e;
   }
-  HeadArgs g = logits(s, xl, wl, shift, 0, s.V);
-  g.stat = reinterpret_cast<float2*>(ws + l.stat);
-  g.sums = !s.teacher && s.smoothing > 0.f ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
-  e = launch_product<T, true, true, HeadStats>(g, l.p, st);
-  if (e != hipSuccess) return e;
   RowsArgs a{};
+  float* z_all = reinterpret_cast<float*>(ws + l.part);
+  if (l.logits) {
+    LineProduct p{};
+    p.a = xl, p.b = wl, p.lda = p.ldb = z.up(s.C), p.a_along = p.b_along = true;
+    p.R = (int)s.P, p.N = (int)s.V, p.K = (int)s.C, p.tile = l.p.tile, p.splits = 1, p.klen = l.p.klen, p.part = z_all;
+    e = launch_line_product(s.elem, p, st);
+  } else {
+    HeadArgs g = logits(s, xl, wl, shift, 0, s.V);
+    a.stat = g.stat = reinterpret_cast<float2*>(ws + l.stat);
+    a.sums = g.sums = !s.teacher && s.smoothing > 0.f ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+    e = launch_product<T, true, true, HeadStats>(g, l.p, st);
+  }
+  if (e != hipSuccess) return e;
   a.t = targets_of(s, t);
-  a.x = x, a.w = w, a.shift = shift, a.stat = g.stat, a.sums = g.sums, a.saved = saved;
+  a.x = x, a.w = w, a.shift = shift, a.saved = saved;
   a.rows = s.mean ? reinterpret_cast<float*>(ws + l.rows) : loss;
   a.code = reinterpret_cast<float*>(ws + l.code);
   a.P = s.P, a.C = (int)s.C, a.tc = l.tc, a.smoothing = s.smoothing;
   const bool mean = s.mean || saved;
   a.loss = s.mean ? loss : nullptr, a.tail = saved ? saved + s.P * (s.K + 1) : nullptr;
-  a.alone = mean && s.P <= (s.teacher ? 1 : kWaves);
+  a.alone = mean && !l.logits && s.P <= (s.teacher ? 1 : kWaves);
   a.factor = (float)(0.69314718055994531 * scale_of(s) * scale_of(s));
-  if (s.teacher)
+  if (l.logits) {
+    const auto rows = s.teacher ? k_head_logits<T, true> : k_head_logits<T, false>;
+    hipLaunchKernelGGL(rows, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
+                       (unsigned)(kWaves * s.K * 12), st, a, z_all);
+  } else if (s.teacher)
     hipLaunchKernelGGL((k_head_rows<T, true>), dim3((unsigned)std::min(s.P, kMaxBlocks)), dim3(kThreads),
                        (unsigned)s.K * 12, st, a);
   else
@@ -814,10 +926,10 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
   const float even = s.teacher ? 0.f : s.smoothing / (float)s.V;
   for (int i = 0; i < l.pieces; ++i) {
     const int64_t v0 = (int64_t)i * l.n, n = std::min<int64_t>(l.n, s.V - v0);
+    const Products& plans = i + 1 < l.pieces ? l.all : l.last;
     HeadArgs g = logits(s, xl, wl, shift, v0, n);
     g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.top = top, g.even = even;
     g.y = ws + l.dz, g.ld = l.ld, g.colsum = cols ? cols + v0 : nullptr, g.cols_ld = s.V;
-    const Products& plans = i + 1 < l.pieces ? l.all : l.last;
     e = launch_product<T, true, true, HeadGradient>(g, plans.z, st);
     if (e != hipSuccess) return e;
     TargetArgs a{};
@@ -825,8 +937,8 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
     a.saved = saved, a.grow = grow, a.top = top, a.P = s.P, a.ld = l.ld;
     a.v0 = (int)v0, a.n = (int)n, a.even = even, a.dz = ws + l.dz, a.fixed = fixed;
     const auto targets = s.teacher ? k_head_targets<T, true> : k_head_targets<T, false>;
-    hipLaunchKernelGGL(targets, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
-                       (unsigned)(kWaves * s.K * 12), st, a);
+    hipLaunchKernelGGL(targets, dim3((unsigned)std::min(ceil_div(s.P, s.teacher ? kWaves : kThreads), kMaxBlocks)),
+                       dim3(kThreads), (unsigned)(kWaves * s.K * 12), st, a);
     e = hipGetLastError();
     if (e == hipSuccess && gr.dx) {
       LineProduct p{};

@@ -315,8 +315,8 @@ hipError_t launch_project_backward(const ProjectShape& s, const void* x, const v
                                    const void* z, const void* dy, const moce_project_grads& gr, void* ws,
                                    hipStream_t st);
 
-// out[r][c] = sum_k A[r][k] B[k][c], B by rows of ldb elements, A by rows of lda
-// (a_along) or [k][r]; rows of whole 16 bytes, cut as product.h's plan() has it
+// out[r][c] = sum_k A[r][k] B[k][c], A by rows of lda elements (a_along) or
+// [k][r], B by rows of ldb or (b_along, with a_along) [c][k]; rows of whole 16 bytes, cut as product.h's plan() has it
 // (tile, splits, klen).  part: [splits][R][N] float32, written or (add) added to,
 // and joined into y; without join y is not written.  Without part y is written directly.
 struct LineProduct {
@@ -328,7 +328,7 @@ struct LineProduct {
   int R, N, K, tile, splits, klen;
   void* y;               // [R][N]
   float* part;
-  bool a_along, add, join;
+  bool a_along, b_along, add, join;
 };
 hipError_t launch_line_product(int elem, const LineProduct& p, hipStream_t st);
 // The weight [O][C] in rows of whole 16 bytes.

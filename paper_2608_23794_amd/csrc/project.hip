@@ -886,7 +886,9 @@ hipError_t line_product(const LineProduct& p, hipStream_t st) {
   g.pick = p.pick, g.other = p.other, g.alpha = p.alpha;
   g.R = p.R, g.N = p.N, g.K = p.K, g.klen = p.klen, g.y = p.y, g.ld = p.N, g.part = p.part, g.add = p.add;
   const Plan c{p.tile, (int)ceil_div(p.K, p.klen), p.klen, 0.};
-  const hipError_t e = p.a_along ? launch_product<T, true, false>(g, c, st) : launch_product<T, false, false>(g, c, st);
+  const hipError_t e = !p.a_along  ? launch_product<T, false, false>(g, c, st)
+                       : p.b_along ? launch_product<T, true, true>(g, c, st)
+                                   : launch_product<T, true, false>(g, c, st);
   if (e != hipSuccess || !p.part || !p.join) return e;
   return launch_join<T>(g, p.splits, st);
 }
