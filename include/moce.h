@@ -525,7 +525,8 @@ moce_status moce_group_norm_backward(const moce_group_norm_desc* desc, const voi
  * weight[v][c] + shift[v] (moce_project gives the logits z themselves).  The
  * calls here take the loss of the logits and its gradients without keeping the
  * logits: the forward leaves the softmax statistics of a row, the backward
- * forms the logits again, in pieces of the classes.
+ * forms the logits again, in pieces of the classes.  Both keep at most 256 MB of
+ * logits or their gradient in the workspace, or 256 classes of all rows.
  *
  * Cross entropy with a label t[p], smoothed by e:
  *   loss[p] = lse - (1 - e) z[p][t] - e mean_v z[p][v],   lse = log sum_v e^z[p][v].
@@ -601,8 +602,9 @@ size_t moce_head_backward_workspace_bytes(const moce_head_desc* desc);
 
 /* The gradients.  The inputs as in the forward, saved as it wrote them; dloss:
  * float32 [P], or [1] for MOCE_LOSS_MEAN.  For bfloat16, dz enters the products
- * rounded to its type; sums are float32, and dshift takes dz as it is.  Rows
- * that are left out may hold anything, NaN too.  ws and errors as for the
+ * rounded to its type relative to the largest |g|; sums are float32, and dshift
+ * takes dz as it is (a row of less than 2^-35 of the largest |g| may not show in
+ * it).  Rows that are left out may hold anything, NaN too.  ws and errors as for the
  * forward; MOCE_ERR_NULL for a missing saved, dloss or grads.  Asynchronous on
  * `stream`. */
 moce_status moce_head_cross_entropy_backward(const moce_head_desc* desc, const void* x, const void* weight,

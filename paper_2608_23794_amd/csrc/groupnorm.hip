@@ -212,6 +212,10 @@ __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kVE<T>])
     store_vector(p, n, v);
 }
 
+// Bound by memory: 64 images of 256 channels at 56 x 56 in bfloat16 (103 MB a
+// tensor), the sums 23 us (4.5 TB/s), the elements 36; of the backward 37 (206
+// MB, 5.6 TB/s) and 48 (309 MB, 6.4 TB/s, some of it from the infinity cache).
+
 // f(image, part, first row, end, first channel, channels) for the parts of the launch
 template <typename T, typename F>
 __device__ __forceinline__ void each_rows(const NormArgs& a, F&& f) {
@@ -645,6 +649,10 @@ struct Columns {
 
 // ONE: a vector's channels are of one group.  A thread then sums them all, and
 // adds up its group's sums by itself.
+//
+// 64 images of 512 channels at 28 x 28 in bfloat16, 103 MB read and written, in
+// 23 us from the infinity cache; of 256 at 56 x 56, a workgroup a CU, 46 so and
+// 59 from memory (3.5 TB/s: one workgroup's reading does not overlap its writing).
 template <typename T, int NT, int N, bool ONE>
 __global__ void __launch_bounds__(NT)
 k_norm_span(NormArgs a) {
@@ -853,8 +861,8 @@ k_norm_span_backward(NormArgs a) {
   });
 }
 
-// Channels-first: a workgroup takes a group, tx threads (a power of two) a
-// plane, `each` vectors of it; a thread's planes follow each other NT / tx
+// Channels-first (64 images of 512 channels at 28 x 28 in bfloat16: 25 us, the
+// gradients 44): a workgroup takes a group, tx threads (a power of two) a plane, `each` vectors of it; a thread's planes follow each other NT / tx
 // apart.  Sums over a plane's threads are joined by its waves.
 constexpr int kMaxPlanes = 1024;
 template <typename T, int NT, int N, typename F>

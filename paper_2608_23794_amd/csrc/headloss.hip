@@ -51,6 +51,9 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
 }
 
 // ---- forward epilogue ------------------------------------------------------------
+// Bound by the products: 8192 rows of 4096 by 65536 classes in 3.28 ms, 1340
+// TFLOP/s (a library product that writes its results: 1457); 3152 of 768 by
+// 21841, twelve stages between the ends of a tile, 137 us, 772.
 // A lane holds 4 FC classes of each of its FR rows; four lanes share a row's
 // classes of the wave, WC waves the tile's.  (NaN is not a maximum, but makes
 // the sum NaN.)
@@ -129,7 +132,8 @@ struct HeadStats {
 // in behind the products: with it, equal weights of the rows are 1, and a
 // label's element, near -1, is rounded by its own small rest; within dz, the
 // rounding of g would be one factor of all rows' gradients (dx and dweight of
-// 8192 rows and 65536 classes were 3.3e-3 off in the 2-norm, not 1.7e-3).
+// 8192 rows and 65536 classes were 3.3e-3 off in the 2-norm, not 1.7e-3).  The
+// pieces of those take 3.48 ms, 6% more than the forward, which has no dz.
 template <typename T, int BYTES, int FR, int FC, int WR, int WC>
 struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
   using F = Finish<T, BYTES, FR, FC, WR, WC>;
@@ -395,7 +399,9 @@ k_head_mean(const float* rows, const float* code, int64_t P, float* loss, float*
 
 // The rows' losses, and what the backward reads.  Labels: a wave a row.  A
 // teacher: a workgroup a row, whose 16 groups of 16 lanes take the targets'
-// dot products (a wave for each: 3152 rows of 768 with 32 entries 77 us).
+// dot products (3152 rows of 768 with 32 entries: 39 us; a wave for each: 77).
+// Bound by the weight's rows: 64 entries of 4095 rows of 2048, 1.07 GB, in 167
+// us, 6.4 TB/s.
 template <typename T, bool TEACHER>
 __global__ void __launch_bounds__(kThreads)
 k_head_rows(RowsArgs a) {
@@ -705,8 +711,8 @@ k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned 
 // ---- launches --------------------------------------------------------------------
 
 // The gradient of the logits goes through the GPU in pieces of so many bytes,
-// which the infinity cache holds from the product that writes them to the two
-// that read them.
+// as many as the infinity cache has, from the product that writes them to the
+// two that read them.
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 constexpr int kPieceClasses = 256;   // a multiple of every tile and of whole lines
 constexpr int64_t kMaxBlocks = 1 << 20;
@@ -773,7 +779,7 @@ struct BwdLayout {
 };
 // How the classes are cut: evenly, or in pieces whose 256 x 256 tiles fill the
 // CUs in whole rounds, by the time of their products (4095 rows of 2048 by
-// 100003 classes: 7 rounds and not 6.1, 6.7 ms to 5.9).
+// 100003 classes: 7 rounds and not 6.1, loss and gradients 6.7 ms to 6.0).
 int64_t piece_of(const HeadShape& s) {
   const Sizes z(s);
   const int64_t most = std::max<int64_t>(kPieceBytes / (int64_t)(s.P * z.el()) / kPieceClasses, 1) * kPieceClasses;
