@@ -11,10 +11,10 @@
 // k_head_rows joins a row's tiles and takes the logits of its targets by dot
 // products of their own.  The backward forms the product again, in pieces of
 // the classes; its epilogue writes g softmax, rounded, and sums it over the
-// rows for dshift.  k_head_targets puts the targets' elements right (from
-// float32 values, so that p - q loses no digits), and a piece then goes through
-// the products of dx (whose partial sums are kept in float32 from piece to
-// piece) and dweight.  8 P V C operations in all, bound by the matrix cores
+// rows for dshift.  A label's element has its part taken off there; a teacher's
+// k_head_targets puts right (from float32 values too, so that p - q loses no
+// digits).  A piece then goes through the products of dx (whose partial sums
+// are kept in float32 from piece to piece) and dweight.  8 P V C operations in all, bound by the matrix cores
 // where C and P are large.
 //
 // Logits are taken in base 2: u = (z + shift) log2(e) / T.
@@ -23,17 +23,43 @@
 namespace moce {
 namespace {
 
+constexpr int kMaxEntries = 1024;   // of a teacher, a row
+constexpr int kWaves = kThreads / kWave;
+
+struct Targets {
+  const void *classes, *logits;
+  int K, V, wide, low;       // wide: classes of 64 bits; low: logits of 16
+  bool teacher;
+  float c1, label;           // log2(e) / T; the weight of a label
+
+  __device__ __forceinline__ int index(int64_t p, int k) const {   // -1: outside the classes
+    const int64_t at = p * K + k;
+    const int64_t v = wide ? static_cast<const int64_t*>(classes)[at] : static_cast<const int32_t*>(classes)[at];
+    return v >= 0 && v < V ? (int)v : -1;
+  }
+  __device__ __forceinline__ float logit(int64_t p, int k) const {
+    const int64_t at = p * K + k;
+    return low ? bf16_to_f32(static_cast<const uint16_t*>(logits)[at]) : static_cast<const float*>(logits)[at];
+  }
+};
+
+// A row as the backward's epilogue reads it.
+struct alignas(16) Row {
+  float lse, g;   // g of 0: the row is left out, or weighs nothing
+  int label;      // -1: none, or a teacher's
+  int reserved;
+};
 struct HeadArgs : GemmArgs {
   float c1;              // log2(e) / T
   // forward
   float2* stat;          // [R][tc] maximum and sum of 2^(u - maximum)
   float* sums;           // [R][tc] sums of z (nullptr: none)
   // backward
-  const float* lse;      // a row's, at lse_ld row
-  int64_t lse_ld;
-  const float* grow;     // [R] g; 0: the row is left out, or weighs nothing
+  const Row* info;       // [R]
   const float* top;      // the largest |g|, and 1 over it
   float even;            // e / V
+  float label;           // a label's weight
+  int v0;                // the piece's first class
   float* colsum;         // [rows of waves][cols_ld] sums of dz (nullptr: none)
   int64_t cols_ld;
 };
@@ -128,7 +154,8 @@ struct HeadStats {
 
 // ---- backward epilogue -----------------------------------------------------------
 // Eight classes a lane, in rows, as Finish has them: g / G (2^(u - lse) - e / V),
-// zeros behind the classes to the end of the line.  G, the largest |g|, comes
+// less a label's part (a teacher's is k_head_targets'), zeros behind the classes
+// to the end of the line.  G, the largest |g|, comes
 // in behind the products: with it, equal weights of the rows are 1, and a
 // label's element, near -1, is rounded by its own small rest; within dz, the
 // rounding of g would be one factor of all rows' gradients (dx and dweight of
@@ -161,22 +188,31 @@ struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
         }
       for (int it = 0; it < F::kIters; it += kBatch) {
         float v[kBatch][8], lse[kBatch], g[kBatch];
+        int label[kBatch];   // its place among the lane's eight
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
           const int row = this->row(f * kPer + it + b), r = min(row, h.R - 1);
-          lse[b] = h.lse[r * h.lse_ld];
-          g[b] = row < h.R ? h.grow[r] * unit : 0.f;
+          const Row q = h.info[r];
+          lse[b] = q.lse;
+          g[b] = row < h.R ? q.g * unit : 0.f;
+          label[b] = q.label - h.v0 - c;
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) this->value(l, it + b, v[b]);
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b)
+        for (int b = 0; b < kBatch; ++b) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[b][i] = exp2_of((v[b][i] + sh[i]) * h.c1 - lse[b]) - h.even;
+          if (__any((unsigned)label[b] < 8u)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[b][i] -= label[b] == i ? h.label : 0.f;
+          }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float p = exp2_of((v[b][i] + sh[i]) * h.c1 - lse[b]);
-            v[b][i] = g[b] == 0.f || i >= left ? 0.f : g[b] * (p - h.even);
+            v[b][i] = g[b] == 0.f || i >= left ? 0.f : g[b] * v[b][i];
             sum[i] += v[b][i];
           }
+        }
         if (left > 0) {
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
@@ -206,26 +242,6 @@ struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
 };
 
 // ---- targets ---------------------------------------------------------------------
-
-constexpr int kMaxEntries = 1024;   // of a teacher, a row
-constexpr int kWaves = kThreads / kWave;
-
-struct Targets {
-  const void *classes, *logits;
-  int K, V, wide, low;       // wide: classes of 64 bits; low: logits of 16
-  bool teacher;
-  float c1, label;           // log2(e) / T; the weight of a label
-
-  __device__ __forceinline__ int index(int64_t p, int k) const {   // -1: outside the classes
-    const int64_t at = p * K + k;
-    const int64_t v = wide ? static_cast<const int64_t*>(classes)[at] : static_cast<const int32_t*>(classes)[at];
-    return v >= 0 && v < V ? (int)v : -1;
-  }
-  __device__ __forceinline__ float logit(int64_t p, int k) const {
-    const int64_t at = p * K + k;
-    return low ? bf16_to_f32(static_cast<const uint16_t*>(logits)[at]) : static_cast<const float*>(logits)[at];
-  }
-};
 
 // A row's targets by one wave, kept in LDS (K of each): the classes (-1 for an
 // entry that counts for nothing or whose class came before) and their
@@ -569,7 +585,9 @@ struct PrepArgs {
   int C, ld, K, mean;
   float T;
   const float *saved, *dloss;
-  float *grow, *gmax;         // gmax: [kPrepBlocks] largest |g|, finite ones, of rows' weights
+  Targets t;
+  Row* info;
+  float* gmax;                // [kPrepBlocks] largest |g|, finite ones, of rows' weights
   float* top;                 // G and 1 / G: here of the mean, else by k_head_top
   unsigned long long* fixed;  // [V] cleared (nullptr: none)
   int V;
@@ -594,7 +612,7 @@ k_head_prep(PrepArgs a) {
     const bool there = a.saved[p * (a.K + 1)] != INFINITY;
     float g = 0.f;
     if (there) g = a.T * (a.mean ? a.dloss[0] / tail[0] : a.dloss[p]);
-    if (lane == 0) a.grow[p] = g;
+    if (lane == 0) a.info[p] = Row{a.saved[p * (a.K + 1)], g, a.t.teacher ? -1 : a.t.index(p, 0), 0};
     if (__builtin_isfinite(g)) top = fmaxf(top, fabsf(g));
     if (!copy) continue;
     const T* x = static_cast<const T*>(a.x) + p * a.C;
@@ -645,15 +663,15 @@ __host__ __device__ inline int fixed_bits(int64_t P) {
 
 struct TargetArgs {
   Targets t;
-  const float *saved, *grow, *top;
+  const Row* info;
+  const float *saved, *top;
   int64_t P, ld;
   int v0, n;                  // the piece's classes
-  float even;
   void* dz;
   unsigned long long* fixed;  // nullptr: none
 };
-// The targets' elements of a piece of dz, a teacher's by a wave a row.
-template <typename T, bool TEACHER>
+// A teacher's elements of a piece of dz, a wave a row.
+template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_head_targets(TargetArgs a) {
   extern __shared__ int entries[];   // a wave's targets
@@ -661,30 +679,20 @@ k_head_targets(TargetArgs a) {
   const RowTargets s = targets_at(entries + wave * 3 * a.t.K, a.t.K);
   const int bits = fixed_bits(a.P);
   const float unit = a.top[1];
-  auto put = [&](int64_t p, float g, int i, float u, float lse, float q) __attribute__((always_inline)) {
-    const float d = g * (exp2_of(u - lse) - a.even - q);
-    static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
-    const double w = (double)g * (double)q;
-    if (a.fixed && __builtin_isfinite(w))
-      atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
-  };
-  if constexpr (!TEACHER) {   // a thread a row
-    for (int64_t p = blockIdx.x * (int64_t)kThreads + threadIdx.x; p < a.P; p += (int64_t)gridDim.x * kThreads) {
-      const float g = a.grow[p] * unit;
-      const int i = a.t.index(p, 0) - a.v0;
-      if (g != 0.f && i >= 0 && i < a.n) put(p, g, i, a.saved[2 * p + 1], a.saved[2 * p], a.t.label);
-    }
-    return;
-  }
   for (int64_t p = blockIdx.x * (int64_t)kWaves + wave; p < a.P; p += (int64_t)gridDim.x * kWaves) {
-    const float g = a.grow[p] * unit;
-    if (g == 0.f || !take_targets<TEACHER>(a.t, p, s, lane)) continue;
+    const Row row = a.info[p];
+    const float g = row.g * unit;
+    if (g == 0.f || !take_targets<true>(a.t, p, s, lane)) continue;
     const float* saved = a.saved + p * (a.t.K + 1);
-    const float lse = saved[0];
+    const float lse = row.lse;
     for (int k = lane; k < a.t.K; k += kWave) {
       const int i = s.cls[k] - a.v0;
       if (s.cls[k] < 0 || i < 0 || i >= a.n) continue;
-      put(p, g, i, saved[1 + k], lse, s.q[k]);
+      const float q = s.q[k], d = g * (exp2_of(saved[1 + k] - lse) - q);
+      static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
+      const double w = (double)g * (double)q;
+      if (a.fixed && __builtin_isfinite(w))
+        atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
     }
     wave_fence();
   }
@@ -693,7 +701,7 @@ k_head_targets(TargetArgs a) {
 // dshift[v]: G times the sums over the rows' groups less the targets'.  16 classes a workgroup.
 __global__ void __launch_bounds__(kThreads)
 k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned long long* __restrict__ fixed,
-              const float* __restrict__ top, int bits, float* __restrict__ out) {
+              const float* __restrict__ top, int bits, float* __restrict__ out) {   // fixed: a teacher's
   __shared__ double s[kThreads];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, v = blockIdx.x * 16 + x;
   double t = 0.;
@@ -705,7 +713,8 @@ k_head_dshift(const float* __restrict__ part, int groups, int V, const unsigned 
   if (y != 0 || v >= V) return;
 #pragma unroll
   for (int i = 1; i < kThreads / 16; ++i) t += s[16 * i + x];
-  out[v] = (float)((double)top[0] * (t - ldexp((double)(long long)fixed[v], -bits)));
+  if (fixed) t -= ldexp((double)(long long)fixed[v], -bits);
+  out[v] = (float)((double)top[0] * t);
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -775,7 +784,7 @@ struct BwdLayout {
   Products all, last;      // of a piece, of the last one
   int n, pieces, groups;   // classes of a piece, pieces; groups of rows of dshift's sums
   int64_t ld;              // of a piece of dz
-  size_t x, w, grow, gmax, top, fixed, cols, dz, part, dx, total;
+  size_t x, w, info, gmax, top, fixed, cols, dz, part, dx, total;
 };
 // How the classes are cut: evenly, or in pieces whose 256 x 256 tiles fill the
 // CUs in whole rounds, by the time of their products (4095 rows of 2048 by
@@ -813,7 +822,7 @@ BwdLayout bwd_layout(const HeadShape& s) {
   };
   l.x = take(z.x_bytes());
   l.w = take(z.w_bytes());
-  l.grow = take((size_t)s.P * sizeof(float));
+  l.info = take((size_t)s.P * sizeof(Row));
   l.gmax = take(kPrepBlocks * sizeof(float));
   l.top = take(2 * sizeof(float));
   l.fixed = take((size_t)s.V * 8);
@@ -906,15 +915,16 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
   const Sizes z(s);
   const BwdLayout l = bwd_layout(s);
   const int blocks = (int)std::min<int64_t>(kPrepBlocks, ceil_div(s.P, kWaves));
-  float *grow = reinterpret_cast<float*>(ws + l.grow), *gmax = reinterpret_cast<float*>(ws + l.gmax);
+  Row* info = reinterpret_cast<Row*>(ws + l.info);
+  float* gmax = reinterpret_cast<float*>(ws + l.gmax);
   float* top = reinterpret_cast<float*>(ws + l.top);
-  unsigned long long* fixed = gr.dshift ? reinterpret_cast<unsigned long long*>(ws + l.fixed) : nullptr;
+  unsigned long long* fixed = gr.dshift && s.teacher ? reinterpret_cast<unsigned long long*>(ws + l.fixed) : nullptr;
   float* cols = gr.dshift ? reinterpret_cast<float*>(ws + l.cols) : nullptr;
   {
     PrepArgs a{};
     a.x = x, a.lines = z.ragged() || gr.dweight ? ws + l.x : nullptr, a.ragged = z.ragged(), a.P = s.P;
     a.C = (int)s.C, a.ld = (int)z.up(s.C), a.K = s.K, a.mean = s.mean, a.T = scale_of(s);
-    a.saved = saved, a.dloss = dloss, a.grow = grow, a.gmax = gmax, a.top = top, a.fixed = fixed;
+    a.t = targets_of(s, t), a.saved = saved, a.dloss = dloss, a.info = info, a.gmax = gmax, a.top = top, a.fixed = fixed;
     a.V = (int)s.V;
     hipLaunchKernelGGL(k_head_prep<T>, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
   }
@@ -934,18 +944,18 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
     const int64_t v0 = (int64_t)i * l.n, n = std::min<int64_t>(l.n, s.V - v0);
     const Products& plans = i + 1 < l.pieces ? l.all : l.last;
     HeadArgs g = logits(s, xl, wl, shift, v0, n);
-    g.lse = saved, g.lse_ld = s.K + 1, g.grow = grow, g.top = top, g.even = even;
+    g.info = info, g.top = top, g.even = even, g.label = 1.f - s.smoothing, g.v0 = (int)v0;
     g.y = ws + l.dz, g.ld = l.ld, g.colsum = cols ? cols + v0 : nullptr, g.cols_ld = s.V;
     e = launch_product<T, true, true, HeadGradient>(g, plans.z, st);
     if (e != hipSuccess) return e;
-    TargetArgs a{};
-    a.t = targets_of(s, t);
-    a.saved = saved, a.grow = grow, a.top = top, a.P = s.P, a.ld = l.ld;
-    a.v0 = (int)v0, a.n = (int)n, a.even = even, a.dz = ws + l.dz, a.fixed = fixed;
-    const auto targets = s.teacher ? k_head_targets<T, true> : k_head_targets<T, false>;
-    hipLaunchKernelGGL(targets, dim3((unsigned)std::min(ceil_div(s.P, s.teacher ? kWaves : kThreads), kMaxBlocks)),
-                       dim3(kThreads), (unsigned)(kWaves * s.K * 12), st, a);
-    e = hipGetLastError();
+    if (s.teacher) {
+      TargetArgs a{};
+      a.t = targets_of(s, t), a.info = info, a.saved = saved, a.top = top, a.P = s.P, a.ld = l.ld;
+      a.v0 = (int)v0, a.n = (int)n, a.dz = ws + l.dz, a.fixed = fixed;
+      hipLaunchKernelGGL(k_head_targets<T>, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
+                         (unsigned)(kWaves * s.K * 12), st, a);
+      e = hipGetLastError();
+    }
     if (e == hipSuccess && gr.dx) {
       LineProduct p{};
       p.a = ws + l.dz, p.lda = l.ld, p.a_along = true;
