@@ -533,3 +533,53 @@ def test_the_weight_is_not_rounded_with_every_element():
             for n in ("dx", "dweight"):
                 far = (got[n].double() - want[n]).norm() / want[n].norm()
                 assert float(far) <= 2.0 ** -8 / 3 ** 0.5, (weight, reduction, n, float(far))
+
+
+@pytest.mark.parametrize("P,C,V,K,T", [(1, 40, 5000, 1024, 2.0), (70, 64, 300, 1000, 4.0), (5, 768, 1, 3, 1.0), (300, 48, 2, 1024, 0.25),
+                                       (40, 1, 700, 20, 100.0), (130, 33, 1030, 257, 1e-2)])
+def test_many_entries_and_extreme_temperatures(P, C, V, K, T):
+    for dtype in (F, H):
+        x, w, b, g = make(P, C, V, dtype, seed=3, spread=1.0)
+        cls, logits = entries(P, K, V, g, dtype)
+        head = HeadLoss(w, b)
+        dloss = torch.full((1,), 2.0, device="cuda")
+        got = both_teacher(head, x, cls, logits, dloss, T)
+        target, there = teacher_target(cls, logits, V, T)
+        want, tol = reference(x, w, b, target, there, T, dloss, True, True)
+        # the teacher's own exponents, l log2(e) / T in float32, are off by 2^-23 of themselves: so much of q, and of
+        # what q weighs
+        off = 2.0 ** -22 * float(logits.double().abs().max()) / T * 2
+        wd, xd = w.double().abs(), x.double().abs()
+        dq = target * off * 2.0 * T / P
+        tol["dx"] = tol["dx"] + torch.matmul(dq, wd)
+        tol["dweight"] = tol["dweight"] + torch.matmul(dq.t().contiguous(), xd)
+        # its targets' share is in whole numbers of 2^-35 of the largest |g| or finer, 2^-51 with so few rows
+        tol["dshift"] = tol["dshift"] + dq.sum(0) + 2.0 ** -51 * 2.0 * T
+        z = torch.matmul(xd, wd.t().contiguous()).max() + b.double().abs().max()
+        tol["loss"] = tol["loss"] + T * T * off * (float(z) / T * 2 + 2 * math.log(max(V, 2)) + 20)
+        check(got, want, tol)
+
+
+def test_calls_at_once():
+    """Two heads' steps on two streams, each with its own buffers, as they are one after the other."""
+    jobs = []
+    for i, (P, C, V) in enumerate([(300, 256, 4000), (700, 520, 1500)]):
+        x, w, b, g = make(P, C, V, H, seed=i)
+        jobs.append((HeadLoss(w, b), x, torch.randint(-2, V, (P,), generator=g, device="cuda"), *entries(P, 7, V, g)))
+    one = torch.ones(1, device="cuda")
+
+    def step(head, x, labels, cls, logits):
+        return list(both(head, x, labels, one, 0.1).values()) + list(both_teacher(head, x, cls, logits, one, 2.0).values())
+
+    want = [step(*j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[], []]
+    for _ in range(5):
+        for i, j in enumerate(jobs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(step(*j))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for run in got[i]:
+            assert all(torch.equal(a, c) for a, c in zip(run, want[i]))
