@@ -188,15 +188,19 @@ __device__ __forceinline__ void sum_params(const NormArgs& a, int block, float2*
 
 constexpr int kAhead = 4;   // rows whose loads are in flight together
 
-// Up to kVE channels at p, n of them there (WHOLE: all, aligned); zeros behind them.
+// Up to kVE channels at p, n of them there (WHOLE: all, aligned), of a row of
+// ld; zeros behind them.  A row's last ones are read with those before them.
 template <typename T, bool WHOLE>
-__device__ __forceinline__ u32x4 load_row(const T* p, int n) {
+__device__ __forceinline__ u32x4 load_row(const T* p, int n, int64_t ld) {
   if constexpr (WHOLE) return *reinterpret_cast<const u32x4*>(p);
   T t[kVE<T>] = {};
   u32x4 v;
-  if (n >= kVE<T>) {
-    __builtin_memcpy(&v, p, 16);
-    return v;
+  if (n >= kVE<T> || ld >= kVE<T>) {
+    const int before = max(kVE<T> - n, 0);
+    __builtin_memcpy(&v, p - before, 16);
+    unsigned __int128 u = __builtin_bit_cast(unsigned __int128, v);
+    u >>= before * (int)sizeof(T) * 8;
+    return __builtin_bit_cast(u32x4, u);
   }
 #pragma unroll
   for (int i = 0; i < kVE<T>; ++i)
@@ -235,14 +239,14 @@ __device__ __forceinline__ void over_rows(const T* const (&p)[M], int64_t base, 
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-      for (int m = 0; m < M; ++m) v[i][m] = load_row<T, WHOLE>(p[m] + base + (r + i * down) * ld, n);
+      for (int m = 0; m < M; ++m) v[i][m] = load_row<T, WHOLE>(p[m] + base + (r + i * down) * ld, n, ld);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) f(base + (r + i * down) * ld, v[i]);
   }
   for (; r < r1; r += down) {
     u32x4 v[M];
 #pragma unroll
-    for (int m = 0; m < M; ++m) v[m] = load_row<T, WHOLE>(p[m] + base + r * ld, n);
+    for (int m = 0; m < M; ++m) v[m] = load_row<T, WHOLE>(p[m] + base + r * ld, n, ld);
     f(base + r * ld, v);
   }
 }
@@ -259,9 +263,9 @@ k_norm_sums_rows(NormArgs a) {
     const T* const x[1] = {static_cast<const T*>(a.x)};
     const int64_t base = b * a.hw * a.C + c;
     float first[VE] = {}, p[VE] = {}, s1[VE] = {}, s2[VE] = {}, m = 0.f;
-    if (n > 0) unpack<T>(load_row<T, WHOLE>(x[0] + base + (int64_t)k * a.len * a.C, n), first);
+    if (n > 0) unpack<T>(load_row<T, WHOLE>(x[0] + base + (int64_t)k * a.len * a.C, n, a.C), first);
     if (n > 0 && r < r1) {
-      unpack<T>(load_row<T, WHOLE>(x[0] + base + (int64_t)r * a.C, n), p);
+      unpack<T>(load_row<T, WHOLE>(x[0] + base + (int64_t)r * a.C, n, a.C), p);
       over_rows<T, WHOLE, 1>(x, base, a.C, r, r1, down, n, [&](int64_t, const u32x4 (&q)[1]) __attribute__((always_inline)) {
         float v[VE];
         unpack<T>(q[0], v);
