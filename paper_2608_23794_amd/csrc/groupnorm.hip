@@ -1237,11 +1237,12 @@ Layout layout_of(const GroupShape& s, bool back) {
   // Few groups of few channels, whole ones in a workgroup, and few parts: joined
   // by the kernels that read them, which saves a launch (8 images of 64 channels
   // at 56 x 56: backward 21 to 17 us).  Each of their workgroups does so: of
-  // many, the launch is cheaper (64 images of 256 channels: 96 us either way).
+  // many, the launch is cheaper (64 images of 256 channels: dx 58 us, not 48 and
+  // 6 for the launch).
   if (l.rows && l.threads == 0) {
     const int64_t cg = s.C / s.G, width = l.tx * (s.elem == MOCE_F32 ? 4 : 8), groups = width / cg;
     if (cg <= 32 && width % cg == 0 && groups * ceil_div(s.HW, l.len) <= 2048 &&
-        s.B * ceil_div(s.HW, l.len) * l.across <= 1024)
+        s.B * ceil_div(s.HW, l.len) * l.across <= 512)
       l.fold = (int)groups;
   }
   l.group_parts = take(l.fold ? (size_t)s.B * s.G * l.chunks * (back ? sizeof(float2) : sizeof(Part)) : 0);

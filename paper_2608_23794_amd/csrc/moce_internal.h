@@ -316,7 +316,8 @@ hipError_t launch_project_backward(const ProjectShape& s, const void* x, const v
                                    hipStream_t st);
 
 // out[r][c] = sum_k A[r][k] B[k][c], A by rows of lda elements (a_along) or
-// [k][r], B by rows of ldb or (b_along, with a_along) [c][k]; rows of whole 16 bytes, cut as product.h's plan() has it
+// [k][r], B by rows of ldb or (b_along, with a_along, into part as it is: no
+// add, join, pick or alpha) [c][k]; rows of whole 16 bytes, cut as product.h's plan() has it
 // (tile, splits, klen).  part: [splits][R][N] float32, written or (add) added to,
 // and joined into y; without join y is not written.  Without part y is written directly.
 struct LineProduct {

@@ -42,13 +42,16 @@ struct GemmArgs {
   int64_t ld, img;
   int hw;
   float* part;            // [split][R][N] partial products in the place of y (nullptr: none)
-  int add;                // to what the partial products hold
   const float *scale, *shift;
   int per_row;            // scale and shift by row (else by column)
   int act;
-  const float* alpha;     // of everything, instead of scale and shift (nullptr: 1)
-  // where *pick is not 0, b lies at `other` (nullptr: no choice)
-  const float* pick;
+};
+// A product of the heads' gradients.  (In GemmArgs these cost the projections 2
+// to 4%: 50432 tokens of 768 by 768, 97 us and not 93.)
+struct LineArgs : GemmArgs {
+  int add;                // to what the partial products hold
+  const float* alpha;     // a factor of everything (nullptr: 1)
+  const float* pick;      // where *pick is not 0, b lies at `other` (nullptr: no choice)
   const void* other;
 };
 
@@ -207,18 +210,20 @@ __device__ __forceinline__ float act_gradient(float z, float dy, int act) {
 // Eight neighbouring columns c.. of row r, from the float32 products v: into
 // the partial products, or through scale, shift, residual and activation into
 // z and y.  sc, sh: those of the eight columns (per column only).
-template <typename T>
-__device__ __forceinline__ void finish8(const GemmArgs& g, int r, int c, int split, float (&v)[8],
+template <typename T, typename G>
+__device__ __forceinline__ void finish8(const G& g, int r, int c, int split, float (&v)[8],
                                         const float (&sc)[8], const float (&sh)[8]) {
   using E = Elem<T>;
   if (r >= g.R || c >= g.N) return;
   const int n = min(8, g.N - c);
   if (g.part) {
     float* p = g.part + ((int64_t)split * g.R + r) * g.N + c;
-    if (g.add) {
+    if constexpr (std::is_same_v<G, LineArgs>) {
+      if (g.add) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) v[i] += p[i];
+        for (int i = 0; i < 8; ++i)
+          if (i < n) v[i] += p[i];
+      }
     }
     if (n == 8) {
       store8(p, v);
@@ -272,11 +277,18 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, int r, int c, int spl
   }
 }
 // scale and shift of columns c.. (ones and zeros where they go by row, or are not there)
-__device__ __forceinline__ void column_affine(const GemmArgs& g, int c, float (&sc)[8], float (&sh)[8]) {
+template <typename G>
+__device__ __forceinline__ void column_affine(const G& g, int c, float (&sc)[8], float (&sh)[8]) {
+  if constexpr (std::is_same_v<G, LineArgs>) {   // no scale and shift
+    const float a = g.alpha ? *g.alpha : 1.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sc[i] = a, sh[i] = 0.f;
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int j = min(c + i, g.N - 1);
-    sc[i] = g.alpha ? *g.alpha : g.scale && !g.per_row ? g.scale[j] : 1.f;
+    sc[i] = g.scale && !g.per_row ? g.scale[j] : 1.f;
     sh[i] = g.shift && !g.per_row ? g.shift[j] : 0.f;
   }
 }
@@ -389,8 +401,8 @@ __device__ __forceinline__ bool tile_of(const GemmArgs& g, int& r, int& c, int& 
 // c of a row lies at c ^ (row & 7).  A lane takes eight columns c of one row
 // in kDown; those that are not all there, or pass from one image to the next,
 // go through finish8.
-template <typename T, int BYTES, int FR, int FC, int WR, int WC>
-struct Finish {
+template <typename G, typename T, int BYTES, int FR, int FC, int WR, int WC>
+struct FinishOf {
   static constexpr int kPitch = FC * 64, kAcross = 2 * FC, kDown = kWave / kAcross, kAll = FR * 16 / kDown;
   static constexpr int kFrags = BYTES / (16 * kPitch) < FR ? BYTES / (16 * kPitch) : FR;   // of rows at a time
   static constexpr int kIters = kFrags * 16 / kDown, kBatch = kIters < 4 ? kIters : 4;
@@ -400,13 +412,13 @@ struct Finish {
   static constexpr bool kAhead = FR * FC * sizeof(T) <= 32;
   typedef T T8 __attribute__((ext_vector_type(8)));
 
-  const GemmArgs& g;
+  const G& g;
   int x, down, r0, c;
   bool fit;        // the lane's eight columns lie side by side
   int64_t at;      // of the first within a row
   T8 ahead[kAhead ? kAll : 1];
 
-  __device__ __forceinline__ Finish(const GemmArgs& g, int r0, int c0, int lane)
+  __device__ __forceinline__ FinishOf(const G& g, int r0, int c0, int lane)
       : g(g), x(lane % kAcross), down(lane / kAcross), r0(r0), c(c0 + 8 * x) {
     at = c;
     fit = c + 8 <= g.N;
@@ -529,6 +541,11 @@ struct Finish {
     }
   }
 };
+
+template <typename T, int BYTES, int FR, int FC, int WR, int WC>
+using Finish = FinishOf<GemmArgs, T, BYTES, FR, FC, WR, WC>;
+template <typename T, int BYTES, int FR, int FC, int WR, int WC>
+using LineFinish = FinishOf<LineArgs, T, BYTES, FR, FC, WR, WC>;
 
 template <int FR, int FC>
 __device__ __forceinline__ void clear(f32x4 (&acc)[FR][FC]) {
@@ -688,9 +705,13 @@ k_project(G g) {
   Copier<T, BK, BK && IMG, TC, true, NT> cb;
   constexpr int kRounds = ca.kRounds + cb.kRounds;
   ca.init(g.a, r0, g.R, k0, tid);
-  Operand b = g.b;
-  if (g.pick && *g.pick != 0.f) b.p = g.other;
-  cb.init(b, c0, g.N, k0, tid);
+  if constexpr (std::is_same_v<G, LineArgs>) {
+    Operand b = g.b;
+    if (g.pick && *g.pick != 0.f) b.p = g.other;
+    cb.init(b, c0, g.N, k0, tid);
+  } else {
+    cb.init(g.b, c0, g.N, k0, tid);
+  }
   f32x4 acc[FR][FC];
   clear(acc);
   // A stage goes in four phases: step 0 and 1, the upper and lower half of the

@@ -119,9 +119,9 @@ k_project_few(GemmArgs g) {
 // eight columns a thread, `down` threads (a power of two) taking every
 // down-th split.  Bound by memory, mostly the cache's (64 rows of 4096: 5 us).
 constexpr int kJoinMany = 16;   // splits from which on eight threads share them
-template <typename T>
+template <typename T, typename G>
 __global__ void __launch_bounds__(kThreads)
-k_project_join(GemmArgs g, int splits, int down) {
+k_project_join(G g, int splits, int down) {
   __shared__ float part[kThreads][8 + 1];
   const int across = kThreads / down, per = (g.N + 7) / 8;
   const int64_t u = (int64_t)blockIdx.x * across + threadIdx.x % across;
@@ -152,7 +152,7 @@ k_project_join(GemmArgs g, int splits, int down) {
       for (int i = 0; i < 8; ++i) v[i] += part[d * across + threadIdx.x][i];
   }
   if (r >= g.R) return;
-  GemmArgs h = g;
+  G h = g;
   h.part = nullptr;
   float sc[8], sh[8];
   column_affine(h, c, sc, sh);
@@ -493,10 +493,10 @@ k_project_lines(Lines t) {
 
 // ---- launches --------------------------------------------------------------------
 
-template <typename T>
-hipError_t launch_join(const GemmArgs& g, int splits, hipStream_t st) {
+template <typename T, typename G>
+hipError_t launch_join(const G& g, int splits, hipStream_t st) {
   const int down = splits >= kJoinMany ? 8 : 1;
-  hipLaunchKernelGGL(k_project_join<T>, dim3((unsigned)ceil_div((int64_t)g.R * ceil_div(g.N, 8), kThreads / down)),
+  hipLaunchKernelGGL((k_project_join<T, G>), dim3((unsigned)ceil_div((int64_t)g.R * ceil_div(g.N, 8), kThreads / down)),
                      dim3(kThreads), 0, st, g, splits, down);
   return hipGetLastError();
 }
@@ -881,14 +881,14 @@ hipError_t backward(const ProjectShape& s, const void* x, const void* w, const f
 
 template <typename T>
 hipError_t line_product(const LineProduct& p, hipStream_t st) {
-  GemmArgs g{};
+  LineArgs g{};
   g.a = Operand{p.a, p.lda, 0, 0}, g.b = Operand{p.b, p.ldb, 0, 0};
-  g.pick = p.pick, g.other = p.other, g.alpha = p.alpha;
-  g.R = p.R, g.N = p.N, g.K = p.K, g.klen = p.klen, g.y = p.y, g.ld = p.N, g.part = p.part, g.add = p.add;
+  g.pick = p.pick, g.other = p.other, g.alpha = p.alpha, g.add = p.add;
+  g.R = p.R, g.N = p.N, g.K = p.K, g.klen = p.klen, g.y = p.y, g.ld = p.N, g.part = p.part;
   const Plan c{p.tile, (int)ceil_div(p.K, p.klen), p.klen, 0.};
-  const hipError_t e = !p.a_along  ? launch_product<T, false, false>(g, c, st)
-                       : p.b_along ? launch_product<T, true, true>(g, c, st)
-                                   : launch_product<T, true, false>(g, c, st);
+  if (p.b_along) return launch_product<T, true, true>(static_cast<const GemmArgs&>(g), c, st);   // into part, no more
+  const hipError_t e = p.a_along ? launch_product<T, true, false, LineFinish>(g, c, st)
+                                 : launch_product<T, false, false, LineFinish>(g, c, st);
   if (e != hipSuccess || !p.part || !p.join) return e;
   return launch_join<T>(g, p.splits, st);
 }
