@@ -603,8 +603,8 @@ size_t moce_head_backward_workspace_bytes(const moce_head_desc* desc);
 /* The gradients.  The inputs as in the forward, saved as it wrote them; dloss:
  * float32 [P], or [1] for MOCE_LOSS_MEAN.  For bfloat16, dz enters the products
  * rounded to its type relative to the largest |g|; sums are float32, and dshift
- * takes dz as it is (a row of less than 2^-35 of the largest |g| may not show in
- * it).  Rows that are left out may hold anything, NaN too.  ws and errors as for the
+ * takes dz as it is (of a teacher, a row of less than 2^-35 of the largest |g|
+ * may not show in it).  Rows that are left out may hold anything, NaN too.  ws and errors as for the
  * forward; MOCE_ERR_NULL for a missing saved, dloss or grads.  Asynchronous on
  * `stream`. */
 moce_status moce_head_cross_entropy_backward(const moce_head_desc* desc, const void* x, const void* weight,

@@ -223,8 +223,9 @@ __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kVE<T>])
 }
 
 // Bound by memory: 64 images of 256 channels at 56 x 56 in bfloat16 (103 MB a
-// tensor), the sums 23 us (4.5 TB/s), the elements 36; of the backward 37 (206
-// MB, 5.6 TB/s) and 48 (309 MB, 6.4 TB/s, some of it from the infinity cache).
+// tensor), the backward's sums 34 us (206 MB, 6.1 TB/s, some of it from the
+// infinity cache), its elements 49 (309 MB); two maps of 128 at 512 x 384, as
+// large, forward 18 (5.5 TB/s) and 36.
 
 // f(image, part, first row, end, first channel, channels) for the parts of the launch
 template <typename T, typename F>
