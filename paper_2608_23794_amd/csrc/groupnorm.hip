@@ -233,7 +233,7 @@ __device__ __forceinline__ void each_rows(const NormArgs& a, F&& f) {
   const int x = threadIdx.x % a.tx, c = (blockIdx.y * a.tx + x) * kVE<T>;
   for (int64_t u = blockIdx.x - a.params; u < a.B * a.chunks; u += gridDim.x - a.params) {
     const int64_t b = u / a.chunks;
-    const int k = (int)(u - b * a.chunks), r0 = k * a.len, r1 = min(a.hw, r0 + a.len);
+    const int k = (int)(u - b * a.chunks), r0 = k * a.len, r1 = r0 + min(a.len, a.hw - r0);
     f(b, k, r0 + (int)threadIdx.x / a.tx, r1, c, min(kVE<T>, a.C - c));
   }
 }
@@ -305,7 +305,7 @@ k_norm_sums_rows(NormArgs a) {
     }
     if (!a.fold) return;
     __syncthreads();
-    const int g = blockIdx.y * a.fold + threadIdx.x, rows = min(a.hw, (k + 1) * a.len) - k * a.len;
+    const int g = blockIdx.y * a.fold + threadIdx.x, rows = min(a.len, a.hw - k * a.len);
     if ((int)threadIdx.x < a.fold && g < a.G) {   // equal counts: the mean of the means
       const Part* o = channels + threadIdx.x * a.cg;
       double mean = 0., m2 = 0.;
@@ -491,29 +491,32 @@ k_norm_dx_rows(NormArgs a) {
 
 // ---- channels-first: tx lanes take a plane's part, eight positions each ------------
 
-// f(image, channel, part, first position, end) for the planes' parts of the launch;
-// all lanes of a wave call it together
+// f(image, channel, part, the lane's first position, positions from it to the
+// part's end, none where that is not above 0) for the planes' parts of the
+// launch; all lanes of a wave call it together.  A plane may have all of 2^31 - 1
+// positions: what lies behind its end has no 32-bit number, so positions are
+// 64 bits and ends are counts.
 template <typename F>
 __device__ __forceinline__ void each_planes(const NormArgs& a, F&& f) {
   const int64_t parts = a.B * a.C * a.chunks, per = kThreads / a.tx;
   for (int64_t u0 = blockIdx.x * per; u0 < parts; u0 += gridDim.x * per) {
     const int64_t u = u0 + threadIdx.x / a.tx, plane = min(u, parts - 1) / a.chunks, b = plane / a.C;
-    const int k = (int)(min(u, parts - 1) - plane * a.chunks), p0 = k * a.len;
-    const int p1 = u < parts ? min(a.hw, p0 + a.len) : p0;
-    f(b, (int)(plane - b * a.C), k, p0 + (int)(threadIdx.x % a.tx) * 8, p1, u < parts && threadIdx.x % a.tx == 0);
+    const int k = (int)(min(u, parts - 1) - plane * a.chunks), p0 = k * a.len, x = threadIdx.x % a.tx;
+    const int count = u < parts ? min(a.len, a.hw - p0) : 0;
+    f(b, (int)(plane - b * a.C), k, (int64_t)p0 + x * 8, count - x * 8, u < parts && x == 0);
   }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_norm_sums_planes(NormArgs a) {
-  each_planes(a, [&](int64_t b, int c, int k, int p, int p1, bool lead) __attribute__((always_inline)) {
+  each_planes(a, [&](int64_t b, int c, int k, int64_t p, int left, bool lead) __attribute__((always_inline)) {
     const T* x = static_cast<const T*>(a.x) + (b * a.C + c) * a.hw;
     float q = 0.f, s1 = 0.f, s2 = 0.f, m = 0.f;
     const float first = Elem<T>::to_f(x[min(k * a.len, a.hw - 1)]);
-    if (p < p1) q = Elem<T>::to_f(x[p]);
-    for (; p < p1; p += 8 * a.tx) {
-      const int n = min(8, p1 - p);
+    if (left > 0) q = Elem<T>::to_f(x[p]);
+    for (; left > 0; left -= 8 * a.tx, p += 8 * a.tx) {
+      const int n = min(8, left);
       float v[8];
       load_n(x + p, n, v);
 #pragma unroll
@@ -534,11 +537,11 @@ k_norm_sums_planes(NormArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_norm_apply_planes(NormArgs a) {
-  each_planes(a, [&](int64_t b, int c, int, int p, int p1, bool) __attribute__((always_inline)) {
+  each_planes(a, [&](int64_t b, int c, int, int64_t p, int left, bool) __attribute__((always_inline)) {
     const int64_t base = (b * a.C + c) * a.hw;
     const Channel q = channel(a, b, c);
-    for (; p < p1; p += 8 * a.tx) {
-      const int n = min(8, p1 - p);
+    for (; left > 0; left -= 8 * a.tx, p += 8 * a.tx) {
+      const int n = min(8, left);
       float v[8];
       load_n(static_cast<const T*>(a.x) + base + p, n, v);
 #pragma unroll
@@ -551,12 +554,12 @@ k_norm_apply_planes(NormArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_norm_dsums_planes(NormArgs a) {
-  each_planes(a, [&](int64_t b, int c, int k, int p, int p1, bool first) __attribute__((always_inline)) {
+  each_planes(a, [&](int64_t b, int c, int k, int64_t p, int left, bool first) __attribute__((always_inline)) {
     const int64_t base = (b * a.C + c) * a.hw;
     const Channel q = channel(a, b, c);
     float s0 = 0.f, s1 = 0.f;
-    for (; p < p1; p += 8 * a.tx) {
-      const int n = min(8, p1 - p);
+    for (; left > 0; left -= 8 * a.tx, p += 8 * a.tx) {
+      const int n = min(8, left);
       float v[8], d[8];
       load_n(static_cast<const T*>(a.x) + base + p, n, v);
       load_n(static_cast<const T*>(a.dy) + base + p, n, d);
@@ -578,12 +581,12 @@ k_norm_dsums_planes(NormArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_norm_dx_planes(NormArgs a) {
-  each_planes(a, [&](int64_t b, int c, int, int p, int p1, bool) __attribute__((always_inline)) {
+  each_planes(a, [&](int64_t b, int c, int, int64_t p, int left, bool) __attribute__((always_inline)) {
     const int64_t base = (b * a.C + c) * a.hw;
     const Channel q = channel(a, b, c);
     const float2 m = a.means[b * a.G + c / a.cg];
-    for (; p < p1; p += 8 * a.tx) {
-      const int n = min(8, p1 - p);
+    for (; left > 0; left -= 8 * a.tx, p += 8 * a.tx) {
+      const int n = min(8, left);
       float v[8], d[8];
       load_n(static_cast<const T*>(a.x) + base + p, n, v);
       load_n(static_cast<const T*>(a.dy) + base + p, n, d);

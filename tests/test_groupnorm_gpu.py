@@ -381,3 +381,60 @@ def test_empty_and_refusals():
                dict(groups=4, layout="chw")):
         with pytest.raises(ValueError):
             GroupNormLayer(**kw)
+
+
+@pytest.mark.parametrize("dtype,B,H,W,layout", [
+    ("bf16", 1, 46340, 46340, "nchw"), ("bf16", 2, (1 << 31) - 1, 1, "nhwc"), ("f32", 1, (1 << 31) - 1, 1, "nchw"),
+])
+def test_a_plane_of_all_positions_there_can_be(dtype, B, H, W, layout):
+    """One channel whose last part ends at 2^31 - 1 positions, or whose parts' multiples pass it.
+
+    The last 174096 positions hold other values, so that statistics and sums without them are far off: their mean of 40
+    adds 0.13 to a variance of 1, their dy of 30 adds 5.2e6 to dshift.  A lane adds up to 2^13 values before its sums
+    are joined, so sums are right to 2^13 x 2^-24 = 2^-11 of their values' sizes, which are about one deviation: a mean
+    to 2^-10 of one (sums are taken about a lane's first value, itself about one away), rstd to 2^-10 of itself."""
+    n, last, chunk = H * W, 174096, 1 << 26
+    shape = (B, 1, H, W) if layout == "nchw" else (B, H, W, 1)
+    x = torch.empty((B, n), dtype=TYPES[dtype], device="cuda").normal_(0.5, 1.0)
+    dy = torch.empty_like(x).normal_()
+    x[:, -last:] += 40
+    dy[:, -last:] = 30
+    scale, shift = torch.full((1,), 1.5, device="cuda"), torch.full((1,), 0.25, device="cuda")
+    layer = GroupNormLayer(1, scale, shift, layout=layout)
+    stats = layer.new_stats(shape)
+    y = torch.full_like(x, math.nan)
+    layer.forward(x.view(shape), y=y.view(shape), stats=stats)
+
+    def sums(b, f):
+        return sum(f(slice(i, i + chunk)).sum() for i in range(0, n, chunk))
+
+    m = [sums(b, lambda s: x[b, s].double()) / n for b in range(B)]
+    r = [1 / torch.sqrt(sums(b, lambda s: (x[b, s].double() - m[b]).square()) / n + 1e-5) for b in range(B)]
+    off = 2.0 ** -10
+    for b in range(B):
+        assert abs(float((stats[0, b, 0].double() - m[b]) * r[b])) <= off
+        assert abs(float(stats[1, b, 0].double() / r[b]) - 1) <= off
+        for i in range(0, n, chunk):
+            h = (x[b, i:i + chunk].double() - m[b]) * r[b]
+            z = 1.5 * h + 0.25
+            tol = 1.5 * off * (1 + h.abs()) * 1.01
+            tol = tol + HALF[x.dtype] * (z.abs() + tol)
+            assert ((y[b, i:i + chunk].double() - z).abs() <= tol).all()
+    out = layer.backward(x.view(shape), dy.view(shape), stats, dx=y.fill_(math.nan).view(shape))
+    sizes, dshift, dscale, worst = 0.0, 0.0, 0.0, 0.0
+    for b in range(B):
+        m[b], r[b] = stats[0, b, 0].double(), stats[1, b, 0].double()      # the gradients of these
+        t0 = sums(b, lambda s: dy[b, s].double())
+        t1 = sums(b, lambda s: dy[b, s].double() * (x[b, s].double() - m[b]) * r[b])
+        a0 = sums(b, lambda s: dy[b, s].double().abs())
+        a1 = sums(b, lambda s: (dy[b, s].double() * (x[b, s].double() - m[b]) * r[b]).abs())
+        dshift, dscale, sizes, worst = dshift + t0, dscale + t1, sizes + a0, worst + a1
+        for i in range(0, n, chunk):
+            h = (x[b, i:i + chunk].double() - m[b]) * r[b]
+            d = dy[b, i:i + chunk].double()
+            want = r[b] * 1.5 * (d - t0 / n - h * t1 / n)
+            tol = r[b] * 1.5 * (2.0 ** -11 * 1.01 * (a0 + h.abs() * a1) / n + 2.0 ** -20 * (d.abs() + h.abs()))
+            tol = tol + HALF[x.dtype] * (want.abs() + tol)
+            assert ((y[b, i:i + chunk].double() - want).abs() <= tol).all()
+    assert abs(float(out["dshift"][0] - dshift)) <= 2.0 ** -11 * float(sizes)
+    assert abs(float(out["dscale"][0] - dscale)) <= 2.0 ** -11 * 1.01 * float(worst)
