@@ -669,8 +669,11 @@ struct TargetArgs {
   int v0, n;                  // the piece's classes
   void* dz;
   unsigned long long* fixed;  // nullptr: none
+  float* colsum;              // with it: the piece's classes of one of the rows' sums of dz
 };
-// A teacher's elements of a piece of dz, a wave a row.
+// A teacher's elements of a piece of dz, a wave a row.  A share that is not
+// finite (of a logit that is not, or of g) has no whole number: it makes the
+// class's sum of dz NaN, as it is where the two parts of dz are subtracted.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_head_targets(TargetArgs a) {
@@ -690,9 +693,12 @@ k_head_targets(TargetArgs a) {
       if (s.cls[k] < 0 || i < 0 || i >= a.n) continue;
       const float q = s.q[k], d = g * (exp2_of(saved[1 + k] - lse) - q);
       static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
+      if (!a.fixed || q == 0.f) continue;
       const double w = (double)g * (double)q;
-      if (a.fixed && __builtin_isfinite(w))
+      if (__builtin_isfinite(w))
         atomicAdd(a.fixed + a.v0 + i, (unsigned long long)(long long)llrint(ldexp(w, bits)));
+      else
+        a.colsum[i] = __builtin_nanf("");   // all who write here write this
     }
     wave_fence();
   }
@@ -951,7 +957,7 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
     if (s.teacher) {
       TargetArgs a{};
       a.t = targets_of(s, t), a.info = info, a.saved = saved, a.top = top, a.P = s.P, a.ld = l.ld;
-      a.v0 = (int)v0, a.n = (int)n, a.dz = ws + l.dz, a.fixed = fixed;
+      a.v0 = (int)v0, a.n = (int)n, a.dz = ws + l.dz, a.fixed = fixed, a.colsum = cols ? cols + v0 : nullptr;
       hipLaunchKernelGGL(k_head_targets<T>, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
                          (unsigned)(kWaves * s.K * 12), st, a);
       e = hipGetLastError();

@@ -583,3 +583,33 @@ def test_calls_at_once():
     for i in range(2):
         for run in got[i]:
             assert all(torch.equal(a, c) for a, c in zip(run, want[i]))
+
+
+@pytest.mark.parametrize("P,C,V,K,dtype", [(64, 72, 90, 9, F), (64, 72, 90, 9, H), (8192, 64, 20000, 5, H), (9001, 1029, 110, 3, F)])
+@pytest.mark.parametrize("reduction", ["mean", "rows"])
+def test_a_teachers_value_that_is_not_finite_is_in_every_gradient(P, C, V, K, dtype, reduction):
+    """It makes its row's dx NaN, and dweight and dshift of the row's classes; nothing else."""
+    x, w, b, g = make(P, C, V, dtype, seed=23)
+    cls, logits = entries(P, K, V, g)
+    cls[3, 0], cls[3, 1], cls[P - 1, 0] = 0, V - 1, V // 2
+    head = HeadLoss(w, b, reduction=reduction)
+    dloss = upstream(head, P, g)
+    clean = both_teacher(head, x, cls, logits, dloss, 2.0)
+    assert all(t.isfinite().all() for t in clean.values())
+    logits[3, 1], logits[P - 1, 0] = math.nan, math.inf
+    got = both_teacher(head, x, cls, logits, dloss, 2.0)
+    rows = torch.zeros(P, dtype=torch.bool, device="cuda")
+    rows[3] = rows[P - 1] = True
+    classes = torch.zeros(V, dtype=torch.bool, device="cuda")
+    classes[cls[rows].flatten()] = True
+    for n, hit in (("dx", rows), ("dweight", classes), ("dshift", classes)):
+        assert got[n][hit].isnan().all(), n
+        assert torch.equal(got[n][~hit], clean[n][~hit]), n
+    # an upstream gradient that is not finite, of one row
+    if reduction == "rows":
+        logits[3, 1] = logits[P - 1, 0] = 0.5
+        for v in (math.inf, -math.inf, math.nan):
+            up = dloss.clone()
+            up[3] = v
+            got = both_teacher(head, x, cls, logits, up, 2.0)
+            assert not got["dshift"][cls[3]].isfinite().any() and not got["dweight"][cls[3]].isfinite().all(1).any()
