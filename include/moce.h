@@ -512,7 +512,8 @@ size_t moce_group_norm_backward_workspace_bytes(const moce_group_norm_desc* desc
  * scale and shift as in the forward, stats as it wrote them (h and z are formed
  * again).  act' of ReLU is 0 where z <= 0.  dx may be dy or x (in place); no
  * other output, and not ws, may overlap an input or another output.  Sums are
- * float32, their order depends on the descriptor alone.  ws as sized above,
+ * float32 (of dscale and dshift over the images float64), their order depends on
+ * the descriptor alone.  ws as sized above,
  * 256-byte aligned.  Errors: those of moce_group_norm; MOCE_ERR_NULL for a
  * missing dy, stats or grads.  Asynchronous on `stream`. */
 moce_status moce_group_norm_backward(const moce_group_norm_desc* desc, const void* x, const float* scale,

@@ -163,12 +163,14 @@ __device__ __forceinline__ void store_n(T* p, int n, const float (&v)[8]) {
 }
 
 // dscale and dshift of 16 channels: their sums over the images, or (fold) over
-// the images' parts.
-__device__ __forceinline__ void sum_params(const NormArgs& a, int block, float2* s) {
+// the images' parts.  A thread has a sixteenth of them, as many as 2^25, so the
+// sums are float64 (a float32 sum of 65536 equal values a thread, of a million
+// rows, was 6e-4 off; of 2^24 it stops growing).
+__device__ __forceinline__ void sum_params(const NormArgs& a, int block, double2* s) {
   const float2* sums = a.fold ? static_cast<const float2*>(a.parts.p) : a.sums;
   const int64_t n = a.fold ? a.B * a.chunks : a.B;
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = block * 16 + x;
-  float2 t = make_float2(0.f, 0.f);
+  double2 t = make_double2(0., 0.);
   if (c < a.C)
 #pragma unroll 8
     for (int64_t i = y; i < n; i += kThreads / 16) {
@@ -180,8 +182,8 @@ __device__ __forceinline__ void sum_params(const NormArgs& a, int block, float2*
   if (y != 0 || c >= a.C) return;
 #pragma unroll
   for (int i = 1; i < kThreads / 16; ++i) t.x += s[16 * i + x].x, t.y += s[16 * i + x].y;
-  if (a.dshift) a.dshift[c] = t.x;
-  if (a.dscale) a.dscale[c] = t.y;
+  if (a.dshift) a.dshift[c] = (float)t.x;
+  if (a.dscale) a.dscale[c] = (float)t.y;
 }
 
 // ---- channels-last: a thread holds 16 bytes of channels of every `down`-th row of a part ----
@@ -443,9 +445,11 @@ template <typename T, bool WHOLE, bool FOLD>
 __global__ void __launch_bounds__(kThreads, 3)
 k_norm_dx_rows(NormArgs a) {
   constexpr int VE = kVE<T>;
-  __shared__ float2 s[kThreads], groups[kThreads];
+  __shared__ double2 params[kThreads];
+  __shared__ float2 groups[kThreads];
+  float2* s = reinterpret_cast<float2*>(params);
   if ((int)blockIdx.x < a.params) {   // uniform
-    if (blockIdx.y == 0) sum_params(a, blockIdx.x, s);
+    if (blockIdx.y == 0) sum_params(a, blockIdx.x, params);
     return;
   }
   const int down = kThreads / a.tx;
@@ -1138,7 +1142,7 @@ k_norm_dstats(NormArgs a, int down) {
 
 __global__ void __launch_bounds__(kThreads)
 k_norm_dparams(NormArgs a) {
-  __shared__ float2 s[kThreads];
+  __shared__ double2 s[kThreads];
   sum_params(a, blockIdx.x, s);
 }
 

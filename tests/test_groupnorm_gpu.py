@@ -438,3 +438,24 @@ def test_a_plane_of_all_positions_there_can_be(dtype, B, H, W, layout):
             assert ((y[b, i:i + chunk].double() - want).abs() <= tol).all()
     assert abs(float(out["dshift"][0] - dshift)) <= 2.0 ** -11 * float(sizes)
     assert abs(float(out["dscale"][0] - dscale)) <= 2.0 ** -11 * 1.01 * float(worst)
+
+
+@pytest.mark.parametrize("C,G", [(64, 8), (60, 6), (96, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_parameters_of_a_million_rows(dtype, C, G):
+    """dscale and dshift where every row adds a value of the same sign and about the same size.
+
+    A row's dz is dy itself, its h is +-k rstd of float32 (one step of rstd, one of the difference, one of each product:
+    less than 8 x 2^-24 of the value together), and the sum over the rows adds no more than its last rounding, 2^-24."""
+    B = (1 << 20) + 3
+    k = 2.0 ** torch.randint(0, 3, (B, 1), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    x = (k * (1 - 2 * (torch.arange(C, device="cuda") % 2))).to(TYPES[dtype])       # every group's mean is 0
+    dy = torch.full_like(x, 0.1)
+    layer = GroupNormLayer(G, torch.ones(C, device="cuda"), torch.zeros(C, device="cuda"))
+    stats = layer.new_stats(x.shape)
+    layer.forward(x, stats=stats)
+    out = layer.backward(x, dy, stats)
+    one = float(dy[0, 0])
+    assert ((out["dshift"].double() - B * one).abs() <= 2.0 ** -23 * B * one).all()
+    want = one * (x.double() / torch.sqrt(k.double() ** 2 + 1e-5)).sum(0)
+    assert ((out["dscale"].double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
