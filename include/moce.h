@@ -513,9 +513,9 @@ size_t moce_group_norm_backward_workspace_bytes(const moce_group_norm_desc* desc
  * again).  act' of ReLU is 0 where z <= 0.  dx may be dy or x (in place); no
  * other output, and not ws, may overlap an input or another output.  Sums are
  * float32 (of dscale and dshift over the images float64), their order depends on
- * the descriptor alone.  ws as sized above,
- * 256-byte aligned.  Errors: those of moce_group_norm; MOCE_ERR_NULL for a
- * missing dy, stats or grads.  Asynchronous on `stream`. */
+ * the descriptor alone.  ws as sized above, 256-byte aligned.  Errors: those of
+ * moce_group_norm; MOCE_ERR_NULL for a missing dy, stats or grads.
+ * Asynchronous on `stream`. */
 moce_status moce_group_norm_backward(const moce_group_norm_desc* desc, const void* x, const float* scale,
                                      const float* shift, const float* stats, const void* dy,
                                      const moce_group_norm_grads* grads, void* ws, size_t ws_bytes, hipStream_t stream);
@@ -564,19 +564,22 @@ size_t moce_head_saved_floats(const moce_head_desc* desc);
 size_t moce_head_workspace_bytes(const moce_head_desc* desc);
 
 /* The losses.  x: [P][C], weight: [V][C], of the descriptor's type, 16-byte
- * aligned; shift: float32 [V] or NULL (minus infinity takes a class out);
- * labels [P], classes [P][K]: integers of index_bytes; logits: [P][K], of
- * teacher_dtype; loss: float32, as the reduction has it; saved: float32, sized
- * as above, or NULL where no backward follows.  All contiguous; no output, and
- * not ws, may overlap an input or another output.  Sums are float32 (over rows
- * float64), their order depends on the descriptor alone; a logit that is not
- * finite makes its row's loss so.  ws: 256-byte aligned, one for each call that can run
- * at the same time, captured calls that are replayed so too.  Asynchronous on
- * `stream`.  Errors: MOCE_ERR_NULL (desc, x, weight, the targets, loss),
- * MOCE_ERR_SHAPE (a size below 1, K not 1 for labels, index_bytes, reduction,
- * smoothing, temperature, memory that overlaps), MOCE_ERR_DTYPE,
- * MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE; MOCE_ERR_UNSUPPORTED
- * when P exceeds 2^24, C or V 2^20, K 1024, V C 2^35, P V 2^35 or P C 2^33. */
+ * aligned; shift: float32 [V] or NULL; labels [P], classes [P][K]: integers of
+ * index_bytes; logits: [P][K], of teacher_dtype; loss: float32, as the reduction
+ * has it; saved: float32, sized as above, or NULL where no backward follows.
+ * All contiguous; no output, and not ws, may overlap an input or another output.
+ * Sums are float32 (over rows float64), their order depends on the descriptor
+ * alone; a row's loss that they leave below 0 is 0.  A logit of minus infinity
+ * (by its shift) takes the class out, of smoothed labels and as a target's the
+ * loss is infinite; one of plus infinity or NaN makes its row's loss NaN, and so
+ * does a teacher's that counts.  ws: 256-byte aligned, one for each call that
+ * can run at the same time, captured calls that are replayed so too.
+ * Asynchronous on `stream`.  Errors: MOCE_ERR_NULL (desc, x, weight, the
+ * targets, loss), MOCE_ERR_SHAPE (a size below 1, K not 1 for labels,
+ * index_bytes, reduction, smoothing, temperature, memory that overlaps),
+ * MOCE_ERR_DTYPE, MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE, MOCE_ERR_DEVICE;
+ * MOCE_ERR_UNSUPPORTED when P exceeds 2^24, C or V 2^20, K 1024, V C 2^35, P V
+ * 2^35 or P C 2^33. */
 moce_status moce_head_cross_entropy(const moce_head_desc* desc, const void* x, const void* weight, const float* shift,
                                     const void* labels, float* loss, float* saved, void* ws, size_t ws_bytes,
                                     hipStream_t stream);

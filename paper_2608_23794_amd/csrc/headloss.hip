@@ -301,6 +301,11 @@ __device__ __forceinline__ bool take_targets(const Targets& t, int64_t p, const 
 
 // ---- the forward's rows ----------------------------------------------------------
 
+// A row's loss: both are at least 0, but the two logarithms that one is the
+// difference of are rounded apart, and a target's logit is a sum of its own.
+// (NaN stays.)
+__device__ __forceinline__ float not_below_0(float l) { return l < 0.f ? 0.f : l; }
+
 struct RowsArgs {
   Targets t;
   const void *x, *w;
@@ -486,7 +491,7 @@ k_head_rows(RowsArgs a) {
       if (a.sums && a.smoothing > 0.f) l += a.smoothing * (lse - sum / (float)a.t.V * a.t.c1);
     }
     if (lane == 0) {
-      a.rows[p] = l * a.factor;
+      a.rows[p] = not_below_0(l) * a.factor;
       a.code[p] = 1.f;
       if (saved) saved[0] = lse;
     }
@@ -567,7 +572,7 @@ k_head_logits(RowsArgs a, const float* __restrict__ logits) {
     loss = wave_sum(loss);
     if (lane == 0) {
       if (!TEACHER && a.smoothing > 0.f) loss += a.smoothing * (lse - sum / (float)V * a.t.c1);
-      a.rows[p] = loss * a.factor;
+      a.rows[p] = not_below_0(loss) * a.factor;
       a.code[p] = 1.f;
       if (saved) saved[0] = lse;
     }

@@ -613,3 +613,29 @@ def test_a_teachers_value_that_is_not_finite_is_in_every_gradient(P, C, V, K, dt
             up[3] = v
             got = both_teacher(head, x, cls, logits, up, 2.0)
             assert not got["dshift"][cls[3]].isfinite().any() and not got["dweight"][cls[3]].isfinite().all(1).any()
+
+
+@pytest.mark.parametrize("P,C,V,dtype", [(3000, 96, 300, F), (3000, 96, 300, H), (40000, 872, 16, F), (70000, 520, 20, H)])
+def test_losses_are_not_below_zero(P, C, V, dtype):
+    """Labels that have all of the probability, and a teacher whose logits are the head's."""
+    x, w, b, g = make(P, C, V, dtype, seed=27, spread=32.0)
+    z = torch.matmul(x.float(), w.float().t()) + b
+    top = z.argmax(1)
+    head = HeadLoss(w, b, reduction="rows")
+    zero = torch.zeros(P, device="cuda")
+    for smoothing in (0.0, 0.1):
+        loss = head.cross_entropy(x, top, smoothing)
+        target, there = label_target(top, V, smoothing)
+        check({"loss": loss}, *reference(x, w, b, target, there, 1.0, zero, False, False))
+        assert float(loss.min()) >= 0.0
+    K = min(V, 64)
+    cls = torch.arange(K, device="cuda").expand(P, K).contiguous()
+    small = HeadLoss(w[:K].contiguous(), b[:K].contiguous(), reduction="rows")
+    loss = small.distill(x, cls, z[:, :K].contiguous(), 1.0)
+    assert float(loss.min()) >= 0.0
+    # infinities and NaN stay: a label whose class is taken out, a row that is not finite
+    out = b.clone()
+    out[top[0]] = -math.inf
+    x[1] = math.nan
+    loss = HeadLoss(w, out, reduction="rows").cross_entropy(x, top)
+    assert float(loss[0]) == math.inf and bool(loss[1].isnan())
