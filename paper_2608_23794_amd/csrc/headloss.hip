@@ -17,7 +17,10 @@
 // are kept in float32 from piece to piece) and dweight.  8 P V C operations in all, bound by the matrix cores
 // where C and P are large.
 //
-// Logits are taken in base 2: u = (z + shift) log2(e) / T.
+// Logits are taken in base 2: u = (z + shift) log2(e) / T, the same 32 bits in
+// the forward and the backward (a logit's sum goes in the same order in every
+// tile): where u is large, what a softmax is of are differences of a few steps
+// of it, and u less a row's lse is above 0 nowhere.
 #include "product.h"
 
 namespace moce {
@@ -65,6 +68,12 @@ struct HeadArgs : GemmArgs {
 };
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+// u, rounded: in one step with the subtraction behind it, the backward's was not the forward's
+// (logits of 2^31: infinite probabilities).
+__device__ __forceinline__ float exponent(float z, float c1) {
+#pragma clang fp contract(off)
+  return z * c1;
+}
 
 // Maximum and sum of 2^(u - maximum); the maximum of nothing is -inf, its sum 0.
 struct Soft {
@@ -112,7 +121,7 @@ struct HeadStats {
         for (int e = 0; e < 4; ++e) {
           const float z = acc[i][j][e] + sh[j][e];
           total += in[j][e] ? z : 0.f;
-          u[j][e] = in[j][e] ? z * g.c1 : -INFINITY;
+          u[j][e] = in[j][e] ? exponent(z, g.c1) : -INFINITY;
           m = fmaxf(m, u[j][e]);
         }
       m = fmaxf(m, __shfl_xor(m, 16, kWave));
@@ -202,7 +211,7 @@ struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[b][i] = exp2_of((v[b][i] + sh[i]) * h.c1 - lse[b]) - h.even;
+          for (int i = 0; i < 8; ++i) v[b][i] = exp2_of(exponent(v[b][i] + sh[i], h.c1) - lse[b]) - h.even;
           if (__any((unsigned)label[b] < 8u)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[b][i] -= label[b] == i ? h.label : 0.f;
@@ -545,7 +554,7 @@ k_head_logits(RowsArgs a, const float* __restrict__ logits) {
 #pragma unroll
       for (int i = 0; i < kAt; ++i) {
         sum += v + i * kWave < V ? u[i] : 0.f;
-        u[i] *= a.t.c1;
+        u[i] = exponent(u[i], a.t.c1);
         top = fmaxf(top, u[i]);
       }
 #pragma unroll
@@ -562,7 +571,7 @@ k_head_logits(RowsArgs a, const float* __restrict__ logits) {
     for (int k = lane; k < K; k += kWave) {
       const int i = s.cls[k];
       if (i < 0) continue;
-      const float q = s.q[k], u = (z[i] + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
+      const float q = s.q[k], u = exponent(z[i] + (a.shift ? a.shift[i] : 0.f), a.t.c1);
       if constexpr (TEACHER)
         loss += q == 0.f ? 0.f : q * (log2f(q) - u + lse);
       else
@@ -676,7 +685,10 @@ struct TargetArgs {
   unsigned long long* fixed;  // nullptr: none
   float* colsum;              // with it: the piece's classes of one of the rows' sums of dz
 };
-// A teacher's elements of a piece of dz, a wave a row.  A share that is not
+// A teacher's elements of a piece of dz, a wave a row, from the logits that the
+// forward took by dot products: g p lost digits to its rounding where p - q has
+// none to spare.  Of p no more is taken from them than that rounding left open,
+// since the other probabilities of the row are those of the tiles' sums.  A share that is not
 // finite (of a logit that is not, or of g) has no whole number: it makes the
 // class's sum of dz NaN, as it is where the two parts of dz are subtracted.
 template <typename T>
@@ -696,8 +708,13 @@ k_head_targets(TargetArgs a) {
     for (int k = lane; k < a.t.K; k += kWave) {
       const int i = s.cls[k] - a.v0;
       if (s.cls[k] < 0 || i < 0 || i >= a.n) continue;
-      const float q = s.q[k], d = g * (exp2_of(saved[1 + k] - lse) - q);
-      static_cast<T*>(a.dz)[p * a.ld + i] = Elem<T>::from_f(d);
+      T* dz = static_cast<T*>(a.dz) + p * a.ld + i;
+      const float q = s.q[k], tile = Elem<T>::to_f(*dz) / g;
+      constexpr float kOpen = sizeof(T) == 2 ? 0x1p-8f : 0x1p-22f;   // half a step of bfloat16; float32: the division's too
+      float prob = exp2_of(saved[1 + k] - lse);
+      const float least = tile * (1.f - kOpen), most = fminf(tile * (1.f + kOpen), 1.f);
+      prob = prob < least ? least : prob > most ? most : prob;
+      *dz = Elem<T>::from_f(g * (prob - q));
       if (!a.fixed || q == 0.f) continue;
       const double w = (double)g * (double)q;
       if (__builtin_isfinite(w))

@@ -639,3 +639,50 @@ def test_losses_are_not_below_zero(P, C, V, dtype):
     x[1] = math.nan
     loss = HeadLoss(w, out, reduction="rows").cross_entropy(x, top)
     assert float(loss[0]) == math.inf and bool(loss[1].isnan())
+
+
+@pytest.mark.parametrize("P,C,V,K,dtype", [
+    (70, 64, 300, 5, F), (70, 64, 300, 5, H), (33, 41, 130, 3, F), (33, 41, 130, 3, H), (300, 541, 2050, 9, H),
+    (8192, 64, 20000, 4, H), (9000, 24, 8000, 2, F), (9001, 1029, 110, 3, F), (70000, 520, 20, 3, H),
+])
+def test_logits_far_apart(P, C, V, K, dtype):
+    """A softmax of values that are more than 2^8 float32 steps of themselves apart has one class, and its gradient is
+    the difference of two classes: exactly for labels, to the rounding of an element of dz for a teacher."""
+    x, w, b, g = make(P, C, V, dtype, seed=33)
+    xd, wd = x.double(), w.double()
+    z = torch.matmul(xd, wd.t().contiguous())
+    two = z.topk(2, 1)
+    size = torch.matmul(xd.abs(), wd.abs().t().contiguous()).max(1)[0]
+    # logits are off by C + 8 steps of 2^-24 of their sizes' sum; 2^-30 times 2^40 parts what they leave by 2^10
+    there = two.values[:, 0] - two.values[:, 1] > (2 * (C + 8) * 2.0 ** -24 + 2.0 ** -22) * size
+    there[::7] = False
+    assert int(there.sum()) > P // 3
+    top = two.indices[:, 0]
+    other = torch.randint(0, V, (P,), generator=g, device="cuda")
+    label = torch.where(torch.arange(P, device="cuda") % 2 == 0, top, other)
+    ones = torch.zeros(P, V, dtype=torch.float64, device="cuda")
+    p = ones.scatter(1, top[:, None], 1.0)
+    q = ones.scatter(1, label[:, None], 1.0)
+    dloss = torch.rand(P, generator=g, device="cuda") + 0.5
+    far = (w.double() * 2.0 ** 40).to(dtype)       # a power of two: the same logits, 2^40 times
+    got = both(HeadLoss(far, None, reduction="rows"), x, torch.where(there, label, -1), dloss)
+    dz = (p - q) * (dloss.double() * there)[:, None]
+    cls = torch.stack([label] + [top] * (K - 1), 1).contiguous()
+    logits = torch.zeros(P, K, device="cuda")
+    logits[:, 0] = 4.0
+    cls = torch.where(there[:, None], cls, -1)
+    soft = both_teacher(HeadLoss(w, None, reduction="rows"), x, cls, logits, dloss, 2.0 ** -40)
+    # Half steps of the type: g p rounded by the tile, what is left open around it, an element of dz, the result: four
+    # at most (a label's dz, the result: two), and a few steps of float32 for its sums and exponentials.  A teacher's p
+    # loses its two whether or not q then takes it away: its share of the sizes is p + q, not |p - q|.
+    e = {F: 2.0 ** -21, H: 4 * 2.0 ** -8}[dtype]
+    apart = (p + q) * (dloss.double() * there)[:, None]
+    for out, scale, factor, s in ((got, 1.0, 2.0 ** 40, dz.abs()), (soft, 2.0 ** -40, 1.0, apart)):
+        want = {"dx": torch.matmul(dz, wd * factor), "dweight": torch.matmul(dz.t().contiguous(), xd), "dshift": dz.sum(0)}
+        sizes = {"dx": torch.matmul(s, wd.abs() * factor), "dweight": torch.matmul(s.t().contiguous(), xd.abs())}
+        for n in sizes:
+            d = (out[n].double() / scale - want[n]).abs()
+            assert (d <= (e + (P + 8) * 2.0 ** -24) * 1.01 * sizes[n] + 1e-30).all(), (n, float((d / sizes[n]).nan_to_num().max()))
+        assert all(t.isfinite().all() for t in out.values())
+    same = (label == top) | ~there
+    assert float(got["dx"][same].abs().max()) == 0.0
