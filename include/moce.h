@@ -551,7 +551,7 @@ typedef struct moce_head_desc {
     int32_t reduction;      /* MOCE_LOSS_ROWS: loss[P]; MOCE_LOSS_MEAN: loss[1], the mean over the
                              * rows that are not left out (0 where all are) */
     float smoothing;        /* e in [0, 1] (not read by the distillation) */
-    float temperature;      /* T, finite, > 0 (not read by the cross entropy) */
+    float temperature;      /* T, 2^-62 to 2^62 (not read by the cross entropy) */
     int32_t reserved;       /* set to 0 */
 } moce_head_desc;
 

@@ -798,7 +798,8 @@ moce_status check_head(const moce_head_desc* d, bool teacher, moce::HeadShape* s
   if (d->reduction != MOCE_LOSS_ROWS && d->reduction != MOCE_LOSS_MEAN) return MOCE_ERR_SHAPE;
   if (d->dtype != MOCE_F32 && d->dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
   if (teacher) {
-    if (!std::isfinite(d->temperature) || !(d->temperature > 0.f)) return MOCE_ERR_SHAPE;
+    // log2(e) / T and T^2 are then normal float32 numbers
+    if (!(d->temperature >= 0x1p-62f && d->temperature <= 0x1p62f)) return MOCE_ERR_SHAPE;
     if (d->teacher_dtype != MOCE_F32 && d->teacher_dtype != MOCE_BF16) return MOCE_ERR_DTYPE;
   } else if (!(d->smoothing >= 0.f && d->smoothing <= 1.f)) {
     return MOCE_ERR_SHAPE;

@@ -584,7 +584,7 @@ class HeadLoss:
             desc = self.desc(x.shape, 1, classes.dtype, smoothing=smoothing)
             _need("labels", classes, rows, classes.dtype, self.device)
         else:
-            if not (math.isfinite(temperature) and temperature > 0.0):
+            if not 2.0 ** -62 <= temperature <= 2.0 ** 62:
                 raise ValueError(f"temperature {temperature}")
             if classes.dim() != len(rows) + 1 or classes.shape[-1] < 1 or logits.dtype not in _DTYPE_OF:
                 raise ValueError(f"classes and logits have to be [..., K], logits of float32 or bfloat16, got "
@@ -669,7 +669,8 @@ class HeadLoss:
     def distill(self, x: torch.Tensor, classes: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0,
                 saved: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
         """moce_head_distill: the loss against a teacher's K logits a row, [..., K] (float32 or bfloat16), and their
-        classes (int32 or int64).  saved (new_saved), where given, receives what the backward needs."""
+        classes (int32 or int64); temperature: 2^-62 to 2^62.  saved (new_saved), where given, receives what the
+        backward needs."""
         return self._forward(x, classes, logits, 0.0, temperature, saved, ws)
 
     def distill_backward(self, x: torch.Tensor, classes: torch.Tensor, logits: torch.Tensor, saved: torch.Tensor,

@@ -686,3 +686,19 @@ def test_logits_far_apart(P, C, V, K, dtype):
         assert all(t.isfinite().all() for t in out.values())
     same = (label == top) | ~there
     assert float(got["dx"][same].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("T", [2.0 ** -62, 2.0 ** 62])
+def test_temperatures_at_their_ends(T):
+    P, C, V, K = 40, 24, 60, 5
+    for dtype in (F, H):
+        x, w, b, g = make(P, C, V, dtype, seed=29)
+        cls, logits = entries(P, K, V, g, dtype)
+        head = HeadLoss(w, b, reduction="rows")
+        got = both_teacher(head, x, cls, logits, torch.ones(P, device="cuda") / P, T)
+        target, there = teacher_target(cls, logits, V, T)
+        want, tol = reference(x, w, b, target, there, T, torch.ones(P, device="cuda") / P, False, True)
+        # the teacher's exponents too are off by 2^-22 of themselves; where they are far apart none has a share but the first
+        tol["loss"] = tol["loss"] + (T * T * 2.0 ** -20 * math.log(V) if T > 1 else 0.0)
+        check({"loss": got["loss"]}, want, tol)
+        assert all(t.isfinite().all() for t in got.values())

@@ -182,3 +182,14 @@ def test_head_overlaps():
                 assert head_backward(d, teacher, **{out: PLACE[name]}) == -2
         assert head_backward(d, teacher, dx=PLACE["dweight"]) == -2
         assert head_backward(d, teacher, ws=PLACE["dshift"]) == -2
+
+
+def test_temperatures_at_their_ends(lib):
+    """A temperature whose square or inverse is no normal float32 number would lose the loss; those at the ends count."""
+    for t in (2.0 ** -63, 2.0 ** 62.01, 1e-38, 1e38):
+        d = head_desc(temperature=t, K=5)
+        assert head(d, True) == -2 and head_backward(d, True) == -2
+        assert lib.moce_head_workspace_bytes(ctypes.byref(d)) == 0
+    for t in (2.0 ** -62, 2.0 ** 62):
+        d = head_desc(temperature=t, K=5)
+        assert lib.moce_head_workspace_bytes(ctypes.byref(d)) > 0 and head(d, True, n=0) == -7
