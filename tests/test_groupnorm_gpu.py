@@ -459,3 +459,43 @@ def test_parameters_of_a_million_rows(dtype, C, G):
     assert ((out["dshift"].double() - B * one).abs() <= 2.0 ** -23 * B * one).all()
     want = one * (x.double() / torch.sqrt(k.double() ** 2 + 1e-5)).sum(0)
     assert ((out["dscale"].double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
+
+
+# Even numbers of positions; of as many elements a group that one more or less would show.
+EXACT = [
+    (2, 64, 8, 7, 8), (3, 16, 4, 12, 10), (4, 512, 32, 14, 14), (2, 256, 32, 100, 90), (1, 64, 8, 120, 100),
+    (1, 64, 8, 200, 100), (2, 330, 11, 30, 32), (1, 128, 128, 300, 300), (5, 768, 1, 2, 1), (40, 96, 12, 64, 64),
+]
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", EXACT)
+def test_statistics_of_whole_numbers(shape, dtype, layout):
+    """Channels of +-1, +-2 and +-3, the sign turning with the position: mean 0, and all sums of one thread are exact.
+
+    What is off is what joins add.  A join of two counts, means and squared deviations loses at most 8 x 2^-24 of what
+    it adds (a reciprocal, a difference, products) and one rounding, 2^-24, of each sum that it holds; a chain of n of
+    them (8 + 2 n) 2^-24 of the squares, half of that of rstd.  Means, of at most 3 in size, each lose a rounding and
+    the products' few, on weights 1 / 2, 1 / 3, ..: less than (n + 32) 2^-24 of 3.  The longest chains: 256 threads over the
+    16-byte vectors of at most 32 across, channels-last; 6 steps of a wave's lanes, channels-first."""
+    B, C, G, H, W = shape
+    ve = 4 if dtype == "f32" else 8
+    across = 1
+    while across < 32 and across * ve < C:
+        across *= 2
+    joins = 256 // across if layout == "nhwc" else 6
+    n = C // G * H * W
+    tol = (joins + 8) * 2.0 ** -24
+    assert tol < 0.5 / n, "a count that is off by one shows"
+    size = 1.0 + torch.arange(C, device="cuda") % 3
+    sign = 1.0 - 2.0 * (torch.arange(H * W, device="cuda") % 2)
+    x = size[:, None] * sign
+    x = x.reshape(1, C, H, W) if layout == "nchw" else x.t().reshape(1, H, W, C)
+    x = x.expand(B, *x.shape[1:]).to(TYPES[dtype]).contiguous()
+    layer = GroupNormLayer(G, layout=layout)
+    stats = layer.new_stats(x.shape)
+    layer.forward(x, stats=stats)
+    rstd = 1 / torch.sqrt((size.double() ** 2).reshape(G, -1).mean(1) + 1e-5)
+    assert (stats[0].abs() <= 3 * (joins + 32) * 2.0 ** -24).all()
+    assert ((stats[1].double() / rstd - 1).abs() <= tol).all()
