@@ -481,11 +481,13 @@ size_t moce_group_norm_workspace_bytes(const moce_group_norm_desc* desc);
 /* The normalisation.  x, y: contiguous, 16-byte aligned; scale, shift: float32
  * [C]; stats (optional): float32 [2][B][G], the means, then the rstd, which the
  * backward reads.  y is fully overwritten and may be x (in place); nothing else
- * may overlap.  Sums are float32 about values of the group, so that a mean that
- * is large against the deviation costs no digits of it; their order depends on
- * the descriptor alone.  A NaN or infinity makes its group NaN, and no other.
- * ws: as sized above, 256-byte aligned; calls that can run at the same time
- * need one each, captured calls that are replayed so too.  Asynchronous on
+ * may overlap.  Sums are float32, squares of deviations from a value of the
+ * group or its mean, so that a mean that is large against the deviation costs no
+ * digits of it (a sum of a group's values, or a square, past float32's range is
+ * infinite); their order depends on the descriptor alone.  A NaN or infinity
+ * makes its group NaN, and no other.  ws: as sized above, 256-byte aligned;
+ * calls that can run at the same time need one each, captured calls that are
+ * replayed so too.  Asynchronous on
  * `stream`.  Errors: MOCE_ERR_NULL (desc, x, y), MOCE_ERR_SHAPE (a size below
  * 1, C not a multiple of G, an unknown act, eps, memory that overlaps),
  * MOCE_ERR_DTYPE, MOCE_ERR_LAYOUT, MOCE_ERR_ALIGN, MOCE_ERR_WORKSPACE,
@@ -606,11 +608,11 @@ size_t moce_head_backward_workspace_bytes(const moce_head_desc* desc);
 
 /* The gradients.  The inputs as in the forward, saved as it wrote them; dloss:
  * float32 [P], or [1] for MOCE_LOSS_MEAN.  For bfloat16, dz enters the products
- * rounded to its type relative to the largest |g|; sums are float32, and dshift
- * takes dz as it is (of a teacher, a row of less than 2^-35 of the largest |g|
- * may not show in it).  Rows that are left out may hold anything, NaN too.  ws and errors as for the
- * forward; MOCE_ERR_NULL for a missing saved, dloss or grads.  Asynchronous on
- * `stream`. */
+ * rounded to its type relative to the largest |g| (for float32 as it is); sums
+ * are float32, and dshift takes dz as it is (of a teacher, a row of less than
+ * 2^-35 of the largest |g| may not show in it).  Rows that are left out may hold
+ * anything, NaN too.  ws and errors as for the forward; MOCE_ERR_NULL for a
+ * missing saved, dloss or grads.  Asynchronous on `stream`. */
 moce_status moce_head_cross_entropy_backward(const moce_head_desc* desc, const void* x, const void* weight,
                                              const float* shift, const void* labels, const float* saved,
                                              const float* dloss, const moce_head_grads* grads, void* ws,

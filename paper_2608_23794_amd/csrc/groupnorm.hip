@@ -494,6 +494,10 @@ k_norm_dx_rows(NormArgs a) {
 }
 
 // ---- channels-first: tx lanes take a plane's part, eight positions each ------------
+//
+// Bound by memory, one load in flight a lane: two maps of 128 channels at 512 x
+// 384 with SiLU, bfloat16 (101 MB a tensor) 66 us and their gradients 116,
+// float32 157 and 240.
 
 // f(image, channel, part, the lane's first position, positions from it to the
 // part's end, none where that is not above 0) for the planes' parts of the

@@ -14,8 +14,8 @@
 // rows for dshift.  A label's element has its part taken off there; a teacher's
 // k_head_targets puts right (from float32 values too, so that p - q loses no
 // digits).  A piece then goes through the products of dx (whose partial sums
-// are kept in float32 from piece to piece) and dweight.  8 P V C operations in all, bound by the matrix cores
-// where C and P are large.
+// are kept in float32 from piece to piece) and dweight.  8 P V C operations in
+// all, 6 with the logits kept; bound by the matrix cores where C and P are large.
 //
 // Logits are taken in base 2: u = (z + shift) log2(e) / T, the same 32 bits in
 // the forward and the backward (a logit's sum goes in the same order in every
@@ -86,7 +86,7 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
 }
 
 // ---- forward epilogue ------------------------------------------------------------
-// Bound by the products: 8192 rows of 4096 by 65536 classes in 3.28 ms, 1340
+// Bound by the products: 8192 rows of 4096 by 65536 classes in 3.24 ms, 1359
 // TFLOP/s (a library product that writes its results: 1457); 3152 of 768 by
 // 21841, twelve stages between the ends of a tile, 137 us, 772.
 // A lane holds 4 FC classes of each of its FR rows; four lanes share a row's
@@ -164,12 +164,16 @@ struct HeadStats {
 // ---- backward epilogue -----------------------------------------------------------
 // Eight classes a lane, in rows, as Finish has them: g / G (2^(u - lse) - e / V),
 // less a label's part (a teacher's is k_head_targets'), zeros behind the classes
-// to the end of the line.  G, the largest |g|, comes
-// in behind the products: with it, equal weights of the rows are 1, and a
-// label's element, near -1, is rounded by its own small rest; within dz, the
-// rounding of g would be one factor of all rows' gradients (dx and dweight of
-// 8192 rows and 65536 classes were 3.3e-3 off in the 2-norm, not 1.7e-3).  The
-// pieces of those take 3.42 ms, 5% more than the forward, which has no dz.
+// to the end of the line.  dz is rounded to the operands' type, which is what
+// the matrix cores take beside the weight and x: in bfloat16, dx and dweight are
+// 2.3e-3 off in the 2-norm for spread targets, 1.66e-3 of it their own rounding;
+// two parts of bfloat16 would double the products dx and dweight, half of a
+// step's time.  G, the largest |g|, comes in behind the products: with it, equal
+// weights of the rows are 1, and a label's element, near -1, is rounded by its
+// own small rest; within dz, the rounding of g would be one factor of all rows'
+// gradients (dx and dweight of 8192 rows and 65536 classes were 3.3e-3 off in
+// the 2-norm, not 1.7e-3).  The pieces of those take 3.40 ms, 5% more than the
+// forward's 3.24, which has no dz.
 template <typename T, int BYTES, int FR, int FC, int WR, int WC>
 struct HeadGradient : Finish<T, BYTES, FR, FC, WR, WC> {
   using F = Finish<T, BYTES, FR, FC, WR, WC>;
@@ -688,9 +692,10 @@ struct TargetArgs {
 // A teacher's elements of a piece of dz, a wave a row, from the logits that the
 // forward took by dot products: g p lost digits to its rounding where p - q has
 // none to spare.  Of p no more is taken from them than that rounding left open,
-// since the other probabilities of the row are those of the tiles' sums.  A share that is not
-// finite (of a logit that is not, or of g) has no whole number: it makes the
-// class's sum of dz NaN, as it is where the two parts of dz are subtracted.
+// since the other probabilities of the row are those of the tiles' sums.  A
+// share that is not finite (of a logit that is not, or of g) has no whole number:
+// it makes the class's sum of dz NaN, as it is where the two parts of dz are
+// subtracted.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_head_targets(TargetArgs a) {
@@ -979,7 +984,8 @@ hipError_t backward(const HeadShape& s, const void* x, const void* w, const floa
     if (s.teacher) {
       TargetArgs a{};
       a.t = targets_of(s, t), a.info = info, a.saved = saved, a.top = top, a.P = s.P, a.ld = l.ld;
-      a.v0 = (int)v0, a.n = (int)n, a.dz = ws + l.dz, a.fixed = fixed, a.colsum = cols ? cols + v0 : nullptr;
+      a.v0 = (int)v0, a.n = (int)n, a.dz = ws + l.dz;
+      a.fixed = fixed, a.colsum = cols ? cols + v0 : nullptr;
       hipLaunchKernelGGL(k_head_targets<T>, dim3((unsigned)std::min(ceil_div(s.P, kWaves), kMaxBlocks)), dim3(kThreads),
                          (unsigned)(kWaves * s.K * 12), st, a);
       e = hipGetLastError();
