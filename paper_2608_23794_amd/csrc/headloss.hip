@@ -499,7 +499,7 @@ k_head_rows(RowsArgs a) {
       const int i = s.cls[0];
       const float d = dot_row<T, kWave>(x, static_cast<const T*>(a.w) + (int64_t)i * a.C, a.C, lane);
       const float z = (d + (a.shift ? a.shift[i] : 0.f)) * a.t.c1;
-      l = (lse - z) * s.q[0];
+      l = s.q[0] == 0.f ? 0.f : (lse - z) * s.q[0];   // fully smoothed: z may be infinite
       if (saved && lane == 0) saved[1] = z;
       if (a.sums && a.smoothing > 0.f) l += a.smoothing * (lse - sum / (float)a.t.V * a.t.c1);
     }
@@ -579,7 +579,7 @@ k_head_logits(RowsArgs a, const float* __restrict__ logits) {
       if constexpr (TEACHER)
         loss += q == 0.f ? 0.f : q * (log2f(q) - u + lse);
       else
-        loss = (lse - u) * q;
+        loss = q == 0.f ? 0.f : (lse - u) * q;
       if (saved) saved[1 + k] = u;
     }
     loss = wave_sum(loss);

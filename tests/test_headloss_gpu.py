@@ -702,3 +702,21 @@ def test_temperatures_at_their_ends(T):
         tol["loss"] = tol["loss"] + (T * T * 2.0 ** -20 * math.log(V) if T > 1 else 0.0)
         check({"loss": got["loss"]}, want, tol)
         assert all(t.isfinite().all() for t in got.values())
+
+
+@pytest.mark.parametrize("P,C,V,dtype", [(50, 40, 33, F), (50, 40, 33, H), (40000, 872, 16, F)])
+@pytest.mark.parametrize("smoothing", [0.1, 1.0])
+def test_a_class_taken_out_of_smoothed_labels(P, C, V, dtype, smoothing):
+    """The loss is infinite, whether or not the class is the label; the gradients are those of the other classes."""
+    x, w, b, g = make(P, C, V, dtype, seed=37)
+    b[3] = -math.inf
+    labels = torch.randint(0, V, (P,), generator=g, device="cuda")
+    labels[::9], labels[1] = 3, -1
+    head = HeadLoss(w, b, reduction="rows")
+    dloss = torch.rand(P, generator=g, device="cuda")
+    got = both(head, x, labels, dloss, smoothing)
+    there = labels >= 0
+    assert (got["loss"][there] == math.inf).all() and float(got["loss"][1]) == 0.0
+    target, _ = label_target(labels, V, smoothing)
+    want, tol = reference(x, w, b, target, there, 1.0, dloss, False, False)
+    check({n: got[n] for n in ("dx", "dweight", "dshift")}, want, tol)
